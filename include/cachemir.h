@@ -36,8 +36,8 @@
  *  - A context's scratch arena is shared by all calls on it: calls on one context must not
  *    overlap in time (enqueue them on one stream, or order the streams).  A plan, a cache and
  *    a rotary-embedding object each hold one work area of their own with the same rule.
- *  - The hot calls (cm_rotate*, cm_vmm_pt*, cm_vmm_kv, cm_kv_append, cm_rope_apply and the
- *    element-wise ones) allocate nothing and only enqueue kernels and device copies once the
+ *  - The hot calls (cm_rotate*, cm_vmm_pt*, cm_vmm_kv, cm_kv_append, cm_kv_fork, cm_kv_take, cm_rope_apply, cm_relbias_apply
+ *    and the element-wise ones) allocate nothing and only enqueue kernels and device copies once the
  *    per-level tables exist (the first call at a level builds them), so they can be captured
  *    into a HIP graph after one eager call.
  */
@@ -331,6 +331,13 @@ int32_t cm_kv_tokens(const cm_kv *kv);
 cm_status cm_kv_load(cm_ctx *ctx, cm_kv *kv, int32_t which, int32_t idx, const cm_ct *ct,
                      void *stream);
 cm_status cm_kv_set_tokens(cm_kv *kv, int32_t ntok);
+/* Where the next append goes (0 <= token <= max_tokens): a place whose tokens have been dropped (cm_kv_take), so that a cache
+ * can be used as a ring.  Appends add onto what is stored: the place has to be empty.  cm_kv_tokens stays one past the highest
+ * place ever filled, and is what query-times-K covers.  cm_kv_set_tokens, cm_kv_take and cm_kv_fork set the place anew. */
+cm_status cm_kv_seek(cm_kv *kv, int32_t token);
+/* Descriptor of a cache ciphertext where it lies (`which` and idx as in cm_kv_load): device memory of the cache, valid until
+ * the cache is destroyed.  Index ciphertext g r_i + j is stored at place j r_o + g, the others in their order. */
+cm_status cm_kv_view(const cm_kv *kv, int32_t which, int32_t idx, cm_ct *out);
 cm_status cm_kv_export(cm_ctx *ctx, const cm_kv *kv, int32_t which, int32_t idx, uint64_t *out);
 /* Every mask the cache uses is a slot rotation of one of three base masks, applied as the
  * Galois permutation of the encoded base.  This replaces a base by given integer coefficients
@@ -360,6 +367,40 @@ cm_status cm_kv_append_group(cm_ctx *ctx, const cm_evk *evk, cm_kv *kv, const cm
  * CM_QK_GROUP / CM_SV_GROUP: the same levels; no keys for the residue rotations are needed. */
 cm_status cm_vmm_kv(cm_ctx *ctx, const cm_evk *evk, const cm_kv *kv, int32_t which,
                     const cm_ct *in, cm_ct *out, void *stream);
+
+/* ---- pages of a cache: copying, forking, freeing, moving ------------------------------------------------
+ * A page is the t tokens c t .. c t + t - 1 (t = S / (heads dim), heads padded): one K ciphertext, one row of every V and
+ * index ciphertext.  These calls only enqueue kernels on `stream`; what they set on the host (token count, place of the next
+ * append, scale) is set when they return.  Caches of one call share heads, dim, r_i and CM_KV_KEY_INDEX (else CM_E_LAYOUT);
+ * the other flags may differ. */
+/* Copies of a cache: beams, drafts, a prompt that several continuations share.  dsts: 1 or more different caches other than
+ * src (else CM_E_INVAL), each at a level of its own up to src's (else CM_E_LEVEL; a copy at a lower level is a level drop) and
+ * with room for its tokens (else CM_E_LAYOUT).  What a dst held is replaced; its pages behind the last token are cleared. */
+cm_status cm_kv_fork(cm_ctx *ctx, const cm_kv *src, cm_kv *const *dsts, int32_t ndst, void *stream);
+/* Which tokens of a cache are kept, and where they go.  keep: host, ntok bytes, non-zero = kept; shift: every kept page c goes to
+ * page c + shift, |shift| < dim, which has to lie in 0 .. dim - 1 (else CM_E_LAYOUT).  Made for caches of the shape and level of
+ * `like` (its tokens are not read), level >= 3 (else CM_E_LEVEL); usable for all of them (the caches of a model's layers).
+ * The masks are encoded at the scale of the prime that the rescale removes.  coeffs (nullable, host [1 + p][n]): their integer
+ * coefficients, for callers that need bit-identical plaintexts on two implementations: first the kept tokens in the layout of
+ * the scores (slots (c, h, tau) of token c t + tau), then, for every different pattern of kept residues among the pages that
+ * keep some but not all of their tokens, in the order of their first page, the slots (e, h, tau) of its residues.  Without a
+ * kept token none is read.  The object holds 1 + p plaintexts of level + 1 limbs. */
+typedef struct cm_kv_sel cm_kv_sel;
+cm_status cm_kv_sel_create(cm_ctx *ctx, const cm_kv *like, const uint8_t *keep, int32_t ntok, int32_t shift,
+                           const int64_t *coeffs, cm_kv_sel **out);
+void cm_kv_sel_destroy(cm_kv_sel *sel);
+/* Rotation steps a take with this selection needs (none for shift 0): returns their number, writes up to cap of them. */
+int32_t cm_kv_sel_steps(const cm_kv_sel *sel, int32_t *steps, int32_t cap);
+/* dst = the kept tokens of src, moved (add = 0; what dst held is replaced), or dst += them (add != 0: the places must be empty
+ * in dst; a fork and an adding take with a shift put two caches behind one another).  Frees pages, takes rejected drafts
+ * back (keep a prefix), slides a window or closes gaps (shift < 0).  dst is another cache, one level below src (else
+ * CM_E_LEVEL), with room for the last kept token (else CM_E_LAYOUT); src holds sel's ntok tokens and nothing behind them
+ * (cm_kv_tokens differs: CM_E_LAYOUT).  Bit for bit: K pages kept whole are dropped one level; every other ciphertext is
+ * multiplied by its mask and rescaled (cm_mul_pt, cm_rescale), and where its place asks for it rotated (cm_rotate).  evk may
+ * be null where sel lists no steps.  Uses dst's work area.  dst's token count becomes one past its last kept token
+ * (add: if that is more than it had), and the next append goes there. */
+cm_status cm_kv_take(cm_ctx *ctx, const cm_evk *evk, const cm_kv_sel *sel, const cm_kv *src, cm_kv *dst, int32_t add,
+                     void *stream);
 
 /* ---- grouped-query attention on a cache that stores every KV head once -------------------------------
  * The paper packs one K / V head per query head (Sec. 5.3).  For a model whose `heads` KV heads are each shared by
@@ -392,6 +433,37 @@ cm_status cm_gqa_qk(cm_ctx *ctx, const cm_evk *evk, const cm_gqa *gqa, const cm_
                     void *stream);
 cm_status cm_gqa_sv(cm_ctx *ctx, const cm_evk *evk, const cm_gqa *gqa, const cm_kv *kv, const cm_ct *scores, cm_ct *out,
                     void *stream);
+
+/* ---- learned relative position bias, by buckets, on scores -----------------------------------------------
+ * Adds to every score an entry of a learned table that depends on the query head and on the distance between the two
+ * tokens, and a mask's value to the scores of pages that a query may not see.  No level, no key.  The cache is a ring of
+ * cap = dim t_kv places (t_kv = S / (heads dim)); the distance of a query at place p from the token at place a is
+ * d = (p - a) mod cap.  For the scores of
+ *   a decode step (prompt = 0): `group` passes, one for each ciphertext cm_gqa_qk makes (group = 1: the one of
+ *     cm_vmm_kv(CM_QK)); the query is at place `token`;
+ *   a group of t = t_kv/group prompt tokens (prompt = 1): t_kv passes, pass delta for the query group moved by the inner rotation
+ *     of delta residues (group = 1: CM_QK_GROUP; else cm_gqa_qk with t_kv for its group and the query heads of a KV head side by side,
+ *     as everywhere in the layout); the group's first token is at place `token`, a multiple of t.
+ * table: host [heads * group][nbuckets], row hk * group + g; bucket: host [cap], a bucket 0 .. nbuckets - 1 for every distance
+ * (else CM_E_INVAL).  The largest t_kv - 1 distances are the tokens behind the query in its own page: a bucket
+ * whose entries are the mask's value there makes the bias causal.  mask: the value for pages that `first` hides (0: none, and `first` has to
+ * be -1).  Every entry and the mask times scale below 2^61 (else CM_E_INVAL), and the padding heads get zeros.  level, scale (0 =
+ * the context scale): those of the scores.  coeffs (nullable, host [passes * phases + 1][n]): integer coefficients of
+ * plaintext [pass][phase] for a query in page 0 -- at place `phase` (decode, t_kv of them) or with the group's first token
+ * at phase * t (prompt, `group` of them) -- and of the mask's value in the slots of row 0; the last is read only with a mask.
+ * Device memory: group * t_kv plaintexts, and with a mask dim + 1 more, one for every number of visible pages. */
+typedef struct cm_relbias cm_relbias;
+cm_status cm_relbias_create(cm_ctx *ctx, int32_t heads, int32_t dim, int32_t group, int32_t prompt, int32_t level,
+                            double scale, int32_t nbuckets, const double *table, const int32_t *bucket, double mask,
+                            const int64_t *coeffs, cm_relbias **out);
+void cm_relbias_destroy(cm_relbias *rb);
+int32_t cm_relbias_passes(const cm_relbias *rb);
+/* out[i] = in[i] + the bias of pass pass0 + i, i < npass.  first = -1: every page is seen; else the place of the first token of
+ * a page (a multiple of t_kv): pages outside first's .. token's, in the order of the ring, get the mask's value on top.
+ * in, out: arrays of npass ciphertexts at the object's level and scale (else CM_E_LEVEL, CM_E_SCALE); out[i] may be in[i]
+ * itself (its second component is then not touched), no other two of them may share memory (CM_E_INVAL). */
+cm_status cm_relbias_apply(cm_ctx *ctx, const cm_relbias *rb, int32_t token, int32_t first, int32_t pass0, int32_t npass,
+                           const cm_ct *in, cm_ct *out, void *stream);
 
 /* ---- rotary embedding with the extraction fused (Sec. 4.2, App. D) ------------------------ */
 /* The element-wise layer after the q / k projections: for token `token`, every pair of dims

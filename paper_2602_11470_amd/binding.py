@@ -104,6 +104,17 @@ _SIGS = {
     "cm_gqa_steps": ([_vp, _vp, _i32], _i32),
     "cm_gqa_qk": ([_vp, _vp, _vp, _vp, _P(cm_ct), _P(cm_ct), _vp], _i32),
     "cm_gqa_sv": ([_vp, _vp, _vp, _vp, _P(cm_ct), _P(cm_ct), _vp], _i32),
+    "cm_kv_seek": ([_vp, _i32], _i32),
+    "cm_kv_view": ([_vp, _i32, _i32, _P(cm_ct)], _i32),
+    "cm_kv_fork": ([_vp, _vp, _vp, _i32, _vp], _i32),
+    "cm_kv_sel_create": ([_vp, _vp, _vp, _i32, _i32, _vp, _P(_vp)], _i32),
+    "cm_kv_sel_destroy": ([_vp], None),
+    "cm_kv_sel_steps": ([_vp, _vp, _i32], _i32),
+    "cm_kv_take": ([_vp, _vp, _vp, _vp, _vp, _i32, _vp], _i32),
+    "cm_relbias_create": ([_vp, _i32, _i32, _i32, _i32, _i32, _f64, _i32, _vp, _vp, _f64, _vp, _P(_vp)], _i32),
+    "cm_relbias_destroy": ([_vp], None),
+    "cm_relbias_passes": ([_vp], _i32),
+    "cm_relbias_apply": ([_vp, _vp, _i32, _i32, _i32, _i32, _vp, _vp, _vp], _i32),
     "cm_profile_enable": ([_vp, _i32], _i32),
     "cm_profile_get": ([_vp, _i32, _P(_f64), _P(_f64), _P(_f64)], _i32),
     "cm_ntt": ([_vp, _vp, _vp, _i32, _i32, _vp], _i32),
@@ -365,6 +376,30 @@ class Context:
         _chk(lib.cm_gqa_sv(self.h, evk.h, gqa.h, gqa.kv.h, arr, C.byref(out.d), _stream()))
         return out
 
+    def kv_fork(self, src, dsts):
+        """Copies of a cache, each at the level of its own cache."""
+        _chk(lib.cm_kv_fork(self.h, src.h, (_vp * len(dsts))(*[d.h for d in dsts]), len(dsts), _stream()))
+
+    def kv_sel(self, like, keep, shift=0, coeffs=None):
+        return KvSelection(self, like, keep, shift, coeffs)
+
+    def kv_take(self, evk, sel, src, dst, add=False):
+        """dst = (add: +=) the tokens of src that sel keeps; evk may be None where sel has no steps."""
+        _chk(lib.cm_kv_take(self.h, evk.h if evk is not None else None, sel.h, src.h, dst.h, int(add), _stream()))
+
+    def relbias(self, heads, dim, table, bucket, level, scale=0.0, group=1, prompt=False, mask=0.0, coeffs=None):
+        return RelBias(self, heads, dim, table, bucket, level, scale, group, prompt, mask, coeffs)
+
+    def relbias_apply(self, bias, token, scores, first=-1, pass0=0, outs=None):
+        """scores (a list, one for each pass from pass0 on) plus their bias; outs may be scores."""
+        outs = outs or [Ct(self, s.level) for s in scores]
+        assert len(outs) == len(scores)
+        a, b = ((cm_ct * len(scores))(*[c.d for c in cts]) for cts in (scores, outs))
+        _chk(lib.cm_relbias_apply(self.h, bias.h, token, first, pass0, len(scores), a, b, _stream()))
+        for o, d in zip(outs, b):
+            o.d = cm_ct(d.dev, d.level, d.ncomp, d.scale)
+        return outs
+
     def vmm_kv(self, evk, kv, which, x):
         out = Ct(self, x.level - (1 if which in (CM_SV, CM_SV_GROUP) or kv.key_index else 2))
         _chk(lib.cm_vmm_kv(self.h, evk.h, kv.h, which, C.byref(x.d), C.byref(out.d), _stream()))
@@ -486,11 +521,60 @@ class Gqa:
             self.h = None
 
 
+class KvSelection:
+    """Which tokens of caches like `like` a take keeps (keep: truth values), and by how many pages they move (cm_kv_sel_*)."""
+
+    def __init__(self, ctx, like, keep, shift=0, coeffs=None):
+        self.ctx, self.h = ctx, _vp()
+        k = _np(np.asarray(keep) != 0, np.uint8)
+        c = _np(coeffs, np.int64) if coeffs is not None else None
+        _chk(lib.cm_kv_sel_create(ctx.h, like.h, k.ctypes.data, k.size, shift, c.ctypes.data if c is not None else None, C.byref(self.h)))
+
+    def steps(self):
+        n = lib.cm_kv_sel_steps(self.h, None, 0)
+        out = np.empty(n, dtype=np.int32)
+        lib.cm_kv_sel_steps(self.h, out.ctypes.data, n)
+        return out.tolist()
+
+    def __del__(self):
+        if getattr(self, "h", None) and lib is not None:
+            lib.cm_kv_sel_destroy(self.h)
+            self.h = None
+
+
+class RelBias:
+    """Relative position bias on scores (cm_relbias_*): table [query heads][buckets], bucket of every distance in the ring."""
+
+    def __init__(self, ctx, heads, dim, table, bucket, level, scale, group, prompt, mask, coeffs):
+        self.ctx, self.h = ctx, _vp()
+        t, b = _np(table, np.float64), _np(bucket, np.int32)
+        cap = ctx.S // (1 << (heads - 1).bit_length())
+        c = _np(coeffs, np.int64) if coeffs is not None else None
+        assert t.ndim == 2 and t.shape[0] == heads * group and b.shape == (cap,)
+        _chk(lib.cm_relbias_create(ctx.h, heads, dim, group, int(prompt), level, scale, t.shape[1], t.ctypes.data, b.ctypes.data, mask,
+                                   c.ctypes.data if c is not None else None, C.byref(self.h)))
+        self.passes = lib.cm_relbias_passes(self.h)
+
+    def __del__(self):
+        if getattr(self, "h", None) and lib is not None:
+            lib.cm_relbias_destroy(self.h)
+            self.h = None
+
+
+class _Words:
+    """Device memory of a cache as torch reads it; keeps the cache alive."""
+
+    def __init__(self, kv, ptr, words):
+        self.kv = kv
+        self.__cuda_array_interface__ = dict(shape=(words,), typestr="<i8", data=(ptr, False), strides=None, version=3)
+
+
 class KvCache:
     def __init__(self, ctx, heads, dim, r_i, level, scale, max_tokens, unrolled_ladders=False, shared_dims=1, key_index=False):
         self.ctx, self.h, self.level, self.key_index = ctx, _vp(), level, key_index
         t = ctx.S // ((1 << (heads - 1).bit_length()) * dim)
         max_tokens = dim * t if max_tokens is None else max_tokens
+        self.dim, self.r_i, self.pages = dim, r_i or dim, -(-max_tokens // t)
         _chk(lib.cm_kv_create_ex(ctx.h, heads, dim, r_i, level, scale, max_tokens,
                                  (CM_KV_UNROLLED_LADDERS if unrolled_ladders else 0) | (CM_KV_KEY_INDEX if key_index else 0),
                                  C.byref(self.h)))
@@ -514,6 +598,18 @@ class KvCache:
 
     def load(self, which, idx, ct):
         _chk(lib.cm_kv_load(self.ctx.h, self.h, which, idx, C.byref(ct.d), _stream()))
+
+    def seek(self, token):
+        _chk(lib.cm_kv_seek(self.h, token))
+
+    def words(self, which):
+        """The ciphertexts where they lie, as a tensor: [index][2][level+1][n], the key index [r_o][r_i][2][level+1][n]."""
+        d = cm_ct()
+        _chk(lib.cm_kv_view(self.h, which, 0, C.byref(d)))
+        limbs, ct = self.level + 1, 2 * (self.level + 1) * self.ctx.n
+        count = self.pages if which == CM_QK else self.dim
+        w = torch.as_tensor(_Words(self, d.dev, count * ct), device="cuda").view(count, 2, limbs, self.ctx.n)
+        return w.unflatten(0, (self.r_i, self.dim // self.r_i)).transpose(0, 1) if which == CM_KV_INDEX else w
 
     def export(self, which, idx):
         out = np.empty((2, self.level + 1, self.ctx.n), dtype=np.uint64)

@@ -13,44 +13,7 @@
 
 #include <utility>
 
-#include "kernels.h"
-
-struct cm_kv {
-    cm_ctx *ctx = nullptr;
-    int S, H, E, t, r_i, r_o, level, max_tokens, ntok, nk_max;
-    double scale;
-    bool scale_set = false;
-    u64 *d_k = nullptr, *d_v = nullptr;     // nk_max / E ciphertexts [2][level+1][n]
-    u64 *d_mask_qk = nullptr;               // base: slots (0, h, tau) all h, tau; level-1; multiplier form
-    u64 *d_mask_k = nullptr;                // base: slots with residue 0;         level+1
-    u64 *d_mask_v = nullptr;                // base: slots (0, h, 0) all h;        level+1
-    u64 *d_mask_kg = nullptr;               // every slot;                         level+1  (token-group append)
-    u64 *d_mask_vg = nullptr;               // base: slots (0, h, tau) all h, tau; level+1  (token-group append)
-    u64 *d_work = nullptr;
-    size_t work_words = 0;
-    // query-times-K runs CM_KS_BATCH key ciphertexts at a time: tables for raising the third
-    // component of their tensor products (level) and the second of their rotated sums (level-1)
-    KsManyTables relin_tabs, rot_tabs;
-    // sum over the head dims of query-times-K in the extended basis: the ladder cut into runs, every run the hoisted
-    // rotations by its subset sums
-    bool unrolled = false;
-    std::vector<std::vector<long long>> dim_groups;
-    // scores-times-V in the same form: giant steps unrolled (one key per multiple of the giant step), the ladder over
-    // the residues in runs; tables for raising the second components of up to CM_KS_BATCH inner sums at once
-    std::vector<std::vector<long long>> res_groups;
-    KsManyTables giant_tabs;
-    // query-times-K with the copy mask applied before the last `shared` terms of the sum over the dims: the sums of
-    // the key ciphertexts (d_T), their masked combinations A_k (d_A) and the E slot rotations of the mask (d_M)
-    // d_Mhat: the transform of d_M along the copy index (the masked sums as a cyclic correlation), with its twiddles
-    // the key index: E ciphertexts like d_v, copy b of ciphertext g r_i + j = dim (b + j) of key group b - g r_i;
-    // query-times-K from it is the scores-times-V schedule with the query in the place of the scores.  Ciphertext
-    // g r_i + j is stored at place j r_o + g: the r_o ciphertexts an append makes from ONE rotation of the new key are
-    // then neighbours (one launch reads that rotation once)
-    bool indexed = false;
-    u64 *d_x = nullptr;
-    int shared = 1;
-    u64 *d_T = nullptr, *d_A = nullptr, *d_M = nullptr, *d_Mhat = nullptr, *d_tw = nullptr, *d_einv = nullptr;
-};
+#include "kv.h"
 
 // ceil(L/3) runs of as equal length as possible, the longer ones first; a run lists its non-empty subset sums
 static std::vector<std::vector<long long>> ladder_groups(const std::vector<long long> &steps) {
@@ -72,12 +35,6 @@ static std::vector<std::vector<long long>> ladder_groups(const std::vector<long 
     return out;
 }
 
-static int ilog2(int x) {
-    int l = 0;
-    while ((1 << l) < x) l++;
-    return l;
-}
-static bool pow2(int x) { return x > 0 && (x & (x - 1)) == 0; }
 
 static cm_status encode_mask(cm_kv *kv, int kind, u64 *dst, int level, const int64_t *coeffs_or_null) {
     cm_ctx *ctx = kv->ctx;
@@ -190,7 +147,6 @@ extern "C" void cm_kv_destroy(cm_kv *kv) {
     ks_many_tables_destroy(&kv->giant_tabs);
     delete kv;
 }
-static u64 rot_g(const cm_kv *kv, long long step);
 // d_M[b] = the copy mask of copy b: the base mask rotated right by b copies (a Galois permutation of its rows)
 static cm_status build_mask_rows(cm_kv *kv) {
     cm_ctx *ctx = kv->ctx;
@@ -306,12 +262,9 @@ extern "C" int32_t cm_kv_steps(const cm_kv *kv, int32_t *steps, int32_t cap) {
 extern "C" int32_t cm_kv_tokens(const cm_kv *kv) { return kv ? kv->ntok : -1; }
 extern "C" cm_status cm_kv_set_tokens(cm_kv *kv, int32_t ntok) {
     if (!kv || ntok < 0 || ntok > kv->max_tokens) return CM_E_INVAL;
-    kv->ntok = ntok;
+    kv->ntok = kv->pos = ntok;
     return CM_OK;
 }
-
-static size_t kv_ctw(const cm_kv *kv) { return 2 * (size_t)(kv->level + 1) * kv->ctx->n; }
-static int x_place(const cm_kv *kv, int k) { return (k % kv->r_i) * kv->r_o + k / kv->r_i; }
 
 extern "C" cm_status cm_kv_load(cm_ctx *ctx, cm_kv *kv, int32_t which, int32_t idx, const cm_ct *ct, void *stream) {
     if (!ctx || !kv || kv->ctx != ctx || !ct || !ct->dev || ct->ncomp != 2) return CM_E_INVAL;
@@ -334,11 +287,6 @@ extern "C" cm_status cm_kv_export(cm_ctx *ctx, const cm_kv *kv, int32_t which, i
     return cm_ct_export(ctx, &ct, out);
 }
 
-static u64 rot_g(const cm_kv *kv, long long step) {
-    long long S = kv->S;
-    return galois_of_step(kv->ctx, (int)(((step % S) + S) % S));
-}
-
 // One token (k_new / v_new hold it at residue ntok mod t), or, group = true, the t tokens of the
 // next K ciphertext at once (Sec. 5.4: token c*t + tau at residue tau, which is already the layout
 // of K ciphertext c; the V masks take whole block rows, all residues together).
@@ -350,8 +298,8 @@ static cm_status kv_append(cm_ctx *ctx, const cm_evk *evk, cm_kv *kv, const cm_c
     CM_TRY
     const int lv = kv->level + 1;
     if (lv > ctx->L || k_new->level != lv || v_new->level != lv) return CM_E_LEVEL;
-    if (kv->ntok >= kv->max_tokens) return CM_E_LAYOUT;
-    if (group && (kv->ntok % kv->t || kv->ntok + kv->t > kv->max_tokens)) return CM_E_LAYOUT;
+    if (kv->pos >= kv->max_tokens) return CM_E_LAYOUT;
+    if (group && (kv->pos % kv->t || kv->pos + kv->t > kv->max_tokens)) return CM_E_LAYOUT;
     if (kv->scale_set && (fabs(k_new->scale / kv->scale - 1) > 1e-9 || fabs(v_new->scale / kv->scale - 1) > 1e-9))
         return CM_E_SCALE;
     if (fabs(k_new->scale / v_new->scale - 1) > 1e-9) return CM_E_SCALE;
@@ -361,7 +309,7 @@ static cm_status kv_append(cm_ctx *ctx, const cm_evk *evk, cm_kv *kv, const cm_c
         if (!find_key(evk, rot_g(kv, (long long)j * kv->H * kv->t))) return CM_E_NOKEY;
     hipStream_t st = (hipStream_t)stream;
     const size_t n = ctx->n, ctw_up = 2 * (size_t)(lv + 1) * n, ctw = kv_ctw(kv);
-    const int tok = kv->ntok, c = tok / kv->t, tau = tok % kv->t;
+    const int tok = kv->pos, c = tok / kv->t, tau = tok % kv->t;
     u64 *mask = kv->d_work, *prod = mask + (size_t)(lv + 1) * n, *res = prod + ctw_up, *shifted = res + ctw_up;
     // K: K_c += rescale(k_new * mask_tau), mask_tau = residue-0 mask rotated right by tau (a group: all ones)
     if (!group) launch_automorphism(ctx, mask, kv->d_mask_k, lv + 1, rot_g(kv, -tau), st);
@@ -423,7 +371,8 @@ static cm_status kv_append(cm_ctx *ctx, const cm_evk *evk, cm_kv *kv, const cm_c
                          [&](int k) { return k < kv->r_o ? k_new->dev : shifted + (size_t)(k / kv->r_o - 1) * ctw_up; },
                          [&](int k) { return rot_g(kv, -((long long)((c + k % kv->r_o * kv->r_i) % kv->E) * kv->H * kv->t + tau)); }));
     }
-    kv->ntok += group ? kv->t : 1;
+    kv->pos += group ? kv->t : 1;
+    if (kv->ntok < kv->pos) kv->ntok = kv->pos;
     kv->scale = k_new->scale * (double)ctx->mod[lv] / (double)ctx->mod[lv];
     kv->scale_set = true;
     RETURN_LAUNCH_STATUS();

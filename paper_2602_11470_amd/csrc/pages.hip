@@ -1,0 +1,337 @@
+// Pages of an encrypted cache: copies of a cache (cm_kv_fork) and the kept tokens of one moved into another (cm_kv_take).
+//
+// Page c of a cache is its tokens c t .. c t + t - 1.  With B = H t slots a row and E rows:
+//   K ciphertext c              holds page c, dim e in row e;
+//   V ciphertext k = g r_i + j  holds page c in row c - j, as dim c - j - g r_i         (rows and dims modulo E);
+//   X ciphertext k = g r_i + j  (the key index) holds page c in row c + g r_i, as dim c + g r_i + j.
+// So dropping tokens multiplies every V and X ciphertext by a rotation of ONE 0/1 mask M (the kept tokens, page c in row c): by
+// Rot(M, j B) and Rot(M, -g r_i B).  A rescale follows: the result lies one level below.  A page that moves from c to c' = c + s
+// keeps its dims, which says where it goes:
+//   V: k' = k + s (mod E), its rows by (g' - g) r_i;      X: k' = k - s (mod E), its rows by j - j'.
+// Every ciphertext therefore moves as a whole: to another place, and by one rotation by whole rows where the giant step (V) or
+// the baby step (X) of the place is another one.  K ciphertexts move without any arithmetic, unless a page keeps some of its
+// tokens only (a mask by residues).
+#include <math.h>
+
+#include <algorithm>
+
+#include "kv.h"
+
+typedef u64 u64x2 __attribute__((ext_vector_type(2)));
+
+struct cm_kv_sel {
+    cm_ctx *ctx = nullptr;
+    int H, E, t, r_i, level, ntok, shift, kept_end;     // level of the source; kept_end: one past the last kept token, after the move
+    bool indexed = false, any = false;                  // any: a token is kept
+    std::vector<int> page;                              // per source page: -1 dropped, 0 kept whole, 1 + p kept through pattern p
+    u64 *d_masks = nullptr;                             // [1 + patterns][level+1][n], multiplier form
+    int *d_from = nullptr;                              // [E] per page of the result: the page copied there, or -1
+    KsManyTables tabs;                                  // raises of CM_KS_BATCH moved ciphertexts, level - 1
+    bool turns = false;                                 // something is rotated
+};
+
+// one place of V (or X) of the result: the ciphertext that comes there, the rows its mask and the ciphertext itself turn by (left)
+struct Place {
+    int from, mask_rows, rows;
+};
+static Place v_place(const cm_kv_sel *s, int place) {
+    const int k = ((place - s->shift) % s->E + s->E) % s->E;
+    return {k, k % s->r_i, ((k / s->r_i - place / s->r_i) * s->r_i % s->E + s->E) % s->E};
+}
+static Place x_place_of(const cm_kv_sel *s, int place) {
+    const int r_o = s->E / s->r_i, kt = place % r_o * s->r_i + place / r_o, k = ((kt + s->shift) % s->E + s->E) % s->E;
+    return {k % s->r_i * r_o + k / s->r_i, s->E - k / s->r_i * s->r_i, ((kt % s->r_i - k % s->r_i) % s->E + s->E) % s->E};
+}
+static std::vector<int> sel_rows(const cm_kv_sel *s) {
+    std::vector<int> rows;
+    for (int p = 0; p < s->E; p++) {
+        rows.push_back(v_place(s, p).rows);
+        if (s->indexed) rows.push_back(x_place_of(s, p).rows);
+    }
+    std::sort(rows.begin(), rows.end());
+    rows.erase(std::unique(rows.begin(), rows.end()), rows.end());
+    if (!rows.empty() && rows[0] == 0) rows.erase(rows.begin());
+    return rows;
+}
+
+static bool same_shape(const cm_kv *a, const cm_kv *b) {
+    return a->H == b->H && a->E == b->E && a->r_i == b->r_i && a->indexed == b->indexed;
+}
+
+// ---- copies -----------------------------------------------------------------------------------------------------------
+// A workgroup moves one piece of PIECE words of a limb to every destination that has the limb, reading it once.
+#define PIECE 4096
+#define FORK_MAX 8
+struct ForkDst {
+    u64 *k, *v, *x;
+    int level, pages;
+};
+struct ForkArgs {
+    const u64 *k, *v, *x;
+    int level, top, pages, E, n, ndst;       // level of the source, highest level of a destination, pages in use
+    ForkDst d[FORK_MAX];
+};
+__global__ __launch_bounds__(256) void k_fork(ForkArgs a) {
+    const int per = a.n / PIECE, l = blockIdx.x / per, part = blockIdx.x % per;
+    const int c = blockIdx.y & 1, z = blockIdx.y >> 1;              // component, ciphertext: K pages, then V, then X
+    const size_t in = ((size_t)c * (a.level + 1) + l) * a.n + (size_t)part * PIECE, ct = 2 * (size_t)(a.level + 1) * a.n;
+    const int i = z < a.pages ? z : z < a.pages + a.E ? z - a.pages : z - a.pages - a.E;
+    const u64 *src = (z < a.pages ? a.k : z < a.pages + a.E ? a.v : a.x) + i * ct + in;
+    u64x2 w[8];
+#pragma unroll
+    for (int u = 0; u < 8; u++) w[u] = *((const u64x2 *)src + threadIdx.x + 256 * u);
+    for (int d = 0; d < a.ndst; d++) {
+        const ForkDst &t = a.d[d];
+        if (l > t.level) continue;
+        u64 *dst = (z < a.pages ? t.k : z < a.pages + a.E ? t.v : t.x) + i * 2 * (size_t)(t.level + 1) * a.n +
+                   ((size_t)c * (t.level + 1) + l) * a.n + (size_t)part * PIECE;
+#pragma unroll
+        for (int u = 0; u < 8; u++) *((u64x2 *)dst + threadIdx.x + 256 * u) = w[u];
+    }
+}
+__global__ __launch_bounds__(256) void k_zero(u64 *p) {
+    u64x2 *q = (u64x2 *)(p + (size_t)blockIdx.x * PIECE);
+#pragma unroll
+    for (int u = 0; u < 8; u++) q[threadIdx.x + 256 * u] = u64x2{0, 0};
+}
+static void launch_zero(u64 *p, size_t words, hipStream_t st) {
+    if (words) hipLaunchKernelGGL(k_zero, dim3((unsigned)(words / PIECE)), dim3(256), 0, st, p);
+}
+
+extern "C" cm_status cm_kv_view(const cm_kv *kv, int32_t which, int32_t idx, cm_ct *out) {
+    if (!kv || !out) return CM_E_INVAL;
+    if (which != CM_QK && which != CM_SV && !(which == CM_KV_INDEX && kv->indexed)) return CM_E_INVAL;
+    if (idx < 0 || idx >= (which == CM_QK ? kv->nk_max : kv->E)) return CM_E_LAYOUT;
+    out->dev = (which == CM_QK ? kv->d_k : which == CM_SV ? kv->d_v : kv->d_x) + (size_t)(which == CM_KV_INDEX ? x_place(kv, idx) : idx) * kv_ctw(kv);
+    out->level = kv->level, out->ncomp = 2, out->scale = kv->scale;
+    return CM_OK;
+}
+extern "C" cm_status cm_kv_seek(cm_kv *kv, int32_t token) {
+    if (!kv || token < 0 || token > kv->max_tokens) return CM_E_INVAL;
+    kv->pos = token;
+    return CM_OK;
+}
+extern "C" cm_status cm_kv_fork(cm_ctx *ctx, const cm_kv *src, cm_kv *const *dsts, int32_t ndst, void *stream) {
+    (void)hipGetLastError();          // stale errors of earlier calls are not this call's
+    if (!ctx || !src || src->ctx != ctx || !dsts || ndst < 1) return CM_E_INVAL;
+    for (int d = 0; d < ndst; d++) {
+        if (!dsts[d] || dsts[d]->ctx != ctx || dsts[d] == src) return CM_E_INVAL;
+        for (int e = 0; e < d; e++) if (dsts[e] == dsts[d]) return CM_E_INVAL;
+        if (!same_shape(src, dsts[d]) || dsts[d]->max_tokens < src->ntok || dsts[d]->max_tokens < src->pos) return CM_E_LAYOUT;
+        if (dsts[d]->level > src->level) return CM_E_LEVEL;
+    }
+    hipStream_t st = (hipStream_t)stream;
+    const int pages = (src->ntok + src->t - 1) / src->t, n = ctx->n;
+    for (int d0 = 0; d0 < ndst; d0 += FORK_MAX) {
+        ForkArgs a{src->d_k, src->d_v, src->d_x, src->level, 0, pages, src->E, n, std::min(ndst - d0, FORK_MAX), {}};
+        for (int d = 0; d < a.ndst; d++) {
+            const cm_kv *t = dsts[d0 + d];
+            a.d[d] = {t->d_k, t->d_v, t->d_x, t->level, t->nk_max};
+            a.top = std::max(a.top, t->level);
+        }
+        const int cts = pages + (src->indexed ? 2 : 1) * src->E;
+        Prof prof_(ctx, CM_K_ELEMENTWISE, (double)cts * 2 * (a.top + 1), st);
+        hipLaunchKernelGGL(k_fork, dim3((a.top + 1) * (n / PIECE), 2 * cts), dim3(256), 0, st, a);
+        for (int d = 0; d < a.ndst; d++)
+            launch_zero(dsts[d0 + d]->d_k + pages * kv_ctw(dsts[d0 + d]), (dsts[d0 + d]->nk_max - pages) * kv_ctw(dsts[d0 + d]), st);
+    }
+    for (int d = 0; d < ndst; d++)
+        dsts[d]->ntok = src->ntok, dsts[d]->pos = src->pos, dsts[d]->scale = src->scale, dsts[d]->scale_set = src->scale_set;
+    RETURN_LAUNCH_STATUS();
+}
+
+// ---- kept tokens ----------------------------------------------------------------------------------------------------------
+extern "C" void cm_kv_sel_destroy(cm_kv_sel *s) {
+    if (!s) return;
+    hipFree(s->d_masks), hipFree(s->d_from);
+    ks_many_tables_destroy(&s->tabs);
+    delete s;
+}
+extern "C" cm_status cm_kv_sel_create(cm_ctx *ctx, const cm_kv *like, const uint8_t *keep, int32_t ntok, int32_t shift, const int64_t *coeffs,
+                                      cm_kv_sel **out) {
+    if (!ctx || !like || like->ctx != ctx || !out || ntok < 0 || (ntok && !keep)) return CM_E_INVAL;
+    if (like->level < 3) return CM_E_LEVEL;                      // the result is a cache, and those begin at level 2
+    const int t = like->t, E = like->E, S = like->S;
+    if (ntok > E * t || shift <= -E || shift >= E) return CM_E_LAYOUT;
+    cm_kv_sel *s = new (std::nothrow) cm_kv_sel();
+    if (!s) return CM_E_NOMEM;
+    cm_status status = CM_OK;
+    try {
+        s->ctx = ctx, s->H = like->H, s->E = E, s->t = t, s->r_i = like->r_i, s->level = like->level, s->ntok = ntok, s->shift = shift, s->kept_end = 0;
+        s->indexed = like->indexed;
+        const int pages = (ntok + t - 1) / t;
+        std::vector<std::vector<uint8_t>> patterns;
+        std::vector<int> from(E, -1);
+        s->page.assign(pages, -1);
+        for (int c = 0; c < pages && status == CM_OK; c++) {
+            const int stored = std::min(t, ntok - c * t);
+            std::vector<uint8_t> p(t, 0);
+            int kept = 0;
+            for (int r = 0; r < stored; r++)
+                if (keep[c * t + r]) p[r] = 1, kept++, s->kept_end = (c + shift) * t + r + 1;
+            if (!kept) continue;
+            if (c + shift < 0 || c + shift >= E) { status = CM_E_LAYOUT; break; }
+            s->any = true;
+            if (kept == stored) {
+                s->page[c] = 0, from[c + shift] = c;
+                continue;
+            }
+            const size_t i = std::find(patterns.begin(), patterns.end(), p) - patterns.begin();
+            if (i == patterns.size()) patterns.push_back(p);
+            s->page[c] = 1 + (int)i;
+        }
+        if (status == CM_OK && s->any) {
+            const int n = ctx->n, lv = s->level;
+            const size_t words = (size_t)(lv + 1) * n;
+            const double scale = (double)ctx->mod[lv];           // what the rescale divides by
+            if (hipMalloc((void **)&s->d_masks, (1 + patterns.size()) * words * 8) != hipSuccess || hipMalloc((void **)&s->d_from, E * sizeof(int)) != hipSuccess)
+                status = CM_E_NOMEM;
+            else if (hipMemcpy(s->d_from, from.data(), E * sizeof(int), hipMemcpyHostToDevice) != hipSuccess)
+                status = CM_E_HIP;
+            std::vector<double> m(S);
+            for (size_t i = 0; i <= patterns.size() && status == CM_OK; i++) {
+                cm_pt pt;
+                pt.dev = s->d_masks + i * words, pt.mont = 1;
+                for (int a = 0; a < S; a++) {                    // slot (row, h, residue)
+                    const int tok = a / (s->H * t) * t + a % t;
+                    m[a] = i ? patterns[i - 1][a % t] : tok < ntok && keep[tok] ? 1.0 : 0.0;
+                }
+                status = coeffs ? cm_pt_from_coeffs(ctx, coeffs + i * n, lv, scale, &pt) : cm_encode(ctx, m.data(), nullptr, S, lv, scale, &pt);
+            }
+            s->turns = !sel_rows(s).empty();
+            if (status == CM_OK && s->turns) status = ks_many_tables_create(ctx, lv - 1, CM_KS_BATCH, &s->tabs, 2, 1);
+            if (status == CM_OK) ks_level(ctx, lv), get_qlinv(ctx, lv);      // the per-level tables that a take reads
+        }
+    } catch (...) {
+        status = CM_E_NOMEM;
+    }
+    if (status != CM_OK) {
+        cm_kv_sel_destroy(s);
+        return status;
+    }
+    *out = s;
+    return CM_OK;
+}
+extern "C" int32_t cm_kv_sel_steps(const cm_kv_sel *s, int32_t *steps, int32_t cap) {
+    if (!s || !s->any) return 0;
+    try {
+        const auto rows = sel_rows(s);
+        for (int i = 0; i < (int)rows.size() && i < cap && steps; i++) steps[i] = rows[i] * s->H * s->t;
+        return (int32_t)rows.size();
+    } catch (...) {
+        return 0;
+    }
+}
+
+// page blockIdx.y of the result (+)= the page from[blockIdx.y] of the source; zero (nothing added) where there is none
+template <bool ADD>
+__global__ __launch_bounds__(256) void k_pages(u64 *__restrict__ out, const u64 *__restrict__ in, const int *__restrict__ from, const ModC *__restrict__ modc, int E,
+                                               int level, int n) {
+    const int per = n / PIECE, l = blockIdx.x / per, part = blockIdx.x % per, c = blockIdx.y & 1, page = blockIdx.y >> 1;
+    const int src = from && page < E ? from[page] : -1;
+    if (ADD && src < 0) return;
+    const u64 q = modc[l].q;
+    u64x2 *dst = (u64x2 *)(out + (((size_t)page * 2 + c) * (level + 1) + l) * n + (size_t)part * PIECE);
+    const u64x2 *p = (const u64x2 *)(in + (((size_t)std::max(src, 0) * 2 + c) * (level + 2) + l) * n + (size_t)part * PIECE);
+#pragma unroll
+    for (int u = 0; u < 8; u++) {
+        u64x2 w = src < 0 ? u64x2{0, 0} : p[threadIdx.x + 256 * u];
+        if (ADD) {
+            const u64x2 o = dst[threadIdx.x + 256 * u];
+            w = u64x2{addmod(w.x, o.x, q), addmod(w.y, o.y, q)};
+        }
+        dst[threadIdx.x + 256 * u] = w;
+    }
+}
+
+extern "C" cm_status cm_kv_take(cm_ctx *ctx, const cm_evk *evk, const cm_kv_sel *s, const cm_kv *src, cm_kv *dst, int32_t add, void *stream) {
+    (void)hipGetLastError();
+    if (!ctx || !s || s->ctx != ctx || !src || src->ctx != ctx || !dst || dst->ctx != ctx || src == dst) return CM_E_INVAL;
+    if (s->turns && s->any && (!evk || !evk_fits(ctx, evk))) return CM_E_INVAL;
+    if (!same_shape(src, dst) || s->H != src->H || s->E != src->E || s->r_i != src->r_i || (src->indexed && !s->indexed)) return CM_E_LAYOUT;
+    if (src->level != s->level || dst->level != s->level - 1) return CM_E_LEVEL;
+    if (src->ntok != s->ntok || s->kept_end > dst->max_tokens) return CM_E_LAYOUT;
+    if (add && src->scale_set && dst->scale_set && fabs(src->scale / dst->scale - 1) > 1e-9) return CM_E_SCALE;
+    CM_TRY
+    const long long B = (long long)s->H * s->t;
+    if (s->any)
+        for (int rows : sel_rows(s))
+            if (!find_key(evk, rot_g(src, rows * B))) return CM_E_NOKEY;
+    hipStream_t st = (hipStream_t)stream;
+    const int lv = s->level, lo = lv - 1, n = ctx->n;
+    const size_t ctw_in = kv_ctw(src), ctw = kv_ctw(dst);
+    // K: pages kept whole are copied, the places without one cleared; then the pages that keep some of their tokens
+    {
+        Prof prof_(ctx, CM_K_ELEMENTWISE, (double)dst->nk_max * 2 * lv, st);
+        const dim3 grid(lv * (n / PIECE), 2 * dst->nk_max);
+        if (add && s->any) hipLaunchKernelGGL(k_pages<true>, grid, dim3(256), 0, st, dst->d_k, src->d_k, s->d_from, ctx->d_modc, s->E, lo, n);
+        else if (!add) hipLaunchKernelGGL(k_pages<false>, grid, dim3(256), 0, st, dst->d_k, src->d_k, s->d_from, ctx->d_modc, s->E, lo, n);
+    }
+    if (!s->any) {
+        if (!add) {
+            launch_zero(dst->d_v, s->E * ctw, st);
+            if (dst->indexed) launch_zero(dst->d_x, s->E * ctw, st);
+        }
+    } else {
+        const KsLevel &kl = ks_level(ctx, lo);
+        const size_t ln = (size_t)(lo + 1) * n, dblk = (size_t)kl.beta * kl.ext * n, ublk = 2 * (size_t)kl.ext * n, mw = (size_t)(lv + 1) * n;
+        // out[0 .. m) (+)= rescale(mask through g * source): products formed inside the rescale, or in two steps
+        auto masked = [&](const MulPtBatch &mb, int m, const u64 *mask, u64 *outp, u64 *work, bool acc) -> cm_status {
+            u64 *last = work, *red = last + (size_t)m * 2 * n, *prods = red + (size_t)m * 2 * lv * n;
+            if (rescale_masked_into(ctx, mb, m, mask, lv, outp, st, last, red, acc)) return CM_OK;
+            launch_mul_pt_rot_batch(ctx, prods, mb, m, mask, lv + 1, st);
+            return rescale_into(ctx, prods, 2 * m, lv, outp, st, last, red, acc);
+        };
+        const int fused = rescale_masked_batch(ctx, lv, dst->work_words), most = fused ? fused : CM_KS_BATCH;
+        for (size_t c = 0; c < s->page.size();) {                 // a run of neighbours with one pattern
+            const int p = s->page[c];
+            int m = 0;
+            MulPtBatch mb;
+            while (p > 0 && m < most && c + m < s->page.size() && s->page[c + m] == p) mb.src[m] = src->d_k + (c + m) * ctw_in, mb.g[m] = 1, m++;
+            if (m) CMCHK(masked(mb, m, s->d_masks + p * mw, dst->d_k + (c + s->shift) * ctw, dst->d_work, add != 0));
+            c += m ? m : 1;
+        }
+        auto move = [&](u64 *out, const u64 *in, auto place_of) -> cm_status {
+            for (int p0 = 0; p0 < s->E;) {
+                const int rows = place_of(s, p0).rows, cap = rows ? std::min(most, CM_KS_BATCH) : most;
+                int m = 0;
+                MulPtBatch mb;
+                for (; m < cap && p0 + m < s->E && place_of(s, p0 + m).rows == rows; m++) {
+                    const Place pl = place_of(s, p0 + m);
+                    mb.src[m] = in + pl.from * ctw_in, mb.g[m] = (unsigned)rot_g(src, pl.mask_rows * B);
+                }
+                if (!rows) {
+                    CMCHK(masked(mb, m, s->d_masks, out + p0 * ctw, dst->d_work, add != 0));
+                } else {
+                    // masked and rescaled next to one another, then turned: one raise, one inner-product launch with the key read once,
+                    // one ModDown
+                    const u64 g = rot_g(src, rows * B), *key = find_key(evk, g);
+                    u64 *tmp = dst->d_work, *ksin = tmp + CM_KS_BATCH * ctw, *digits = ksin + CM_KS_BATCH * ln, *work = digits + CM_KS_BATCH * dblk;
+                    CMCHK(masked(mb, m, s->d_masks, tmp, work, false));
+                    CMCHK(ks_raise_many(ctx, s->tabs, tmp, ksin, digits, st, m, g));
+                    u64 *bu = arena_batch_sums(ctx);
+                    IpBatch ip;
+                    ip.nz = m, ip.nsum = 1;
+                    const u64 *adds[CM_KS_BATCH], *accs[CM_KS_BATCH];
+                    u64 *outs[CM_KS_BATCH];
+                    for (int r = 0; r < m; r++) {
+                        ip.it[r].dig = digits + r * dblk, ip.it[r].key = key, ip.out[r] = bu + r * ublk;
+                        adds[r] = tmp + r * ctw, outs[r] = out + (p0 + r) * ctw, accs[r] = add ? outs[r] : nullptr;
+                    }
+                    launch_inner_product_shared_key(ctx, ip, kl.beta, lo, st);
+                    CMCHK(moddown_batch_into(ctx, bu, lo, m, adds, 1, g, accs, outs, st));
+                }
+                p0 += m;
+            }
+            return CM_OK;
+        };
+        CMCHK(move(dst->d_v, src->d_v, v_place));
+        if (src->indexed) CMCHK(move(dst->d_x, src->d_x, x_place_of));
+    }
+    dst->ntok = add ? std::max(dst->ntok, s->kept_end) : s->kept_end;
+    dst->pos = dst->ntok;
+    if (!add) dst->scale = src->scale, dst->scale_set = src->scale_set && s->any;
+    else if (s->any && src->scale_set && !dst->scale_set) dst->scale = src->scale, dst->scale_set = true;
+    RETURN_LAUNCH_STATUS();
+    CM_CATCH
+}

@@ -1,0 +1,162 @@
+// Learned relative position bias on encrypted attention scores.
+//
+// Scores hold the token of place c t_kv + j in row c, residue j, of every KV head; the cache is a ring of cap = E t_kv places.  A query
+// at place p sees the token of a place at the distance d = (p - place) mod cap; its score takes table[head][bucket[d]].  What a
+// query of row c_q adds is what one of row 0 with the same residue adds, c_q rows further on: ONE plaintext per pass and residue
+// (decode) or per pass and group of residues (prompt) serves every position, through the Galois map that moves slots by whole rows --
+// an exact permutation of the plaintext's values.  The mask of the rows outside the pages that a query may see (the start of a packed
+// sequence, a window) is the sum of rotations of one plaintext row, formed once per number of rows.
+#include <math.h>
+
+#include "kv.h"
+
+struct cm_relbias {
+    cm_ctx *ctx = nullptr;
+    int H, E, t_kv, G, level, passes, phases;
+    bool prompt = false;
+    double scale;
+    u64 *d_pts = nullptr;          // [passes][phases][level+1][n]
+    u64 *d_unseen = nullptr;       // [E+1][level+1][n]: entry m < E: the mask's value in the rows m .. E-1, entry E: in row 0; null without a mask
+};
+
+// out = a + (b through the Galois map g), rows limbs
+__global__ void k_add_turned(u64 *out, const u64 *a, const u64 *b, const ModC *__restrict__ modc, unsigned g, int n, int logn) {
+    const unsigned i = blockIdx.x * 256 + threadIdx.x;
+    const size_t row = (size_t)blockIdx.y * n;
+    out[row + i] = addmod(a[row + i], b[row + perm_src(i, g, logn)], modc[blockIdx.y].q);
+}
+
+#define BIAS_BATCH 32
+struct BiasBatch {
+    const u64 *in[BIAS_BATCH], *pt[BIAS_BATCH];
+    u64 *out[BIAS_BATCH];
+};
+// out[z] = in[z] + (pt[z] through g, row through gr, 0)
+__global__ __launch_bounds__(256) void k_relbias(BiasBatch b, const u64 *row, unsigned g, unsigned gr, const ModC *__restrict__ modc, int limbs, int n,
+                                                 int logn) {
+    const unsigned i = blockIdx.x * 256 + threadIdx.x;
+    const int l = blockIdx.y, z = blockIdx.z;
+    const size_t at = (size_t)l * n + i, cs = (size_t)limbs * n;
+    const u64 q = modc[l].q;
+    u64 v = addmod(b.in[z][at], b.pt[z][(size_t)l * n + perm_src(i, g, logn)], q);
+    if (row) v = addmod(v, row[(size_t)l * n + perm_src(i, gr, logn)], q);
+    b.out[z][at] = v;
+    if (b.out[z] != b.in[z]) b.out[z][at + cs] = b.in[z][at + cs];
+}
+
+extern "C" void cm_relbias_destroy(cm_relbias *rb) {
+    if (!rb) return;
+    hipFree(rb->d_pts), hipFree(rb->d_unseen);
+    delete rb;
+}
+extern "C" cm_status cm_relbias_create(cm_ctx *ctx, int32_t heads, int32_t dim, int32_t group, int32_t prompt, int32_t level, double scale,
+                                       int32_t nbuckets, const double *table, const int32_t *bucket, double mask, const int64_t *coeffs,
+                                       cm_relbias **out) {
+    if (!ctx || !out || heads < 1 || dim < 1 || group < 1 || nbuckets < 1 || !table || !bucket || (prompt != 0 && prompt != 1)) return CM_E_INVAL;
+    if (level < 0 || level > ctx->L) return CM_E_LEVEL;
+    const int S = ctx->n / 2;
+    if (heads > S || dim > S) return CM_E_LAYOUT;
+    const int H = 1 << ilog2(heads), real = heads;
+    if (!pow2(dim) || (long long)H * dim > S || !pow2(group) || S / (H * dim) % group) return CM_E_LAYOUT;
+    const int t_kv = S / (H * dim), t = t_kv / group, cap = dim * t_kv;
+    if (scale == 0) scale = ctx->prm.scale;
+    if (!(scale > 0) || !isfinite(scale) || !isfinite(mask)) return CM_E_INVAL;
+    // a slot holds a table entry and at most one mask value: their coefficients have to fit the signed words of the encoding
+    double top = fabs(mask);
+    for (size_t i = 0; i < (size_t)real * group * nbuckets; i++) {
+        if (!isfinite(table[i])) return CM_E_INVAL;
+        top = fmax(top, fabs(table[i]));
+    }
+    if (top * scale >= 0x1p61) return CM_E_INVAL;
+    for (int d = 0; d < cap; d++) if (bucket[d] < 0 || bucket[d] >= nbuckets) return CM_E_INVAL;
+    cm_relbias *rb = new (std::nothrow) cm_relbias();
+    if (!rb) return CM_E_NOMEM;
+    cm_status status = CM_OK;
+    try {
+        rb->ctx = ctx, rb->H = H, rb->E = dim, rb->t_kv = t_kv, rb->G = group, rb->level = level, rb->prompt = prompt != 0, rb->scale = scale;
+        rb->passes = prompt ? t_kv : group, rb->phases = prompt ? group : t_kv;
+        const int n = ctx->n, polys = rb->passes * rb->phases;
+        const size_t words = (size_t)(level + 1) * n;
+        u64 *row = nullptr;
+        if (hipMalloc((void **)&rb->d_pts, polys * words * 8) != hipSuccess) status = CM_E_NOMEM;
+        if (status == CM_OK && mask != 0 && hipMalloc((void **)&rb->d_unseen, (dim + 1) * words * 8) != hipSuccess) status = CM_E_NOMEM;
+        auto encode = [&](u64 *dst, const std::vector<double> &m, int i) {
+            cm_pt pt;
+            pt.dev = dst, pt.mont = 0;
+            return coeffs ? cm_pt_from_coeffs(ctx, coeffs + (size_t)i * n, level, scale, &pt) : cm_encode(ctx, m.data(), nullptr, S, level, scale, &pt);
+        };
+        std::vector<double> m(S);
+        for (int p = 0; p < polys && status == CM_OK; p++) {
+            const int delta = p / rb->phases, phase = p % rb->phases;
+            for (int x = 0; x < dim; x++)
+                for (int j = 0; j < t_kv; j++) {
+                    const int u = (j - delta + t_kv) % t_kv;                 // prompt: the query's residue in its page
+                    const int g = prompt ? u / t : ((j / t - delta) % group + group) % group;
+                    const int place = prompt ? phase * t + u % t : phase, d = ((place - j - x * t_kv) % cap + cap) % cap;
+                    for (int h = 0; h < H; h++) m[(size_t)(x * H + h) * t_kv + j] = h < real ? table[(size_t)(h * group + g) * nbuckets + bucket[d]] : 0.0;
+                }
+            status = encode(rb->d_pts + p * words, m, p);
+        }
+        if (status == CM_OK && mask != 0) {
+            for (int i = 0; i < S; i++) m[i] = i < H * t_kv ? mask : 0.0;
+            row = rb->d_unseen + dim * words;
+            status = encode(row, m, polys);
+            if (status == CM_OK) {
+                // entry E - 1: the row turned right by E - 1; entry i: entry i + 1 and the row turned right by i
+                for (int i = dim - 1; i >= 0; i--) {
+                    const u64 g = galois_of_step(ctx, (int)(((long long)S - (long long)i * H * t_kv) % S));
+                    if (i == dim - 1) launch_automorphism(ctx, rb->d_unseen + i * words, row, level + 1, g, 0);
+                    else hipLaunchKernelGGL(k_add_turned, dim3(n / 256, level + 1), dim3(256), 0, 0, rb->d_unseen + i * words,
+                                            rb->d_unseen + (i + 1) * words, row, ctx->d_modc, (unsigned)g, n, ctx->logn);
+                }
+                if (hipDeviceSynchronize() != hipSuccess || hipGetLastError() != hipSuccess) status = CM_E_HIP;
+            }
+        }
+    } catch (...) {
+        status = CM_E_NOMEM;
+    }
+    if (status != CM_OK) {
+        cm_relbias_destroy(rb);
+        return status;
+    }
+    *out = rb;
+    return CM_OK;
+}
+extern "C" int32_t cm_relbias_passes(const cm_relbias *rb) { return rb ? rb->passes : 0; }
+extern "C" cm_status cm_relbias_apply(cm_ctx *ctx, const cm_relbias *rb, int32_t token, int32_t first, int32_t pass0, int32_t npass, const cm_ct *in,
+                                      cm_ct *out, void *stream) {
+    (void)hipGetLastError();          // stale errors of earlier calls are not this call's
+    if (!ctx || !rb || rb->ctx != ctx || !in || !out || npass < 1 || pass0 < 0) return CM_E_INVAL;
+    const int cap = rb->E * rb->t_kv, t = rb->t_kv / rb->G;
+    if (token < 0 || token >= cap || (rb->prompt && token % t) || first < -1 || first >= cap || (first > 0 && first % rb->t_kv)) return CM_E_LAYOUT;
+    if (first >= 0 && !rb->d_unseen) return CM_E_LAYOUT;
+    if (npass > rb->passes - pass0) return CM_E_LAYOUT;
+    for (int p = 0; p < npass; p++) {
+        if (!in[p].dev || !out[p].dev || in[p].ncomp != 2) return CM_E_INVAL;
+        for (int r = 0; r < npass; r++) if (r != p && (out[r].dev == in[p].dev || out[r].dev == out[p].dev)) return CM_E_INVAL;
+        if (in[p].level != rb->level) return CM_E_LEVEL;
+        if (!(fabs(in[p].scale / rb->scale - 1) < 1e-9)) return CM_E_SCALE;
+    }
+    hipStream_t st = (hipStream_t)stream;
+    const int n = ctx->n, limbs = rb->level + 1, S = n / 2, page = token / rb->t_kv, phase = rb->prompt ? token % rb->t_kv / t : token % rb->t_kv;
+    const size_t words = (size_t)limbs * n;
+    auto turn = [&](int rows) { return (unsigned)galois_of_step(ctx, (int)(((long long)S - (long long)rows * rb->H * rb->t_kv) % S)); };
+    const u64 *row = nullptr;
+    unsigned gr = 0;
+    if (first >= 0) {
+        const int from = first / rb->t_kv, seen = (page - from + rb->E) % rb->E + 1;
+        if (seen < rb->E) row = rb->d_unseen + seen * words, gr = turn(from);
+    }
+    for (int p0 = 0; p0 < npass; p0 += BIAS_BATCH) {
+        const int m = npass - p0 < BIAS_BATCH ? npass - p0 : BIAS_BATCH;
+        BiasBatch b;
+        for (int z = 0; z < m; z++) {
+            b.in[z] = in[p0 + z].dev, b.out[z] = out[p0 + z].dev;
+            b.pt[z] = rb->d_pts + ((size_t)(pass0 + p0 + z) * rb->phases + phase) * words;
+        }
+        Prof prof_(ctx, CM_K_ELEMENTWISE, (double)m * limbs, st);
+        hipLaunchKernelGGL(k_relbias, dim3(n / 256, limbs, m), dim3(256), 0, st, b, row, turn(page), gr, ctx->d_modc, limbs, n, ctx->logn);
+    }
+    for (int p = 0; p < npass; p++) out[p].level = in[p].level, out[p].ncomp = 2, out[p].scale = in[p].scale;
+    RETURN_LAUNCH_STATUS();
+}
