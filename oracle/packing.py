@@ -370,6 +370,63 @@ class KvLayout:
     def k_index_append_group_mask(self, k, c):
         return sum(self.k_index_append_mask(k, c * self.t + tau) for tau in range(self.t))
 
+    # ---- kept tokens, moved by whole pages (page c = tokens c t .. c t + t - 1) --------------------------------
+    def keep_rows(self, keep):
+        """The kept tokens in the layout of the scores: token c*t + tau at (c, h, tau) for every head."""
+        m = np.zeros(self.S)
+        for n in np.flatnonzero(keep):
+            for h in range(self.H):
+                m[self.slot(n // self.t, h, n % self.t)] = 1.0
+        return m
+
+    def keep_residues(self, keep, c):
+        """The kept residues of page c, in every (e, h) block."""
+        m = np.zeros(self.S)
+        for tau in range(self.t):
+            if c * self.t + tau < len(keep) and keep[c * self.t + tau]:
+                m[tau::self.t] = 1.0
+        return m
+
+    def partial_pages(self, keep):
+        """The pages that keep some but not all of their tokens."""
+        pages = [np.asarray(keep[c * self.t:(c + 1) * self.t], dtype=bool) for c in range(-(-len(keep) // self.t))]
+        return [c for c, p in enumerate(pages) if p.any() and not p.all()]
+
+    def v_place(self, k, shift):
+        """Where V ciphertext k goes when its pages move by `shift`, and the rows it turns LEFT by: a token keeps its dim."""
+        to = (k + shift) % self.E
+        return to, (k // self.r_i - to // self.r_i) * self.r_i % self.E
+
+    def k_index_place(self, k, shift):
+        to = (k - shift) % self.E
+        return to, (to % self.r_i - k % self.r_i) % self.E
+
+    def take_steps(self, shift, index):
+        rows = {self.v_place(k, shift)[1] for k in range(self.E)}
+        rows |= {self.k_index_place(k, shift)[1] for k in range(self.E)} if index else set()
+        return sorted(r * self.H * self.t for r in rows if r)
+
+    # ---- relative position bias: E t places in a ring, distance of a query at p from place a = (p - a) mod E t ---------
+    def bias_slots(self, table, bucket, token, first=None, mask=0.0, group=1, delta=0, prompt=False):
+        """What pass delta of the scores takes for a query at place `token` (a prompt's group begins there): in slot (c, hk, j)
+        table[hk * group + g][bucket[distance]] of the query head g that meets residue j there, and `mask` in the pages that are
+        not among those from `first`'s to the query's."""
+        cap, t = self.E * self.t, self.t // group
+        out = np.zeros(self.S)
+        for c in range(self.E):
+            hidden = first is not None and (c - first // self.t) % self.E > (token // self.t - first // self.t) % self.E
+            for hk in range(self.H):
+                for j in range(self.t):
+                    if prompt:
+                        u = (j - delta) % self.t
+                        g, place = u // t, token + u % t
+                    else:
+                        g, place = (j // t - delta) % group, token
+                    d = (place - (c * self.t + j)) % cap
+                    v = table[hk * group + g][bucket[d]] if hk < self.heads else 0.0
+                    out[self.slot(c, hk, j)] = v + (mask if hidden else 0.0)
+        return out
+
     def k_index_steps(self):
         """Rotation amounts the index needs: the baby steps (of the query, and of a new key at append) and the giant step."""
         s = [j * self.H * self.t for j in range(1, self.r_i)]

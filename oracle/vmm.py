@@ -490,6 +490,30 @@ def kv_append_group(ops, lay: KvLayout, k_cts, v_cts, c, ck_grp, cv_grp, k_mask,
         _index_append(ops, lay, x_cts, ck_grp, x_masks)
 
 
+def kv_take(ops, lay: KvLayout, k_cts, v_cts, keep, shift, row_masks, page_masks, x_cts=None):
+    """The kept tokens of a cache, moved by `shift` pages, one level below: (K ciphertexts by page, V, index).  row_masks[r]: the
+    kept tokens (lay.keep_rows) turned left by r rows; page_masks[c]: lay.keep_residues of the pages kept in part."""
+    B = lay.H * lay.t
+    k_out = {}
+    for c in range(-(-len(keep) // lay.t)):
+        page = keep[c * lay.t:(c + 1) * lay.t]
+        if all(page):
+            k_out[c + shift] = ops.drop(k_cts[c])
+        elif any(page):
+            k_out[c + shift] = ops.rescale(ops.mul_pt(k_cts[c], page_masks[c]))
+
+    def moved(cts, mask_rows, place):
+        out = [None] * lay.E
+        for k in range(lay.E):
+            to, rows = place(k, shift)
+            y = ops.rescale(ops.mul_pt(cts[k], row_masks[mask_rows(k) % lay.E]))
+            out[to] = ops.rotate(y, rows * B) if rows else y
+        return out
+    v_out = moved(v_cts, lambda k: k % lay.r_i, lay.v_place)
+    x_out = moved(x_cts, lambda k: -(k // lay.r_i) * lay.r_i, lay.k_index_place) if x_cts is not None else None
+    return k_out, v_out, x_out
+
+
 def gqa_qk_scores(ops, glay: GqaLayout, cq, k_cts, masks, rot_plaintexts, qk=None):
     """q K^T of one token against a cache that stores every KV head once (packing.GqaLayout).  cq: the query
     at (e, h, 0) of the H-head layout, one level above the cache.  It is replicated over its t residues

@@ -1,0 +1,460 @@
+"""Copies of an encrypted cache (cm_kv_fork) and kept tokens moved into another one (cm_kv_take): word for word against the single
+calls they stand for (level drop, product with the mask, rescale, rotation, addition), against the oracle, and decrypted."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+SMALL, BIG, WIDE = "4096: 5+1", "65536: 24+4", "4096: 54 bits"
+
+
+@pytest.fixture(scope="module")
+def rings():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    from paper_2602_11470_amd import binding as B
+    made = {}
+
+    def get(name):
+        if name not in made:
+            made[name] = B.config1() if name == SMALL else B.llama_ring(24, 4) if name == BIG else B.Context(4096, 6, 2, 2, 54, 54, 60, 2.0 ** 50)
+        return made[name]
+    yield get
+    for c in made.values():
+        c.close()
+
+
+def _residues(ctx, shape, limbs, gen):
+    import torch
+    out = torch.empty(*shape, limbs, ctx.n, dtype=torch.int64, device="cuda")
+    for i, q in enumerate(ctx.moduli()[:limbs]):
+        out[..., i, :] = torch.empty(*shape, ctx.n, dtype=torch.int64, device="cuda").random_(0, int(q), generator=gen)
+    return out
+
+
+def _which(B, index):
+    return [B.CM_QK, B.CM_SV] + ([B.CM_KV_INDEX] if index else [])
+
+
+def _filled(ctx, heads, dim, r_i, level, index, ntok, seed, max_tokens=None, fill_all=True):
+    """A cache of random residues: pages in use, every value and index ciphertext; junk in the unused pages if fill_all."""
+    import torch
+    from paper_2602_11470_amd import binding as B
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    kv = ctx.kv_create(heads, dim, level, r_i=r_i, max_tokens=max_tokens, key_index=index)
+    for w in _which(B, index):
+        words = kv.words(w)
+        words.copy_(_residues(ctx, words.shape[:-2], level + 1, gen))
+    t = ctx.S // ((1 << (heads - 1).bit_length()) * dim)
+    if not fill_all:
+        kv.words(B.CM_QK)[-(-ntok // t):] = 0
+    kv.set_tokens(ntok)
+    return kv
+
+
+def _ct(ctx, words):
+    from paper_2602_11470_amd import binding as B
+    c = B.Ct(ctx, words.shape[-2] - 1)
+    c.buf[: words.numel()] = words.reshape(-1)
+    c.d.scale = ctx.scale
+    return c
+
+
+def _words(c):
+    n = c.ctx.n
+    return c.buf[: c.ncomp * (c.level + 1) * n].view(c.ncomp, c.level + 1, n)
+
+
+def _turned(ctx, coeffs, step):
+    """Coefficients of the plaintext whose slots are rotated left by step."""
+    n = ctx.n
+    e = np.arange(n) * pow(5, step % ctx.S, 2 * n) % (2 * n)
+    out = np.empty(n, dtype=np.int64)
+    out[e % n] = np.where(e < n, coeffs, -coeffs)
+    return out
+
+
+def _modadd(ctx, a, b):
+    import torch
+    q = torch.tensor([int(m) for m in ctx.moduli()[: a.shape[-2]]], device="cuda")[:, None]
+    s = a + b
+    return torch.where(s >= q, s - q, s)
+
+
+# heads, dim, r_i, index, level, tokens, what is kept, shift
+CASES = [
+    (SMALL, 4, 16, 16, True, 3, 300, "ragged", 0), (SMALL, 4, 16, 4, True, 4, 512, "pages", 0), (SMALL, 3, 32, 8, False, 3, 101, "tail", 0),
+    (SMALL, 4, 16, 4, True, 3, 300, "tail", 4), (SMALL, 4, 16, 4, True, 3, 300, "head", -3), (SMALL, 4, 16, 16, True, 4, 290, "head", -5),
+    (SMALL, 2, 64, 1, True, 3, 500, "head", -9), (SMALL, 2, 64, 8, True, 3, 300, "ragged", 11), (SMALL, 4, 128, 128, False, 3, 77, "tail", 50),
+    (SMALL, 8, 256, 16, False, 3, 200, "ragged", 0), (SMALL, 1, 1, 1, True, 3, 2000, "ragged", 0), (SMALL, 1, 1, 1, False, 3, 1, "all", 0),
+    (SMALL, 4, 16, 4, True, 3, 300, "none", 0), (SMALL, 4, 16, 4, True, 3, 0, "all", 0), (SMALL, 4, 16, 4, True, 3, 1, "all", 3),
+    (SMALL, 4, 16, 8, True, 3, 512, "all", 0), (SMALL, 4, 16, 2, True, 3, 33, "last", -1),
+    (WIDE, 4, 16, 4, True, 4, 300, "ragged", 0), (WIDE, 4, 16, 4, True, 5, 300, "head", -6),
+    (BIG, 32, 8, 4, True, 3, 700, "ragged", 0), (BIG, 32, 8, 2, True, 4, 600, "head", -3), (BIG, 12, 16, 4, False, 9, 1000, "pages", 0),
+    (BIG, 64, 32, 8, True, 3, 100, "tail", 13), (BIG, 64, 64, 64, False, 5, 400, "ragged", 0),
+]
+
+
+def _kept(what, ntok, t, shift, rng):
+    keep = np.ones(ntok, dtype=bool)
+    if what == "ragged":
+        keep = rng.uniform(size=ntok) < 0.7
+    elif what == "pages":
+        keep = np.repeat(rng.uniform(size=-(-ntok // t)) < 0.5, t)[:ntok]
+        keep[t // 2] = not keep[t // 2]
+    elif what == "tail":
+        keep[max(0, ntok - t - 3):] = False
+    elif what == "none":
+        keep[:] = False
+    elif what == "last":
+        keep[:-1] = False
+    keep[: max(0, -shift) * t] = False
+    return keep
+
+
+@pytest.mark.parametrize("add,two_step,stored_a", [(False, False, False), (True, False, False), (True, True, True)])
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "-".join(str(x) for x in c[1:]) + ("" if c[0] == SMALL else " " + c[0]))
+def test_take_equals_the_single_calls(rings, case, add, two_step, stored_a):
+    import torch
+    from oracle import packing
+    from paper_2602_11470_amd import binding as B
+    ring, heads, dim, r_i, index, level, ntok, what, shift = case
+    if stored_a and ring == BIG:
+        pytest.skip("the option changes the keys only; covered on the small rings")
+    ctx = rings(ring)
+    lay = packing.KvLayout(ctx.S, heads, dim, r_i)
+    rng = np.random.default_rng(ntok + level)
+    keep = _kept(what, ntok, lay.t, shift, rng)
+    src = _filled(ctx, heads, dim, r_i, level, index, ntok, 1)
+    dst = _filled(ctx, heads, dim, r_i, level - 1, index, 0, 2)
+    before = {w: dst.words(w).clone() for w in _which(B, index)}
+    scale = float(ctx.moduli()[level])
+    slots = [lay.keep_rows(keep)] + [lay.keep_residues(keep, c) for c in lay.partial_pages(keep)]
+    patterns = []
+    for s in slots[1:]:
+        if not any(np.array_equal(s, p) for p in patterns):
+            patterns.append(s)
+    coeffs = [ctx.encode_coeffs(s, scale) for s in [slots[0]] + patterns]
+    try:
+        ctx.set_option(B.CM_OPT_TWO_STEP_MASKS, two_step)
+        ctx.set_option(B.CM_OPT_EVK_STORED_A, stored_a)
+        sel = ctx.kv_sel(src, keep, shift, coeffs=np.stack(coeffs) if rng.uniform() < 0.5 else None)
+        assert sorted(s % ctx.S for s in sel.steps()) == ([s % ctx.S for s in lay.take_steps(shift, index)] if keep.any() else [])
+        keys = ctx.keygen_rotations(ctx.keygen_secret(1), sel.steps(), 2) if sel.steps() else None
+        ctx.kv_take(keys, sel, src, dst, add)
+    finally:
+        ctx.set_option(B.CM_OPT_TWO_STEP_MASKS, 0)
+    kept = np.flatnonzero(keep)
+    assert dst.tokens() == (kept[-1] + 1 + shift * lay.t if len(kept) else 0)
+    want = {w: torch.zeros_like(b) for w, b in before.items()}
+
+    def masked(words, c, step):
+        pt = ctx.pt_from_coeffs(_turned(ctx, c, step), level, scale, mont=True)
+        return ctx.rescale(ctx.mul_pt(_ct(ctx, words), pt))
+    pages = np.pad(keep, (0, -ntok % lay.t)).reshape(-1, lay.t)
+    for c in np.flatnonzero(pages.any(axis=1)):
+        words = src.words(B.CM_QK)[int(c)]
+        if keep[c * lay.t:(c + 1) * lay.t].all():
+            want[B.CM_QK][int(c) + shift] = words[:, :level]
+        else:
+            i = [np.array_equal(lay.keep_residues(keep, c), p) for p in patterns].index(True)
+            want[B.CM_QK][int(c) + shift] = _words(masked(words, coeffs[1 + i], 0))
+    B_ = lay.H * lay.t
+    for k in range(dim if len(kept) else 0):
+        for w, place, rows in ((B.CM_SV, lay.v_place, k % r_i), (B.CM_KV_INDEX, lay.k_index_place, -(k // r_i) * r_i)):
+            if w not in want:
+                continue
+            at = (lambda i: (i // r_i, i % r_i)) if w == B.CM_KV_INDEX else (lambda i: (i,))
+            y = masked(src.words(w)[at(k)], coeffs[0], rows * B_)
+            to, turn = place(k, shift)
+            want[w][at(to)] = _words(ctx.rotate(keys, y, turn * B_) if turn else y)
+    for w in want:
+        assert torch.equal(dst.words(w), _modadd(ctx, before[w], want[w]) if add else want[w]), w
+    ctx.set_option(B.CM_OPT_EVK_STORED_A, 0)
+
+
+@pytest.mark.parametrize("ring,heads,dim,r_i,index,level,ntok,to", [
+    (SMALL, 4, 16, 4, True, 4, 300, [4]), (SMALL, 4, 16, 4, True, 4, 300, [4, 2, 3]), (SMALL, 3, 32, 32, False, 3, 0, [2, 3]),
+    (SMALL, 4, 16, 4, True, 3, 512, [2] * 9 + [3] * 3), (SMALL, 1, 1, 1, False, 2, 1, [2]), (BIG, 32, 8, 4, True, 5, 700, [5, 3]),
+    (BIG, 12, 16, 16, False, 9, 1, [4, 9, 9, 2]), (WIDE, 4, 16, 4, True, 5, 33, [5, 2])])
+def test_fork_copies_every_page(rings, ring, heads, dim, r_i, index, level, ntok, to):
+    import torch
+    from paper_2602_11470_amd import binding as B
+    ctx = rings(ring)
+    src = _filled(ctx, heads, dim, r_i, level, index, ntok, 3, max_tokens=max(1, ntok))
+    dsts = [_filled(ctx, heads, dim, r_i, lv, index, 0, 4 + i, max_tokens=None if i % 2 else max(1, ntok)) for i, lv in enumerate(to)]
+    ctx.kv_fork(src, dsts)
+    t = ctx.S // ((1 << (heads - 1).bit_length()) * dim)
+    used = -(-ntok // t)
+    for d, lv in zip(dsts, to):
+        assert d.tokens() == ntok
+        assert torch.equal(d.words(B.CM_QK)[:used], src.words(B.CM_QK)[:used, :, : lv + 1])
+        assert not d.words(B.CM_QK)[used:].any()
+        for w in _which(B, index)[1:]:
+            assert torch.equal(d.words(w), src.words(w)[..., : lv + 1, :])
+
+
+def test_view_shows_what_export_reads(rings):
+    from paper_2602_11470_amd import binding as B
+    ctx = rings(SMALL)
+    kv = _filled(ctx, 4, 16, 4, 3, True, 300, 5)
+    for w, idx in ((B.CM_QK, 7), (B.CM_SV, 13), (B.CM_KV_INDEX, 6), (B.CM_KV_INDEX, 15)):
+        words = kv.words(w)[(idx // 4, idx % 4) if w == B.CM_KV_INDEX else idx]
+        assert np.array_equal(ctx.ct_export(_ct(ctx, words)), kv.export(w, idx))
+
+
+def test_take_matches_the_oracle(rings):
+    """Encrypted tokens, a ragged selection moved by three pages: every ciphertext limb for limb the oracle's."""
+    from oracle import ckks, packing, params, vmm
+    from paper_2602_11470_amd import binding as B
+    ctx, octx = rings(SMALL), ckks.Context(params.config1())
+    H, E, r_i, ntok, level, shift = 4, 16, 4, 200, 4, 3
+    lay = packing.KvLayout(octx.S, H, E, r_i)
+    rng = np.random.default_rng(9)
+    K, V = rng.normal(size=(2, ntok, H, E))
+    keep = rng.uniform(size=ntok) < 0.8
+    osk, gsk = octx.keygen_secret(1), ctx.keygen_secret(1)
+    scale, q = octx.prm.scale, float(octx.mod[level])
+
+    def both(slots, seed):
+        c = octx.encode_coeffs(slots, scale)
+        return octx.encrypt(osk, octx.pt_from_coeffs(c, level, scale), seed), ctx.encrypt(gsk, ctx.pt_from_coeffs(c, level, scale), seed)
+    src, dst = (ctx.kv_create(H, E, lv, r_i=r_i, key_index=True) for lv in (level, level - 1))
+    okc, ovc, oxc = [], [], []
+    for which, n, pack, mine in ((B.CM_QK, -(-ntok // lay.t), lambda c: lay.pack_k(K, c), okc), (B.CM_SV, E, lambda k: lay.pack_v(V, k), ovc),
+                                 (B.CM_KV_INDEX, E, lambda k: lay.pack_k_index(K, k), oxc)):
+        for i in range(n):
+            o, g = both(pack(i), 100 * which + i)
+            mine.append(o)
+            src.load(which, i, g)
+    src.set_tokens(ntok)
+    patterns = []
+    for c in lay.partial_pages(keep):
+        if not any(np.array_equal(lay.keep_residues(keep, c), p) for p in patterns):
+            patterns.append(lay.keep_residues(keep, c))
+    coeffs = [octx.encode_coeffs(s, q) for s in [lay.keep_rows(keep)] + patterns]
+    sel = ctx.kv_sel(src, keep, shift, coeffs=np.stack(coeffs))
+    okeys = octx.keygen_rotations(osk, lay.take_steps(shift, True), 2)
+    ctx.kv_take(ctx.keygen_rotations(gsk, sel.steps(), 2), sel, src, dst)
+    pt = lambda c: octx.pt_from_coeffs(c, level, q)  # noqa: E731
+    row_masks = {r: pt(_turned(ctx, coeffs[0], r * lay.H * lay.t)) for r in range(E)}
+    page_masks = {c: pt(coeffs[1 + [np.array_equal(lay.keep_residues(keep, c), p) for p in patterns].index(True)]) for c in lay.partial_pages(keep)}
+    ok, ov, ox = vmm.kv_take(vmm.CkksOps(octx, okeys), lay, okc, ovc, keep, shift, row_masks, page_masks, oxc)
+    for c in range(E):
+        if c in ok:
+            assert np.array_equal(dst.export(B.CM_QK, c), octx.canonical(ok[c])), c
+        assert np.array_equal(dst.export(B.CM_SV, c), octx.canonical(ov[c])), c
+        assert np.array_equal(dst.export(B.CM_KV_INDEX, c), octx.canonical(ox[c])), c
+
+
+def test_refusals(rings):
+    import ctypes as C
+    from paper_2602_11470_amd import binding as B
+    ctx, other = rings(SMALL), B.config1()
+    made = dict(heads=4, dim=16, r_i=4, index=True)
+    src = _filled(ctx, level=4, ntok=100, seed=1, **made)
+    kv = lambda level=3, ctx=ctx, **kw: ctx.kv_create(kw.get("heads", 4), kw.get("dim", 16), level, r_i=kw.get("r_i", 4), max_tokens=kw.get("room"),  # noqa: E731
+                                                      key_index=kw.get("index", True))
+
+    def status(f):
+        try:
+            f()
+        except B.CachemirError as e:
+            return e.status
+        return 0
+    good, foreign = kv(), kv(ctx=other)
+    # forks
+    assert status(lambda: ctx.kv_fork(src, [])) == -1
+    assert status(lambda: ctx.kv_fork(src, [src])) == -1
+    assert status(lambda: ctx.kv_fork(src, [good, good])) == -1
+    assert status(lambda: ctx.kv_fork(src, [foreign])) == -1
+    assert status(lambda: other.kv_fork(src, [good])) == -1
+    assert status(lambda: ctx.kv_fork(good, [src])) == -2                     # a copy cannot gain a level
+    for bad in (kv(heads=2), kv(dim=32), kv(r_i=8), kv(index=False), kv(room=99)):
+        assert status(lambda: ctx.kv_fork(src, [bad])) == -5
+    seeked = _filled(ctx, level=4, ntok=10, seed=1, **made)
+    seeked.seek(200)
+    assert status(lambda: ctx.kv_fork(seeked, [kv(room=100)])) == -5          # the next append would lie outside
+    # selections
+    keep = np.ones(100, dtype=bool)
+    assert status(lambda: ctx.kv_sel(kv(level=2), keep)) == -2
+    assert status(lambda: ctx.kv_sel(src, keep, 16)) == -5
+    assert status(lambda: ctx.kv_sel(src, keep, -16)) == -5
+    assert status(lambda: ctx.kv_sel(src, keep, -1)) == -5                    # page 0 is kept and would go to page -1
+    assert status(lambda: ctx.kv_sel(src, keep, 13)) == -5                    # page 3 would go to page 16
+    assert status(lambda: ctx.kv_sel(src, np.ones(513, dtype=bool))) == -5
+    assert status(lambda: other.kv_sel(src, keep)) == -1
+    h = C.c_void_p()
+    assert B.lib.cm_kv_sel_create(ctx.h, src.h, None, 3, 0, None, C.byref(h)) == -1
+    assert B.lib.cm_kv_sel_create(ctx.h, src.h, None, -1, 0, None, C.byref(h)) == -1
+    # takes
+    sel, moved = ctx.kv_sel(src, keep), ctx.kv_sel(src, keep, 3)
+    assert sel.steps() == [] and len(moved.steps()) > 0
+    assert status(lambda: ctx.kv_take(None, sel, src, src)) == -1
+    assert status(lambda: ctx.kv_take(None, moved, src, good)) == -1          # keys are needed
+    assert status(lambda: ctx.kv_take(ctx.keygen_rotations(ctx.keygen_secret(1), moved.steps()[:1], 2), moved, src, good)) == -4
+    assert status(lambda: ctx.kv_take(None, sel, src, foreign)) == -1
+    assert status(lambda: ctx.kv_take(None, sel, src, kv(level=4))) == -2
+    assert status(lambda: ctx.kv_take(None, sel, src, kv(level=2))) == -2
+    assert status(lambda: ctx.kv_take(None, sel, kv(level=3), kv(level=2))) == -2
+    for bad in (kv(heads=2), kv(dim=32), kv(r_i=8), kv(index=False), kv(room=99)):
+        assert status(lambda: ctx.kv_take(None, sel, src, bad)) == -5
+    src.set_tokens(101)
+    assert status(lambda: ctx.kv_take(None, sel, src, good)) == -5            # a token that the selection knows nothing of
+    src.set_tokens(100)
+    assert status(lambda: ctx.kv_take(None, sel, src, kv(room=100))) == 0
+    far = kv(level=3)
+    far.load(B.CM_QK, 0, _ct(ctx, good.words(B.CM_QK)[0]))
+    src.load(B.CM_QK, 0, _ct(ctx, src.words(B.CM_QK)[0]))
+    c = _ct(ctx, far.words(B.CM_QK)[0])
+    c.d.scale *= 2
+    twice = kv(level=3)
+    twice.load(B.CM_QK, 0, c)
+    assert status(lambda: ctx.kv_take(None, sel, src, twice, add=True)) == -3
+    assert status(lambda: ctx.kv_take(None, sel, src, far, add=True)) == 0
+    # places of appends, views
+    assert status(lambda: good.seek(-1)) == -1 and status(lambda: good.seek(513)) == -1 and status(lambda: good.seek(512)) == 0
+    assert status(lambda: kv(index=False).words(B.CM_KV_INDEX)) == -1
+    d = B.cm_ct()
+    assert B.lib.cm_kv_view(good.h, B.CM_SV, 16, C.byref(d)) == -5 and B.lib.cm_kv_view(good.h, B.CM_SV, -1, C.byref(d)) == -5
+    other.close()
+
+
+@pytest.mark.parametrize("side_stream", [False, True])
+def test_captured_and_replayed(rings, side_stream):
+    """Fork and take (masked and moved) in a graph: every replay equals the eager calls, with eager work between the replays."""
+    import torch
+    from paper_2602_11470_amd import binding as B
+    ctx = rings(SMALL)
+    src = _filled(ctx, 4, 16, 4, 4, True, 300, 1)
+    copies, taken = [_filled(ctx, 4, 16, 4, lv, True, 0, 2) for lv in (4, 3)], _filled(ctx, 4, 16, 4, 3, True, 0, 3)
+    keep = np.ones(300, dtype=bool)
+    keep[[5, 70, 71, 299]] = False
+    sel = ctx.kv_sel(src, keep, 2)
+    keys = ctx.keygen_rotations(ctx.keygen_secret(1), sel.steps(), 2)
+
+    def work():
+        ctx.kv_fork(src, copies)
+        ctx.kv_take(keys, sel, src, taken)
+        ctx.kv_take(keys, sel, src, copies[1], add=True)
+    stream = torch.cuda.Stream() if side_stream else torch.cuda.current_stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        work()
+    torch.cuda.synchronize()
+    all_words = lambda: [c.words(w).clone() for c in copies + [taken] for w in _which(B, True)]  # noqa: E731
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        work()
+    for seed in (11, 12, 13):
+        gen = torch.Generator(device="cuda").manual_seed(seed)
+        for w in _which(B, True):
+            src.words(w).copy_(_residues(ctx, src.words(w).shape[:-2], 5, gen))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = all_words()
+        for c in copies + [taken]:
+            for w in _which(B, True):
+                c.words(w).zero_()
+        work()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, all_words()))
+
+
+def test_a_session_that_forks_rolls_back_and_slides(rings):
+    """Appends, a fork, rejected drafts taken back on one branch, the window moved by whole pages and more appends, another branch
+    put behind the first, an append into a freed page: after every step q K^T and scores V of the cache are those of the token list."""
+    from oracle import packing
+    from paper_2602_11470_amd import binding as B
+    ctx = B.Context(4096, 12, 2, 2, 50, 50, 60, 2.0 ** 50)
+    try:
+        H, E, r_i = 4, 16, 4
+        lay = packing.KvLayout(ctx.S, H, E, r_i)
+        t, rng = lay.t, np.random.default_rng(3)
+        sk = ctx.keygen_secret(1)
+        kv = ctx.kv_create(H, E, 9, r_i=r_i, key_index=True)
+        steps = set(kv.steps())
+        keys = None
+        K, V = [np.zeros((lay.capacity, H, E)) for _ in range(2)]
+
+        def enc(slots, level, seed):
+            return ctx.encrypt(sk, ctx.encode(slots, level), seed)
+
+        def append(cache, K, V, n, seed):
+            k, v = rng.normal(size=(2, H, E))
+            K[n], V[n] = k, v
+            cache.append(keys, enc(lay.pack_vec(k, n % t), cache.level + 1, seed), enc(lay.pack_vec(v, n % t), cache.level + 1, seed + 1))
+
+        def group(cache, K, V, c, seed):
+            k, v = rng.normal(size=(2, t, H, E))
+            K[c * t:c * t + t], V[c * t:c * t + t] = k, v
+            pack = lambda a: sum(lay.pack_vec(a[r], r) for r in range(t))  # noqa: E731
+            cache.append_group(keys, enc(pack(k), cache.level + 1, seed), enc(pack(v), cache.level + 1, seed + 1))
+
+        def check(cache, K, V):
+            q, s = rng.normal(size=(H, E)), rng.uniform(size=(H, lay.capacity))
+            got = ctx.decrypt(sk, ctx.vmm_kv(keys, cache, B.CM_QK, enc(lay.pack_vec(q), cache.level, 5))).real
+            assert np.abs(got - lay.pack_scores(np.einsum("he,nhe->hn", q, K))).max() < 1e-4
+            got = ctx.decrypt(sk, ctx.vmm_kv(keys, cache, B.CM_SV, enc(lay.pack_scores(s), cache.level, 6))).real
+            assert np.abs(lay.unpack_vec(got) - np.einsum("hn,nhe->he", s, V)).max() < 1e-4
+        # keys for everything that follows
+        probe = ctx.kv_create(H, E, 9, r_i=r_i, key_index=True)
+        for sh in (-2, 5):
+            steps |= set(ctx.kv_sel(probe, np.arange(3 * t) >= 2 * t, sh).steps())
+        keys = ctx.keygen_rotations(sk, sorted(steps), 2, with_relin=True)
+        for c in range(5):
+            group(kv, K, V, c, 100 + 10 * c)
+        for n in range(5 * t, 5 * t + 3):
+            append(kv, K, V, n, 300 + 2 * n)
+        check(kv, K, V)
+        a, b = (ctx.kv_create(H, E, lv, r_i=r_i, key_index=True) for lv in (9, 7))
+        ctx.kv_fork(kv, [a, b])
+        append(a, K, V, 5 * t + 3, 900)                         # a draft on branch a
+        check(a, K, V)
+        assert a.tokens() == 5 * t + 4 and b.tokens() == kv.tokens() == 5 * t + 3
+        # four tokens of branch a are taken back
+        keep = np.arange(a.tokens()) < 5 * t
+        a8 = ctx.kv_create(H, E, 8, r_i=r_i, key_index=True)
+        ctx.kv_take(None, ctx.kv_sel(a, keep), a, a8)
+        Ka, Va = K.copy(), V.copy()
+        Ka[5 * t:], Va[5 * t:] = 0, 0
+        assert a8.tokens() == 5 * t
+        check(a8, Ka, Va)
+        # the oldest two pages leave, the others move down, and the next token comes behind them
+        a7 = ctx.kv_create(H, E, 7, r_i=r_i, key_index=True)
+        ctx.kv_take(keys, ctx.kv_sel(a8, np.arange(5 * t) >= 2 * t, -2), a8, a7)
+        Ka, Va = (np.concatenate([x[2 * t:5 * t], np.zeros_like(x[3 * t:])]) for x in (Ka, Va))
+        assert a7.tokens() == 3 * t
+        append(a7, Ka, Va, 3 * t, 1000)
+        check(a7, Ka, Va)
+        # the first three pages and a bit of branch b behind branch a, five pages on
+        keep = (np.arange(b.tokens()) < 3 * t + 5) & (np.arange(b.tokens()) % 7 != 3)
+        both = ctx.kv_create(H, E, 6, r_i=r_i, key_index=True)
+        ctx.kv_fork(a7, [both])
+        ctx.kv_take(keys, ctx.kv_sel(b, keep, 5), b, both, add=True)
+        for n in np.flatnonzero(keep):
+            Ka[n + 5 * t], Va[n + 5 * t] = K[n], V[n]
+        assert both.tokens() == np.flatnonzero(keep)[-1] + 1 + 5 * t
+        check(both, Ka, Va)
+        # page 1 is freed and filled again while the others stay
+        n = both.tokens()
+        keep = np.ones(n, dtype=bool)
+        keep[t:2 * t] = False
+        ring = ctx.kv_create(H, E, 5, r_i=r_i, key_index=True)
+        ctx.kv_take(None, ctx.kv_sel(both, keep), both, ring)
+        Ka[t:2 * t], Va[t:2 * t] = 0, 0
+        check(ring, Ka, Va)
+        ring.seek(t)
+        append(ring, Ka, Va, t, 2000)
+        append(ring, Ka, Va, t + 1, 2002)
+        assert ring.tokens() == n
+        check(ring, Ka, Va)
+        # everything dropped: an empty cache that takes tokens again
+        empty = ctx.kv_create(H, E, 4, r_i=r_i, key_index=True)
+        ctx.kv_take(None, ctx.kv_sel(ring, np.zeros(n, dtype=bool)), ring, empty)
+        assert empty.tokens() == 0
+        K0, V0 = np.zeros_like(K), np.zeros_like(V)
+        append(empty, K0, V0, 0, 3000)
+        check(empty, K0, V0)
+    finally:
+        ctx.close()

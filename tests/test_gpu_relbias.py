@@ -1,0 +1,270 @@
+"""Relative position bias on encrypted scores (cm_relbias_*): limb for limb against the sum with the plaintexts it stands for, the
+library's own plaintexts against the oracle's slots, and together with q K^T of decode steps, grouped queries and prompt groups."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def rings():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    from paper_2602_11470_amd import binding as B
+    made = {}
+
+    def get(name):
+        if name not in made:
+            made[name] = {"small": B.config1, "big": lambda: B.llama_ring(24, 4), "wide": lambda: B.Context(4096, 6, 2, 2, 58, 54, 60, 2.0 ** 50)}[name]()
+        return made[name]
+    yield get
+    for c in made.values():
+        c.close()
+
+
+def _random(ctx, level, gen):
+    import torch
+    from paper_2602_11470_amd import binding as B
+    c = B.Ct(ctx, level)
+    v = c.buf[: 2 * (level + 1) * ctx.n].view(2, level + 1, ctx.n)
+    for i, q in enumerate(ctx.moduli()[: level + 1]):
+        v[:, i] = torch.empty(2, ctx.n, dtype=torch.int64, device="cuda").random_(0, int(q), generator=gen)
+    c.d.scale = ctx.scale
+    return c
+
+
+def _words(c):
+    return c.buf[: 2 * (c.level + 1) * c.ctx.n].view(2, c.level + 1, c.ctx.n)
+
+
+def _turned(ctx, coeffs, step):
+    n = ctx.n
+    e = np.arange(n) * pow(5, step % ctx.S, 2 * n) % (2 * n)
+    out = np.empty(n, dtype=np.int64)
+    out[e % n] = np.where(e < n, coeffs, -coeffs)
+    return out
+
+
+def _plain_sum(ctx, c, coeff_list):
+    """c plus the plaintexts of integer coefficients (their sum may pass 64 bits: one after the other)."""
+    import torch
+    q = torch.tensor([int(m) for m in ctx.moduli()[: c.level + 1]], device="cuda")[:, None]
+    out = _words(c).clone()
+    for co in coeff_list:
+        pt = ctx.pt_from_coeffs(co, c.level, c.scale)
+        s = out[0] + pt.buf.view(c.level + 1, ctx.n)
+        out[0] = torch.where(s >= q, s - q, s)
+    return out
+
+
+# ring, heads, dim, group, prompt, level, token, first
+CASES = [
+    ("small", 4, 16, 1, False, 2, 77, -1), ("small", 4, 16, 1, False, 0, 511, 96), ("small", 3, 32, 2, False, 4, 0, 0), ("small", 4, 128, 4, False, 3, 300, 500),
+    ("small", 2, 64, 4, True, 1, 508, 32), ("small", 4, 16, 1, True, 2, 64, -1), ("small", 1, 16, 2, True, 1, 1920, 128), ("small", 1, 1, 1, False, 1, 2047, -1),
+    ("small", 1, 1, 1, False, 1, 2047, 0), ("small", 8, 256, 1, True, 3, 255, 0), ("small", 1, 2048, 1, False, 3, 5, 7),
+    ("wide", 4, 16, 1, False, 5, 300, 320), ("wide", 4, 32, 2, True, 3, 120, 16),
+    ("big", 32, 128, 1, False, 9, 1000, 8), ("big", 8, 128, 4, False, 3, 4095, 2016), ("big", 12, 64, 1, True, 2, 96, -1),
+]
+
+
+@pytest.mark.parametrize("case", CASES, ids=str)
+def test_adds_the_plaintexts(rings, case):
+    """Given coefficients (random ones, the size of a bias): every pass, out of place and in place, and a part of the passes."""
+    import torch
+    from oracle import packing
+    ring, heads, dim, group, prompt, level, token, first = case
+    ctx = rings(ring)
+    lay = packing.KvLayout(ctx.S, heads, dim)
+    t_kv, cap = lay.t, dim * lay.t
+    passes, phases = (t_kv, group) if prompt else (group, t_kv)
+    rng = np.random.default_rng(token + level)
+    coeffs = rng.integers(-(1 << 55), 1 << 55, size=(passes * phases + 1, ctx.n))
+    bucket, table = rng.integers(0, 5, cap), rng.normal(size=(heads * group, 5))
+    mask = -20.0 if first >= 0 else 0.0
+    bias = ctx.relbias(heads, dim, table, bucket, level, group=group, prompt=prompt, mask=mask, coeffs=coeffs)
+    assert bias.passes == passes
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    scores = [_random(ctx, level, gen) for _ in range(passes)]
+    before = [_words(s).clone() for s in scores]
+    row, page = lay.H * t_kv, token // t_kv
+    hidden = []
+    if first >= 0:
+        seen = (page - first // t_kv) % dim + 1
+        hidden = [_turned(ctx, coeffs[-1], -(first // t_kv + i) * row) for i in range(seen, dim)]
+    phase = token % t_kv // (t_kv // phases)
+    check = sorted({0, passes - 1, passes // 2})                             # of many passes, some
+    want = {p: _plain_sum(ctx, scores[p], [_turned(ctx, coeffs[p * phases + phase], -page * row)] + hidden) for p in check}
+    outs = ctx.relbias_apply(bias, token, scores, first=first)
+    for p in range(passes):
+        assert torch.equal(_words(scores[p]), before[p]) and torch.equal(_words(outs[p])[1], before[p][1])
+        assert outs[p].level == level and outs[p].scale == scores[p].scale
+    assert all(torch.equal(_words(outs[p]), want[p]) for p in check)
+    some = ctx.relbias_apply(bias, token, scores[passes // 2:], first=first, pass0=passes // 2)
+    assert all(torch.equal(_words(a), _words(b)) for a, b in zip(some, outs[passes // 2:]))
+    again = ctx.relbias_apply(bias, token, scores, first=first, outs=scores)
+    assert again is scores and all(torch.equal(_words(a), _words(b)) for a, b in zip(scores, outs))
+
+
+@pytest.mark.parametrize("heads,dim,group,prompt,token,first", [(4, 16, 1, False, 333, -1), (3, 64, 4, False, 100, 48), (4, 128, 2, True, 250, 8),
+                                                               (4, 64, 1, True, 64, 480)])
+def test_own_plaintexts_are_the_oracles_slots(rings, heads, dim, group, prompt, token, first):
+    """Encoded by the library: decrypted scores differ by the oracle's slots.  The sum of up to `dim` encodings is off by half a
+    unit of the scale each in every coefficient, at most dim * n / 2 / scale in a slot, next to the noise of one encryption."""
+    from oracle import packing
+    ctx = rings("wide")
+    sk = ctx.keygen_secret(1)
+    lay = packing.KvLayout(ctx.S, heads, dim)
+    rng = np.random.default_rng(dim)
+    cap, level = dim * lay.t, 3
+    table, bucket = rng.normal(size=(heads * group, 9)), rng.integers(0, 9, cap)
+    bias = ctx.relbias(heads, dim, table, bucket, level, group=group, prompt=prompt, mask=-30.0)
+    z = [rng.normal(size=ctx.S) for _ in range(bias.passes)]
+    scores = [ctx.encrypt(sk, ctx.encode(v, level), 50 + i) for i, v in enumerate(z)]
+    outs = ctx.relbias_apply(bias, token, scores, first=first)
+    for d in sorted({0, 1 % bias.passes, bias.passes - 1}):
+        want = z[d] + lay.bias_slots(table, bucket, token, first if first >= 0 else None, -30.0, group, d, prompt)
+        got = ctx.decrypt(sk, outs[d])
+        noise = np.abs(ctx.decrypt(sk, scores[d]) - z[d]).max()
+        assert np.abs(got - want).max() <= noise + dim * ctx.n / 2 / ctx.scale + 1e-12 * 64
+
+
+def test_with_the_scores_of_decode_steps_groups_and_prompts(rings):
+    """q K^T, then the bias, decrypted: a decode step, four passes of a grouped query, and a prompt group in all its passes on a grouped
+    cache (as many passes as tokens in a page), with the pages of another sequence hidden and causal inside the page."""
+    from oracle import packing
+    from paper_2602_11470_amd import binding as B
+    ctx = rings("wide")
+    sk = ctx.keygen_secret(1)
+    Hkv, E, G = 2, 128, 4
+    lay = packing.KvLayout(ctx.S, Hkv, E, 16)
+    t_kv, cap, ntok = lay.t, E * lay.t, 101
+    t, rng = t_kv // G, np.random.default_rng(2)
+    K = rng.normal(size=(ntok, Hkv, E)) * 0.2
+    kv = ctx.kv_create(Hkv, E, 4, r_i=16, key_index=True, unrolled_ladders=True)
+    for k in range(E):
+        kv.load(B.CM_KV_INDEX, k, ctx.encrypt(sk, ctx.encode(lay.pack_k_index(K, k), 4), 100 + k))
+    kv.set_tokens(ntok)
+    decode, prompt = ctx.gqa(kv, G), ctx.gqa(kv, t_kv)
+    keys = ctx.keygen_rotations(sk, sorted(set(kv.steps() + decode.steps() + prompt.steps())), 2, with_relin=True)
+    half = 8
+    bucket = np.where(np.arange(cap) > cap - t_kv, half, np.minimum(np.arange(cap) // 4, half - 1))
+    table = np.concatenate([rng.normal(size=(Hkv * G, half)), np.full((Hkv * G, 1), -40.0)], 1)
+    full = np.zeros((cap, Hkv, E))
+    full[:ntok] = K
+    for gqa, is_prompt, token, first in ((decode, False, ntok, 40), (prompt, True, 56 + t, 24)):
+        # a query: heads (hk, g) and, in a prompt, the t tokens of the group, in the runs of a block
+        q = rng.normal(size=(t if is_prompt else 1, Hkv, G, E)) * 0.2
+        slots = np.zeros(ctx.S)
+        for e in range(E):
+            for hk in range(Hkv):
+                for g in range(G):
+                    for tau in range(len(q)):
+                        slots[lay.slot(e, hk, g * t + tau)] = q[tau, hk, g, e]
+        scores = ctx.gqa_qk(keys, gqa, ctx.encrypt(sk, ctx.encode(slots, 5), 9))
+        bias = ctx.relbias(Hkv, E, table, bucket, scores[0].level, scores[0].scale, group=G, prompt=is_prompt, mask=-40.0)
+        assert bias.passes == len(scores)
+        ctx.relbias_apply(bias, token, scores, first=first, outs=scores)
+        vecs = [ctx.decrypt(sk, s).real for s in scores]
+        for hk in range(Hkv):
+            for g in range(G):
+                for tau in range(len(q)):
+                    for key in range(cap):
+                        c, j = key // t_kv, key % t_kv
+                        delta = (j - (g * t + tau)) % t_kv if is_prompt else (j // t - g) % G
+                        got, dot = vecs[delta][lay.slot(c, hk, j)], q[tau, hk, g] @ full[key, hk]
+                        if first <= key <= token + tau:
+                            assert abs(got - dot - table[hk * G + g][bucket[token + tau - key]]) < 1e-4
+                        else:
+                            assert got - dot < -30.0
+
+
+def test_refusals(rings):
+    import ctypes as C
+    import torch
+    from paper_2602_11470_amd import binding as B
+    ctx, other = rings("small"), B.config1()
+    table, bucket = np.zeros((8, 3)), np.zeros(512, dtype=np.int32)
+
+    def status(f):
+        try:
+            f()
+        except B.CachemirError as e:
+            return e.status
+        return 0
+    make = lambda heads=4, dim=16, level=2, scale=0.0, group=2, table=table, bucket=bucket, **kw: ctx.relbias(heads, dim, table, bucket, level, scale, group, **kw)  # noqa: E731
+    assert status(make) == 0
+    assert status(lambda: make(level=-1)) == -2 and status(lambda: make(level=5)) == -2
+    assert status(lambda: make(group=3, table=np.zeros((12, 3)))) == -5
+    assert status(lambda: make(group=64, table=np.zeros((256, 3)))) == -5             # more runs than residues
+    assert status(lambda: make(dim=24)) == -5
+    assert status(lambda: make(dim=1024)) == -5
+    assert status(lambda: make(dim=0)) == -1 and status(lambda: make(group=0, table=np.zeros((0, 3)))) == -1
+    assert status(lambda: make(table=np.zeros((8, 0)))) == -1
+    assert status(lambda: make(scale=-1.0)) == -1 and status(lambda: make(scale=float("nan"))) == -1 and status(lambda: make(scale=float("inf"))) == -1
+    assert status(lambda: make(mask=float("-inf"))) == -1 and status(lambda: make(mask=2.0 ** 21)) == -1    # 2^21 * 2^40 does not fit
+    assert status(lambda: make(table=np.full((8, 3), np.nan))) == -1 and status(lambda: make(table=np.full((8, 3), -(2.0 ** 21)))) == -1
+    assert status(lambda: make(table=np.full((8, 3), np.inf))) == -1
+    for bad in (-1, 3):
+        b = bucket.copy()
+        b[511] = bad
+        assert status(lambda: make(bucket=b)) == -1
+    h = C.c_void_p()
+    args = [ctx.h, 4, 16, 2, 0, 2, 0.0, 3, table.ctypes.data, bucket.ctypes.data, 0.0, None, C.byref(h)]
+    for i in (0, 8, 9, 12):
+        assert B.lib.cm_relbias_create(*[None if j == i else a for j, a in enumerate(args)]) == -1
+    assert B.lib.cm_relbias_create(*[2 if j == 4 else a for j, a in enumerate(args)]) == -1
+    bias, plain, prompt = make(mask=-9.0), make(), make(prompt=True)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    s = [_random(ctx, 2, gen) for _ in range(3)]
+    before = [_words(x).clone() for x in s]
+    two, apply = s[:2], ctx.relbias_apply
+    for token, first in ((-1, -1), (512, -1), (0, -2), (0, 31), (0, 512)):
+        assert status(lambda: apply(bias, token, two, first=first)) == -5
+    assert status(lambda: apply(plain, 0, two, first=0)) == -5                       # made without a mask
+    assert status(lambda: apply(prompt, 8, two)) == -5                               # not the first token of a group of 16
+    assert status(lambda: apply(bias, 0, s)) == -5                                   # three of two passes
+    assert status(lambda: apply(bias, 0, two, pass0=1)) == -5 and status(lambda: apply(bias, 0, two, pass0=-1)) == -1
+    assert status(lambda: apply(bias, 0, two, pass0=2 ** 31 - 1)) == -5
+    assert status(lambda: apply(bias, 0, [])) == -1
+    assert status(lambda: apply(bias, 0, two, outs=two[::-1])) == -1                 # another pass's input
+    assert status(lambda: apply(bias, 0, two, outs=[s[2], s[2]])) == -1
+    assert status(lambda: apply(bias, 0, [two[0], two[0]], outs=[two[0], s[2]])) == -1
+    assert status(lambda: apply(bias, 0, [two[0], _random(ctx, 3, gen)])) == -2
+    odd = _random(ctx, 2, gen)
+    odd.d.scale *= 1.001
+    assert status(lambda: apply(bias, 0, [two[0], odd])) == -3
+    odd.d.scale = float("nan")
+    assert status(lambda: apply(bias, 0, [odd])) == -3
+    three = _random(ctx, 2, gen)
+    three.d.ncomp = 3
+    assert status(lambda: apply(bias, 0, [three])) == -1
+    assert status(lambda: other.relbias_apply(bias, 0, two)) == -1
+    assert all(torch.equal(_words(x), b) for x, b in zip(s, before))
+    other.close()
+
+
+def test_captured_and_replayed(rings):
+    import torch
+    ctx = rings("small")
+    rng = np.random.default_rng(1)
+    bias = ctx.relbias(4, 16, rng.normal(size=(8, 3)), rng.integers(0, 3, 512), 2, group=2, mask=-5.0)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    scores, outs = ([_random(ctx, 2, gen) for _ in range(2)] for _ in range(2))
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        ctx.relbias_apply(bias, 100, scores, first=64, outs=outs)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ctx.relbias_apply(bias, 100, scores, first=64, outs=outs)
+        ctx.relbias_apply(bias, 33, outs, first=480, outs=outs)
+    for _ in range(3):
+        for s in scores:
+            _words(s).copy_(_words(_random(ctx, 2, gen)))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [_words(o).clone() for o in outs]
+        eager = ctx.relbias_apply(bias, 33, ctx.relbias_apply(bias, 100, scores, first=64), first=480)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, _words(b)) for a, b in zip(got, eager))
