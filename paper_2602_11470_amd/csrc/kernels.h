@@ -31,10 +31,11 @@ void launch_to_mont(cm_ctx *ctx, u64 *data, const int *d_mod_idx, int limbs, hip
 void launch_from_mont(cm_ctx *ctx, u64 *out, const u64 *in, const int *d_mod_idx, int limbs, hipStream_t st);
 void launch_add(cm_ctx *ctx, u64 *out, const u64 *a, const u64 *b, int ncomp, int limbs, hipStream_t st);
 void launch_mul_pt(cm_ctx *ctx, u64 *out, const u64 *a, const u64 *pt_mont, int ncomp, int limbs, hipStream_t st);
-// out[z][2][limbs][n] = src[z] * (pt rotated by the Galois element g[z]) for z < cnt <= CM_MASK_BATCH
+// out[z][2][limbs][n] = src[z] * (plaintext at[z] of an array pt[..][limbs][n], rotated by the Galois element g[z]) for z < cnt <= CM_MASK_BATCH
 struct MulPtBatch {
     const u64 *src[CM_MASK_BATCH];
     unsigned g[CM_MASK_BATCH];
+    unsigned at[CM_MASK_BATCH] = {};
 };
 void launch_mul_pt_rot_batch(cm_ctx *ctx, u64 *out, const MulPtBatch &b, int cnt, const u64 *pt_mont, int limbs, hipStream_t st);
 // the same products on the last of the `limbs` limbs only: out[z][2][n]
@@ -181,13 +182,17 @@ struct FinishBatch {
     // u_r is not stored but formed on the fly as u[r] * (mul_pt read through the Galois map mul_g[r]): the masked
     // products of a cache append, whose rescale is this tail (mul_pt[ext][n], multiplier form; nullable)
     const u64 *mul_pt = nullptr;
-    unsigned mul_g[CM_MASK_BATCH] = {};
+    unsigned mul_g[CM_MASK_BATCH] = {}, mul_at[CM_MASK_BATCH] = {};
 };
 void launch_cols_inv(cm_ctx *ctx, u64 *data, const int *d_rows, const int *d_mod_idx, int limbs, hipStream_t st);
 // forward transform of conv[items*ncomp*(level+1)][n] (mods 0..level repeating) with that tail
 // with src: the first pass reads row d_src_rows[i] of src for limb i (words below twice that limb's modulus) instead of conv
 void launch_ntt_fwd_finish(cm_ctx *ctx, u64 *conv, const int *d_mods, const FinishBatch &fb, hipStream_t st,
                            const u64 *src = nullptr, const int *d_src_rows = nullptr);
+// The masked products of fb rescaled: out_r = (u_r mask_r - the last limb's residues) q_level^-1 (+ accum_r), fb.ext = level + 1.  The residues
+// of the last limb have to fit the other moduli as they are.  scratch: last[2 items][n] and red[2 items][level][n].
+void launch_masked_rescale(cm_ctx *ctx, const FinishBatch &fb, u64 *last, u64 *red, const int *d_last_mods, const int *d_red_mods, const int *d_red_src,
+                           hipStream_t st);
 
 // Base conversion of `batch` items and the forward transform of the results.  Item z: table (z % tab_period)*tab_step
 // (tab_period 0 = batch), input (z / in_group)*in_stride, output z*out_stride; own_src: the items' own source rows are
@@ -212,7 +217,7 @@ void launch_conv_ntt(cm_ctx *ctx, const ConvBatch &b, u64 *out, const u64 *in, h
 
 // ops.hip internals shared with vmm.hip
 int rescale_masked_batch(cm_ctx *ctx, int level, size_t words);
-bool rescale_masked_into(cm_ctx *ctx, const MulPtBatch &mb, int cnt, const u64 *pt, int level, u64 *out, hipStream_t st,
+bool rescale_masked_into(cm_ctx *ctx, const MulPtBatch &mb, int cnt, const u64 *pt, int level, u64 *const *outs, hipStream_t st,
                          u64 *last, u64 *red, bool accumulate);
 struct KsLevel {            // cached per level: which rows of the digit array are converted / transformed
     int level, ext, beta;
@@ -264,7 +269,9 @@ cm_status moddown_second_keep(cm_ctx *ctx, const u64 *R, int level, u64 *out, hi
 // the same for m <= CM_KS_BATCH stacked R[r] = [2][ext][n]: outs[r] + (level+1)*n <- ModDown(R[r][1])
 cm_status moddown_second_keep_many(cm_ctx *ctx, const u64 *Rs, int level, int m, u64 *const *outs, hipStream_t st);
 cm_status moddown_many(cm_ctx *ctx, u64 *us, int level, int cnt, u64 *const *outs, hipStream_t st);
-// one batch (m <= CM_KS_BATCH): outs[r] = ModDown(us + r*2*ext*n) + perm_g(addends[r]) on the first addend_comps
+// key switches that one moddown_batch_into takes at a level, at least CM_KS_BATCH, at most CM_MASK_BATCH
+int ks_batch_max(const cm_ctx *ctx, int level);
+// one batch (m <= ks_batch_max): outs[r] = ModDown(us + r*2*ext*n) + perm_g(addends[r]) on the first addend_comps
 // components (+ accums[r]); addends / accums nullable arrays of nullable pointers
 cm_status moddown_batch_into(cm_ctx *ctx, u64 *us, int level, int m, const u64 *const *addends, int addend_comps, u64 g,
                              const u64 *const *accums, u64 *const *outs, hipStream_t st, bool rows_done = false);
@@ -293,7 +300,7 @@ cm_status moddown_rescale_into(cm_ctx *ctx, u64 *u, int level, u64 *tmp, u64 *ou
 // out[2][level][n] = rescale(Rot(in) + accum) (+ extra as rotate_into), likewise
 cm_status rotate_rescale_into(cm_ctx *ctx, const u64 *key, const u64 *in, int level, u64 g, u64 *tmp, u64 *out, hipStream_t st,
                               const u64 *accum = nullptr, const u64 *extra = nullptr);
-// room for CM_KS_BATCH key-switch sums [2][L+1+K][n] (what moddown_batch_into consumes)
+// room for the key-switch sums [2][ext][n] of one moddown_batch_into
 u64 *arena_batch_sums(const cm_ctx *ctx);
 cm_status ks_apply_many(cm_ctx *ctx, const u64 *digits, int level, int cnt, const u64 *const *keys, const u64 *gs,
                         const u64 *in, u64 *const *outs, hipStream_t st);

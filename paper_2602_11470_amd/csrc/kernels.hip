@@ -88,7 +88,7 @@ __global__ void k_mul_pt_rot_batch(u64 *__restrict__ out, MulPtBatch b, const u6
     const ModC m = modc[l];
     const unsigned g = b.g[z];
     const unsigned s = g ? perm_src(i, g, logn) : i;
-    out[((size_t)z * 2 * limbs + r) * n + i] = redc((u128)b.src[z][(size_t)r * n + i] * pt_mont[(size_t)l * n + s], m.q, m.qinv);
+    out[((size_t)z * 2 * limbs + r) * n + i] = redc((u128)b.src[z][(size_t)r * n + i] * pt_mont[((size_t)b.at[z] * limbs + l) * n + s], m.q, m.qinv);
 }
 __global__ void k_mul_pt_rot_last(u64 *__restrict__ out, MulPtBatch b, const u64 *__restrict__ pt_mont,
                                   const ModC *__restrict__ modc, int limbs, int n, int logn) {
@@ -97,7 +97,7 @@ __global__ void k_mul_pt_rot_last(u64 *__restrict__ out, MulPtBatch b, const u64
     const ModC m = modc[l];
     const unsigned g = b.g[z];
     const unsigned s = g ? perm_src(i, g, logn) : i;
-    out[((size_t)z * 2 + c) * n + i] = redc((u128)b.src[z][((size_t)c * limbs + l) * n + i] * pt_mont[(size_t)l * n + s], m.q, m.qinv);
+    out[((size_t)z * 2 + c) * n + i] = redc((u128)b.src[z][((size_t)c * limbs + l) * n + i] * pt_mont[((size_t)b.at[z] * limbs + l) * n + s], m.q, m.qinv);
 }
 void launch_mul_pt_rot_last(cm_ctx *ctx, u64 *out, const MulPtBatch &b, int cnt, const u64 *pt_mont, int limbs, hipStream_t st) {
     Prof prof_(ctx, CM_K_ELEMENTWISE, cnt * 2, st);
@@ -114,7 +114,7 @@ __global__ void k_mul_pt_rot_same(u64 *__restrict__ out, MulPtBatch b, int cnt, 
     for (int z = 0; z < cnt; z++) {
         const unsigned g = b.g[z];
         const unsigned s = g ? perm_src(i, g, logn) : i;
-        out[((size_t)z * 2 * limbs + r) * n + i] = redc((u128)v * pt_mont[(size_t)l * n + s], m.q, m.qinv);
+        out[((size_t)z * 2 * limbs + r) * n + i] = redc((u128)v * pt_mont[((size_t)b.at[z] * limbs + l) * n + s], m.q, m.qinv);
     }
 }
 void launch_mul_pt_rot_batch(cm_ctx *ctx, u64 *out, const MulPtBatch &b, int cnt, const u64 *pt_mont, int limbs, hipStream_t st) {

@@ -338,8 +338,9 @@ static cm_status kv_append(cm_ctx *ctx, const cm_evk *evk, cm_kv *kv, const cm_c
         for (int kb = 0; kb < kv->E; kb += B) {
             const int m = kv->E - kb < B ? kv->E - kb : B;
             MulPtBatch mb;
-            for (int r = 0; r < m; r++) mb.src[r] = src(kb + r), mb.g[r] = (unsigned)g(kb + r);
-            if (rescale_masked_into(ctx, mb, m, vmask, lv, dst + (size_t)kb * ctw, st, last, red, true)) continue;
+            u64 *outs[CM_MASK_BATCH];
+            for (int r = 0; r < m; r++) mb.src[r] = src(kb + r), mb.g[r] = (unsigned)g(kb + r), outs[r] = dst + (size_t)(kb + r) * ctw;
+            if (rescale_masked_into(ctx, mb, m, vmask, lv, outs, st, last, red, true)) continue;
             launch_mul_pt_rot_batch(ctx, prods, mb, m, vmask, lv + 1, st);
             CMCHK(rescale_into(ctx, prods, 2 * m, lv, dst + (size_t)kb * ctw, st, last, red, true));
         }

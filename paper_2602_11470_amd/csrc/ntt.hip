@@ -493,7 +493,7 @@ __device__ __forceinline__ void finish_tail(AT at, const A &ar, const u64 *lds, 
     if (fb.mul_pt) {
         // u = u[r] * (mul_pt through the Galois map mul_g[r]), formed here instead of being read
         const typename A::Tail tl(ar, t, l, pi, pis);
-        const u64 *mp = fb.mul_pt + (size_t)l * n;
+        const u64 *mp = fb.mul_pt + ((size_t)fb.mul_at[r] * fb.ext + l) * n;
         const unsigned mg = fb.mul_g[r];
 #pragma unroll
         for (int k = 0; k < NW; k++) uu[k] = up[LANES * k];
@@ -1138,7 +1138,7 @@ __global__ __launch_bounds__(SMALL_THREADS) void small_rows_inv_mul(u64 *__restr
     __shared__ u64 lds[SMALL_CHUNK + SMALL_CHUNK / 16];
     const int per = n / SMALL_CHUNK, limb = blockIdx.x / per, chunk = blockIdx.x % per, z = limb >> 1, c = limb & 1;
     u64 *p = data + (size_t)limb * n + (size_t)chunk * SMALL_CHUNK;
-    const u64 *src = b.src[z] + ((size_t)c * limbs + limbs - 1) * n, *m = pt + (size_t)(limbs - 1) * n;
+    const u64 *src = b.src[z] + ((size_t)c * limbs + limbs - 1) * n, *m = pt + ((size_t)b.at[z] * limbs + limbs - 1) * n;
     if (t.fpq[mi].q != 0.0) small_rows_inv_mul_body<FpArith>(lds, p, src, m, b.g[z], t, mi, n, chunk);
     else small_rows_inv_mul_body<IntArith>(lds, p, src, m, b.g[z], t, mi, n, chunk);
 }
@@ -1201,16 +1201,13 @@ __device__ __forceinline__ void full_fwd_body(u64 *lds, u64 *p, typename A::T (&
 #pragma unroll
     for (int k = 0; k < 8; k++) p[tid + 512 * k] = lds[pad8(tid + 512 * k)];
 }
-// up to the last factor: v[k] = word tid + 512 k, whose place in lds no other lane touches any more
-template <class A>
-__device__ __forceinline__ void full_inv_regs(u64 *lds, typename A::T (&v)[8], const A &ar, const u64 *ps, unsigned g, int n, int limb, const FoldIn &fi) {
+// up to the last factor: v[k] = word tid + 512 k, whose place in lds no other lane touches any more; load(w): the limb's words tid + 512 k
+template <class A, class LD>
+__device__ __forceinline__ void full_inv_words(u64 *lds, typename A::T (&v)[8], const A &ar, LD load) {
     const int tid = threadIdx.x, h2 = tid >> 6, l2 = tid & 63, h3 = tid >> 3, l3 = tid & 7;
     {
-        const int logn = 31 - __clz(n);
         u64 w[8];
-#pragma unroll
-        for (int k = 0; k < 8; k++) w[k] = ps[g ? perm_src((unsigned)(tid + 512 * k), g, logn) : tid + 512 * k];
-        fold_in(fi, limb, n, logn, w, [&](int k) { return (unsigned)(tid + 512 * k); });
+        load(w);
 #pragma unroll
         for (int k = 0; k < 8; k++) lds[pad8(tid + 512 * k)] = w[k];
         const Tw<A, 3> tw(ar, 512 + tid);
@@ -1246,6 +1243,15 @@ __device__ __forceinline__ void full_inv_regs(u64 *lds, typename A::T (&v)[8], c
         for (int k = 0; k < 8; k++) v[k] = ar.from_mid(lds[pad8(k * 512 + tid)]);
         radix_inv<3, 0>(v, ar, tw);
     }
+}
+template <class A>
+__device__ __forceinline__ void full_inv_regs(u64 *lds, typename A::T (&v)[8], const A &ar, const u64 *ps, unsigned g, int n, int limb, const FoldIn &fi) {
+    full_inv_words(lds, v, ar, [&](u64 (&w)[8]) {
+        const int tid = threadIdx.x, logn = 31 - __clz(n);
+#pragma unroll
+        for (int k = 0; k < 8; k++) w[k] = ps[g ? perm_src((unsigned)(tid + 512 * k), g, logn) : tid + 512 * k];
+        fold_in(fi, limb, n, logn, w, [&](int k) { return (unsigned)(tid + 512 * k); });
+    });
 }
 template <class A>
 __device__ __forceinline__ void full_inv_body(u64 *lds, u64 *p, const u64 *ps, unsigned g, const NttTables &t, int mi, int n, int limb,
@@ -1295,6 +1301,47 @@ __global__ __launch_bounds__(FULL_THREADS) void ntt_full_inv(u64 *data, const u6
         full_inv_body<FpArith>(lds, p, ps, g, t, mi, n, limb, fi);
     else
         full_inv_body<IntArith>(lds, p, ps, g, t, mi, n, limb, fi);
+}
+
+// A masked product rescaled in one launch (n = 4096): workgroup = one output limb l of component c of item r.  It forms the product's last
+// limb, takes it to coefficients (w mod q_level, canonical), which leaves every lane the words its forward transform begins with, transforms
+// them under q_l, and ends in the tail.  Every output limb repeats the inverse transform; see JOIN_TARGETS.
+template <class A>
+__device__ __forceinline__ void masked_full_last(u64 *lds, u64 (&w)[8], const NttTables &ti, const FinishBatch &fb, int r, int c, int n) {
+    const int lv = fb.level + 1, logn = 31 - __clz(n);
+    A ar;
+    ar.init(ti, lv, n);
+    const ModC m = ti.modc[lv];
+    const u64 *src = fb.u[r] + ((size_t)c * fb.ext + lv) * n, *mask = fb.mul_pt + ((size_t)fb.mul_at[r] * fb.ext + lv) * n;
+    const unsigned g = fb.mul_g[r];
+    typename A::T v[8];
+    full_inv_words(lds, v, ar, [&](u64 (&x)[8]) {
+        u64 y[8];
+#pragma unroll
+        for (int k = 0; k < 8; k++) x[k] = src[threadIdx.x + 512 * k], y[k] = mask[g ? perm_src(threadIdx.x + 512 * k, g, logn) : threadIdx.x + 512 * k];
+#pragma unroll
+        for (int k = 0; k < 8; k++) x[k] = redc((u128)x[k] * y[k], m.q, m.qinv);
+    });
+#pragma unroll
+    for (int k = 0; k < 8; k++) w[k] = ar.to_rest_inv(v[k]);
+}
+template <class A>
+__device__ __forceinline__ void masked_full_limb(u64 *lds, const u64 (&w)[8], const NttTables &t, const FinishBatch &fb, int l, int limb, int n) {
+    A ar;
+    ar.init(t, l, n);
+    typename A::T v[8];
+#pragma unroll
+    for (int k = 0; k < 8; k++) v[k] = ar.from_lazy(w[k]);
+    full_fwd_body<A, true>(lds, nullptr, v, ar, t, n, limb, fb);
+}
+__global__ __launch_bounds__(FULL_THREADS) void masked_full(FinishBatch fb, NttTables t, NttTables ti, int n) {
+    __shared__ u64 lds[FULL_LDS];
+    const int limb = blockIdx.x, limbs = fb.level + 1, r = limb / (2 * limbs), c = limb / limbs & 1, l = limb % limbs;
+    u64 w[8];
+    if (ti.fpq[limbs].q != 0.0) masked_full_last<FpArith>(lds, w, ti, fb, r, c, n);
+    else masked_full_last<IntArith>(lds, w, ti, fb, r, c, n);
+    if (t.fpq[l].q != 0.0) masked_full_limb<FpArith>(lds, w, t, fb, l, limb, n);
+    else masked_full_limb<IntArith>(lds, w, t, fb, l, limb, n);
 }
 
 // ---- fast base conversion, fused into the first pass of the forward transform of its results --------------------------
@@ -1890,6 +1937,19 @@ void launch_ntt_fwd_finish(cm_ctx *ctx, u64 *conv, const int *d_mods, const Fini
 // other.
 #define JOIN_TARGETS 512
 bool conv_joins_inv(const cm_ctx *ctx, bool near, int ns, int targets) { return ctx->n == 4096 && near && ns == 1 && targets <= JOIN_TARGETS; }
+void launch_masked_rescale(cm_ctx *ctx, const FinishBatch &fb, u64 *last, u64 *red, const int *d_last_mods, const int *d_red_mods, const int *d_red_src,
+                           hipStream_t st) {
+    const int n = ctx->n, level = fb.level + 1, comps = 2 * fb.items, limbs = comps * level;
+    if (n == 4096 && limbs <= JOIN_TARGETS) {
+        Prof prof_(ctx, CM_K_NTT_FWD, limbs, st);
+        hipLaunchKernelGGL(masked_full, dim3(limbs), dim3(FULL_THREADS), 0, st, fb, tables_of(ctx, false, limbs), tables_of(ctx, true, 0), n);
+        return;
+    }
+    MulPtBatch mb;
+    for (int r = 0; r < fb.items; r++) mb.src[r] = fb.u[r], mb.g[r] = fb.mul_g[r], mb.at[r] = fb.mul_at[r];
+    launch_mul_pt_rot_last_inv(ctx, last, mb, fb.items, fb.mul_pt, level + 1, d_last_mods, st);
+    launch_ntt_fwd_finish(ctx, red, d_red_mods, fb, st, last, d_red_src);
+}
 void launch_conv_ntt(cm_ctx *ctx, const ConvBatch &b, u64 *out, const u64 *in, hipStream_t st, const int *d_rows, const int *d_mods,
                      int limbs, const FinishBatch *fb) {
     const int n = ctx->n, ns = b.ns;              // rounded up to an instantiated bound below

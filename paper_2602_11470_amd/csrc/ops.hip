@@ -62,11 +62,11 @@ struct KsLevelFull : KsLevel {
     bool last_fits = false;     // the last modulus is below twice every other one (and below 2^52): its residues can enter
                                 // the other limbs' transforms as they are
     int *d_last_rows = nullptr; // rows c*(level+1)+level of stacked components
-    int *d_bsp_rows = nullptr, *d_bsp_mods = nullptr;   // special rows of CM_KS_BATCH stacked [2][ext] blocks
+    int *d_bsp_rows = nullptr, *d_bsp_mods = nullptr;   // special rows of CM_MASK_BATCH stacked [2][ext] blocks
     int *d_bsp1_rows = nullptr;                         // those of the second components only
     int *d_sp1_rows = nullptr;                          // special rows of the second component of one [2][ext] block
     ConvDev *d_moddown0 = nullptr;                      // the ModDown conversion reading its K input limbs from rows 0..K-1
-    int *d_bq_mods = nullptr;                           // 0..level repeated 2*CM_KS_BATCH times
+    int *d_bq_mods = nullptr;                           // 0..level repeated 2*CM_MASK_BATCH times
     std::vector<int> h_ntt_rows, h_ntt_mods;            // host copies of d_ntt_rows / d_ntt_mods
     // ks_drop with one and with two sets of special limbs: tables, rows (the last limb and the special ones of every component of
     // up to CM_KS_BATCH sums, of one with two sets) with their moduli, (P q_level)^-1 mod q_i with companions
@@ -278,7 +278,7 @@ static void build_ks(cm_ctx *ctx, int level, KsLevelFull &k) {
     k.d_red_src = up(red_src);
     {
         std::vector<int> br, bm, bq;
-        for (int r = 0; r < CM_KS_BATCH; r++)
+        for (int r = 0; r < CM_MASK_BATCH; r++)
             for (int c = 0; c < 2; c++) {
                 for (int sp = 0; sp < ctx->K; sp++) {
                     br.push_back((r * 2 + c) * k.ext + level + 1 + sp);
@@ -509,7 +509,13 @@ u64 *arena_digits(const cm_ctx *ctx) { return arena_of(ctx).digits; }
 size_t arena_digits_words(const cm_ctx *ctx) { return arena_of(ctx).misc - arena_of(ctx).digits; }
 u64 *arena_batch_sums(const cm_ctx *ctx) { return arena_of(ctx).bu; }
 
-// ModDown of m <= CM_KS_BATCH stacked sums bu[r][2][ext][n] in one batch of launches:
+// How many key switches one batch takes at a level: the arena holds the sums of two batches and the converted limbs of one, of CM_KS_BATCH
+// at the top level each, so the low levels, where a batch is short launches, have room for more.
+int ks_batch_max(const cm_ctx *ctx, int level) {
+    const int sums = 2 * CM_KS_BATCH * (ctx->L + 1 + ctx->K) / (level + 1 + ctx->K), conv = CM_KS_BATCH * (ctx->L + 1) / (level + 1);
+    return std::min(CM_MASK_BATCH, std::min(sums, conv));
+}
+// ModDown of m <= ks_batch_max stacked sums bu[r][2][ext][n] in one batch of launches:
 // outs[r] = ModDown(bu[r]) (+ perm_{gs[r]}(addends[r]) on the first addend_comps components) (+ accums[r])
 static void moddown_batch(cm_ctx *ctx, const KsLevelFull &k, u64 *bu, int m, const u64 *const *addends, int addend_comps,
                           const u64 *gs, const u64 *const *accums, u64 *const *outs, hipStream_t st, bool rows_done = false) {
@@ -532,8 +538,8 @@ static void moddown_batch(cm_ctx *ctx, const KsLevelFull &k, u64 *bu, int m, con
 }
 cm_status moddown_batch_into(cm_ctx *ctx, u64 *us, int level, int m, const u64 *const *addends, int addend_comps, u64 g,
                              const u64 *const *accums, u64 *const *outs, hipStream_t st, bool rows_done) {
-    if (m < 1 || m > CM_KS_BATCH) return CM_E_INVAL;
-    u64 gs[CM_KS_BATCH];
+    if (m < 1 || m > ks_batch_max(ctx, level)) return CM_E_INVAL;
+    u64 gs[CM_MASK_BATCH];
     for (int r = 0; r < m; r++) gs[r] = g;
     moddown_batch(ctx, ks_level_full(ctx, level), us, m, addends, addend_comps, gs, accums, outs, st, rows_done);
     return CM_OK;
@@ -1091,26 +1097,25 @@ int rescale_masked_batch(cm_ctx *ctx, int level, size_t words) {
     const size_t fit = words / (2 * (size_t)(level + 1) * ctx->n);
     return fit < CM_MASK_BATCH ? (int)fit : CM_MASK_BATCH;
 }
-// out[r] (+)= rescale(src_r * (pt through the Galois map g_r)) for r < cnt, src_r = mb.src[r] ([2][level+1][n]), out
-// stacked at stride 2*level*n: the products are never stored; only their last limbs are formed (for the inverse
+// outs[r] (+)= rescale(src_r * (plaintext at_r of pt through the Galois map g_r)) for r < cnt, src_r = mb.src[r] ([2][level+1][n]),
+// outs[r] [2][level][n]: the products are never stored; only their last limbs are formed (for the inverse
 // transform), the others inside the tail of the forward transform.  Only where rescale_into would take its fused path
 // and the last limb's residues fit (returns false otherwise: the caller multiplies and rescales in two steps).
-bool rescale_masked_into(cm_ctx *ctx, const MulPtBatch &mb, int cnt, const u64 *pt, int level, u64 *out, hipStream_t st,
+bool rescale_masked_into(cm_ctx *ctx, const MulPtBatch &mb, int cnt, const u64 *pt, int level, u64 *const *outs, hipStream_t st,
                          u64 *last, u64 *red, bool accumulate) {
     const KsLevelFull &k = ks_level_full(ctx, level);
     if (!k.last_fits || cnt < 1 || cnt > CM_MASK_BATCH || !last || !red) return false;
     if (ctx->two_step_masks) return false;                  // CM_OPT_TWO_STEP_MASKS: multiply, store, then rescale
-    launch_mul_pt_rot_last_inv(ctx, last, mb, cnt, pt, level + 1, k.d_last_mods, st);
     FinishBatch fb;
     fb.items = cnt, fb.level = level - 1, fb.ext = level + 1, fb.addend_comps = 0, fb.ncomp = 2, fb.comp0 = 0;
     for (int r = 0; r < CM_MASK_BATCH; r++) fb.addend[r] = nullptr, fb.accum[r] = nullptr, fb.u[r] = nullptr, fb.out[r] = nullptr, fb.g[r] = 0;
     for (int r = 0; r < cnt; r++) {
-        fb.u[r] = mb.src[r], fb.out[r] = out + (size_t)r * 2 * level * ctx->n, fb.mul_g[r] = mb.g[r];
+        fb.u[r] = mb.src[r], fb.out[r] = outs[r], fb.mul_g[r] = mb.g[r], fb.mul_at[r] = mb.at[r];
         fb.accum[r] = accumulate ? fb.out[r] : nullptr;
     }
     fb.mul_pt = pt;
     fb.pinv = get_qlinv(ctx, level);
-    launch_ntt_fwd_finish(ctx, red, k.d_red_mods, fb, st, last, k.d_red_src);
+    launch_masked_rescale(ctx, fb, last, red, k.d_last_mods, k.d_red_mods, k.d_red_src, st);
     return true;
 }
 extern "C" cm_status cm_rescale(cm_ctx *ctx, const cm_ct *a, cm_ct *out, void *stream) {

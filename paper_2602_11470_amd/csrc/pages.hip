@@ -19,40 +19,22 @@
 
 typedef u64 u64x2 __attribute__((ext_vector_type(2)));
 
+// One ciphertext of the result that is a masked product: where it comes from and goes to (array 0 K, 1 V, 2 X as stored), which mask, the
+// Galois element that the mask is read through, the rows it turns by (left).
+struct Move {
+    int array, from, to, mask, rows;
+    unsigned g;
+};
 struct cm_kv_sel {
     cm_ctx *ctx = nullptr;
     int H, E, t, r_i, level, ntok, shift, kept_end;     // level of the source; kept_end: one past the last kept token, after the move
     bool indexed = false, any = false;                  // any: a token is kept
-    std::vector<int> page;                              // per source page: -1 dropped, 0 kept whole, 1 + p kept through pattern p
+    std::vector<Move> moves;                            // ordered by rows
+    std::vector<int> rows;                              // the amounts other than 0, ascending
     u64 *d_masks = nullptr;                             // [1 + patterns][level+1][n], multiplier form
     int *d_from = nullptr;                              // [E] per page of the result: the page copied there, or -1
-    KsManyTables tabs;                                  // raises of CM_KS_BATCH moved ciphertexts, level - 1
-    bool turns = false;                                 // something is rotated
+    KsManyTables tabs;                                  // raises of ks_batch_max moved ciphertexts, level - 1
 };
-
-// one place of V (or X) of the result: the ciphertext that comes there, the rows its mask and the ciphertext itself turn by (left)
-struct Place {
-    int from, mask_rows, rows;
-};
-static Place v_place(const cm_kv_sel *s, int place) {
-    const int k = ((place - s->shift) % s->E + s->E) % s->E;
-    return {k, k % s->r_i, ((k / s->r_i - place / s->r_i) * s->r_i % s->E + s->E) % s->E};
-}
-static Place x_place_of(const cm_kv_sel *s, int place) {
-    const int r_o = s->E / s->r_i, kt = place % r_o * s->r_i + place / r_o, k = ((kt + s->shift) % s->E + s->E) % s->E;
-    return {k % s->r_i * r_o + k / s->r_i, s->E - k / s->r_i * s->r_i, ((kt % s->r_i - k % s->r_i) % s->E + s->E) % s->E};
-}
-static std::vector<int> sel_rows(const cm_kv_sel *s) {
-    std::vector<int> rows;
-    for (int p = 0; p < s->E; p++) {
-        rows.push_back(v_place(s, p).rows);
-        if (s->indexed) rows.push_back(x_place_of(s, p).rows);
-    }
-    std::sort(rows.begin(), rows.end());
-    rows.erase(std::unique(rows.begin(), rows.end()), rows.end());
-    if (!rows.empty() && rows[0] == 0) rows.erase(rows.begin());
-    return rows;
-}
 
 static bool same_shape(const cm_kv *a, const cm_kv *b) {
     return a->H == b->H && a->E == b->E && a->r_i == b->r_i && a->indexed == b->indexed;
@@ -141,6 +123,23 @@ extern "C" cm_status cm_kv_fork(cm_ctx *ctx, const cm_kv *src, cm_kv *const *dst
 }
 
 // ---- kept tokens ----------------------------------------------------------------------------------------------------------
+// V ciphertext k goes to place k + s, index ciphertext k to k - s (in the numbering of cm_kv_load)
+static void sel_moves(cm_kv_sel *s, const cm_kv *kv) {
+    const int E = s->E, r_i = s->r_i;
+    const long long B = (long long)s->H * s->t;
+    auto mod = [E](int a) { return (a % E + E) % E; };
+    for (int to = 0; to < E; to++) {
+        const int k = mod(to - s->shift);
+        s->moves.push_back({1, k, to, 0, mod((k / r_i - to / r_i) * r_i), (unsigned)rot_g(kv, k % r_i * B)});
+    }
+    for (int p = 0; p < E && s->indexed; p++) {                   // by places, so that neighbours share their source's neighbourhood
+        const int r_o = E / r_i, to = p % r_o * r_i + p / r_o, k = mod(to + s->shift);
+        s->moves.push_back({2, x_place(kv, k), p, 0, mod(to % r_i - k % r_i), (unsigned)rot_g(kv, -(k / r_i * r_i) * B)});
+    }
+    std::stable_sort(s->moves.begin(), s->moves.end(), [](const Move &a, const Move &b) { return a.rows < b.rows; });
+    for (const Move &m : s->moves)
+        if (m.rows && (s->rows.empty() || s->rows.back() != m.rows)) s->rows.push_back(m.rows);
+}
 extern "C" void cm_kv_sel_destroy(cm_kv_sel *s) {
     if (!s) return;
     hipFree(s->d_masks), hipFree(s->d_from);
@@ -162,7 +161,6 @@ extern "C" cm_status cm_kv_sel_create(cm_ctx *ctx, const cm_kv *like, const uint
         const int pages = (ntok + t - 1) / t;
         std::vector<std::vector<uint8_t>> patterns;
         std::vector<int> from(E, -1);
-        s->page.assign(pages, -1);
         for (int c = 0; c < pages && status == CM_OK; c++) {
             const int stored = std::min(t, ntok - c * t);
             std::vector<uint8_t> p(t, 0);
@@ -173,13 +171,14 @@ extern "C" cm_status cm_kv_sel_create(cm_ctx *ctx, const cm_kv *like, const uint
             if (c + shift < 0 || c + shift >= E) { status = CM_E_LAYOUT; break; }
             s->any = true;
             if (kept == stored) {
-                s->page[c] = 0, from[c + shift] = c;
+                from[c + shift] = c;
                 continue;
             }
             const size_t i = std::find(patterns.begin(), patterns.end(), p) - patterns.begin();
             if (i == patterns.size()) patterns.push_back(p);
-            s->page[c] = 1 + (int)i;
+            s->moves.push_back({0, c, c + shift, 1 + (int)i, 0, 1});
         }
+        if (s->any) sel_moves(s, like);
         if (status == CM_OK && s->any) {
             const int n = ctx->n, lv = s->level;
             const size_t words = (size_t)(lv + 1) * n;
@@ -198,8 +197,7 @@ extern "C" cm_status cm_kv_sel_create(cm_ctx *ctx, const cm_kv *like, const uint
                 }
                 status = coeffs ? cm_pt_from_coeffs(ctx, coeffs + i * n, lv, scale, &pt) : cm_encode(ctx, m.data(), nullptr, S, lv, scale, &pt);
             }
-            s->turns = !sel_rows(s).empty();
-            if (status == CM_OK && s->turns) status = ks_many_tables_create(ctx, lv - 1, CM_KS_BATCH, &s->tabs, 2, 1);
+            if (status == CM_OK && !s->rows.empty()) status = ks_many_tables_create(ctx, lv - 1, ks_batch_max(ctx, lv - 1), &s->tabs, 2, 1);
             if (status == CM_OK) ks_level(ctx, lv), get_qlinv(ctx, lv);      // the per-level tables that a take reads
         }
     } catch (...) {
@@ -213,14 +211,9 @@ extern "C" cm_status cm_kv_sel_create(cm_ctx *ctx, const cm_kv *like, const uint
     return CM_OK;
 }
 extern "C" int32_t cm_kv_sel_steps(const cm_kv_sel *s, int32_t *steps, int32_t cap) {
-    if (!s || !s->any) return 0;
-    try {
-        const auto rows = sel_rows(s);
-        for (int i = 0; i < (int)rows.size() && i < cap && steps; i++) steps[i] = rows[i] * s->H * s->t;
-        return (int32_t)rows.size();
-    } catch (...) {
-        return 0;
-    }
+    if (!s) return 0;
+    for (int i = 0; i < (int)s->rows.size() && i < cap && steps; i++) steps[i] = s->rows[i] * s->H * s->t;
+    return (int32_t)s->rows.size();
 }
 
 // page blockIdx.y of the result (+)= the page from[blockIdx.y] of the source; zero (nothing added) where there is none
@@ -247,16 +240,14 @@ __global__ __launch_bounds__(256) void k_pages(u64 *__restrict__ out, const u64 
 extern "C" cm_status cm_kv_take(cm_ctx *ctx, const cm_evk *evk, const cm_kv_sel *s, const cm_kv *src, cm_kv *dst, int32_t add, void *stream) {
     (void)hipGetLastError();
     if (!ctx || !s || s->ctx != ctx || !src || src->ctx != ctx || !dst || dst->ctx != ctx || src == dst) return CM_E_INVAL;
-    if (s->turns && s->any && (!evk || !evk_fits(ctx, evk))) return CM_E_INVAL;
-    if (!same_shape(src, dst) || s->H != src->H || s->E != src->E || s->r_i != src->r_i || (src->indexed && !s->indexed)) return CM_E_LAYOUT;
+    if (!s->rows.empty() && (!evk || !evk_fits(ctx, evk))) return CM_E_INVAL;
+    if (!same_shape(src, dst) || s->H != src->H || s->E != src->E || s->r_i != src->r_i || s->indexed != src->indexed) return CM_E_LAYOUT;
     if (src->level != s->level || dst->level != s->level - 1) return CM_E_LEVEL;
     if (src->ntok != s->ntok || s->kept_end > dst->max_tokens) return CM_E_LAYOUT;
     if (add && src->scale_set && dst->scale_set && fabs(src->scale / dst->scale - 1) > 1e-9) return CM_E_SCALE;
     CM_TRY
-    const long long B = (long long)s->H * s->t;
-    if (s->any)
-        for (int rows : sel_rows(s))
-            if (!find_key(evk, rot_g(src, rows * B))) return CM_E_NOKEY;
+    for (int rows : s->rows)
+        if (!find_key(evk, rot_g(src, (long long)rows * s->H * s->t))) return CM_E_NOKEY;
     hipStream_t st = (hipStream_t)stream;
     const int lv = s->level, lo = lv - 1, n = ctx->n;
     const size_t ctw_in = kv_ctw(src), ctw = kv_ctw(dst);
@@ -273,60 +264,57 @@ extern "C" cm_status cm_kv_take(cm_ctx *ctx, const cm_evk *evk, const cm_kv_sel 
             if (dst->indexed) launch_zero(dst->d_x, s->E * ctw, st);
         }
     } else {
+        // K pages kept in part, V and X: masked products, rescaled, as many a batch as the work area has room for; those that turn
+        // next to one another and then rotated, CM_KS_BATCH at a time with the key read once
         const KsLevel &kl = ks_level(ctx, lo);
-        const size_t ln = (size_t)(lo + 1) * n, dblk = (size_t)kl.beta * kl.ext * n, ublk = 2 * (size_t)kl.ext * n, mw = (size_t)(lv + 1) * n;
-        // out[0 .. m) (+)= rescale(mask through g * source): products formed inside the rescale, or in two steps
-        auto masked = [&](const MulPtBatch &mb, int m, const u64 *mask, u64 *outp, u64 *work, bool acc) -> cm_status {
-            u64 *last = work, *red = last + (size_t)m * 2 * n, *prods = red + (size_t)m * 2 * lv * n;
-            if (rescale_masked_into(ctx, mb, m, mask, lv, outp, st, last, red, acc)) return CM_OK;
-            launch_mul_pt_rot_batch(ctx, prods, mb, m, mask, lv + 1, st);
-            return rescale_into(ctx, prods, 2 * m, lv, outp, st, last, red, acc);
-        };
-        const int fused = rescale_masked_batch(ctx, lv, dst->work_words), most = fused ? fused : CM_KS_BATCH;
-        for (size_t c = 0; c < s->page.size();) {                 // a run of neighbours with one pattern
-            const int p = s->page[c];
+        const size_t ln = (size_t)lv * n, dblk = (size_t)kl.beta * kl.ext * n, ublk = 2 * (size_t)kl.ext * n;
+        const u64 *in[3] = {src->d_k, src->d_v, src->d_x};
+        u64 *out[3] = {dst->d_k, dst->d_v, dst->d_x};
+        const int fused = rescale_masked_batch(ctx, lv, dst->work_words);
+        // those that turn: stacked in front of the masked product's last limbs and residues, and of what a batch of key switches takes;
+        // the work area has room for CM_KS_BATCH of them (fused or in two steps)
+        const int batch = ks_batch_max(ctx, lo);
+        int turning = CM_KS_BATCH;
+        while (fused && turning < CM_MASK_BATCH &&
+               (turning + 1) * ctw + std::max(std::min(turning + 1, batch) * (ln + dblk), (turning + 1) * ctw_in) <= dst->work_words)
+            turning++;
+        for (size_t i = 0; i < s->moves.size();) {
+            const int rows = s->moves[i].rows, cap = rows ? turning : fused ? fused : CM_KS_BATCH;
             int m = 0;
             MulPtBatch mb;
-            while (p > 0 && m < most && c + m < s->page.size() && s->page[c + m] == p) mb.src[m] = src->d_k + (c + m) * ctw_in, mb.g[m] = 1, m++;
-            if (m) CMCHK(masked(mb, m, s->d_masks + p * mw, dst->d_k + (c + s->shift) * ctw, dst->d_work, add != 0));
-            c += m ? m : 1;
-        }
-        auto move = [&](u64 *out, const u64 *in, auto place_of) -> cm_status {
-            for (int p0 = 0; p0 < s->E;) {
-                const int rows = place_of(s, p0).rows, cap = rows ? std::min(most, CM_KS_BATCH) : most;
-                int m = 0;
-                MulPtBatch mb;
-                for (; m < cap && p0 + m < s->E && place_of(s, p0 + m).rows == rows; m++) {
-                    const Place pl = place_of(s, p0 + m);
-                    mb.src[m] = in + pl.from * ctw_in, mb.g[m] = (unsigned)rot_g(src, pl.mask_rows * B);
-                }
-                if (!rows) {
-                    CMCHK(masked(mb, m, s->d_masks, out + p0 * ctw, dst->d_work, add != 0));
-                } else {
-                    // masked and rescaled next to one another, then turned: one raise, one inner-product launch with the key read once,
-                    // one ModDown
-                    const u64 g = rot_g(src, rows * B), *key = find_key(evk, g);
-                    u64 *tmp = dst->d_work, *ksin = tmp + CM_KS_BATCH * ctw, *digits = ksin + CM_KS_BATCH * ln, *work = digits + CM_KS_BATCH * dblk;
-                    CMCHK(masked(mb, m, s->d_masks, tmp, work, false));
-                    CMCHK(ks_raise_many(ctx, s->tabs, tmp, ksin, digits, st, m, g));
-                    u64 *bu = arena_batch_sums(ctx);
-                    IpBatch ip;
-                    ip.nz = m, ip.nsum = 1;
-                    const u64 *adds[CM_KS_BATCH], *accs[CM_KS_BATCH];
-                    u64 *outs[CM_KS_BATCH];
-                    for (int r = 0; r < m; r++) {
-                        ip.it[r].dig = digits + r * dblk, ip.it[r].key = key, ip.out[r] = bu + r * ublk;
-                        adds[r] = tmp + r * ctw, outs[r] = out + (p0 + r) * ctw, accs[r] = add ? outs[r] : nullptr;
-                    }
-                    launch_inner_product_shared_key(ctx, ip, kl.beta, lo, st);
-                    CMCHK(moddown_batch_into(ctx, bu, lo, m, adds, 1, g, accs, outs, st));
-                }
-                p0 += m;
+            u64 *outs[CM_MASK_BATCH], *to[CM_MASK_BATCH];
+            for (; m < cap && i + m < s->moves.size() && s->moves[i + m].rows == rows; m++) {
+                const Move &v = s->moves[i + m];
+                mb.src[m] = in[v.array] + v.from * ctw_in, mb.g[m] = v.g, mb.at[m] = v.mask;
+                to[m] = out[v.array] + v.to * ctw, outs[m] = rows ? dst->d_work + m * ctw : to[m];
             }
-            return CM_OK;
-        };
-        CMCHK(move(dst->d_v, src->d_v, v_place));
-        if (src->indexed) CMCHK(move(dst->d_x, src->d_x, x_place_of));
+            u64 *work = dst->d_work + (rows ? m * ctw : 0), *last = work, *red = last + (size_t)m * 2 * n, *prods = red + (size_t)m * 2 * lv * n;
+            const bool acc = add && !rows;
+            if (!rescale_masked_into(ctx, mb, m, s->d_masks, lv, outs, st, last, red, acc)) {
+                launch_mul_pt_rot_batch(ctx, prods, mb, m, s->d_masks, lv + 1, st);
+                for (int r = 0; r < m; r++) CMCHK(rescale_into(ctx, prods + r * ctw_in, 2, lv, outs[r], st, last, red, acc));
+            }
+            for (int r0 = 0; r0 < m && rows; r0 += batch) {
+                const u64 g = rot_g(src, (long long)rows * s->H * s->t), *key = find_key(evk, g);
+                const int b = std::min(m - r0, batch);
+                const bool half = rows_ip_fits(ctx, kl.beta, lo, b, 1);
+                u64 *ksin = work, *digits = ksin + b * ln, *bu = arena_batch_sums(ctx);
+                CMCHK(ks_raise_many(ctx, s->tabs, outs[r0], ksin, digits, st, b, g, half));
+                IpBatch ip;
+                ip.nz = b, ip.nsum = 1;
+                const u64 *adds[CM_MASK_BATCH], *accs[CM_MASK_BATCH];
+                for (int r = 0; r < b; r++) {
+                    ip.it[r].dig = digits + r * dblk, ip.it[r].key = key, ip.out[r] = bu + r * ublk;
+                    ip.it[r].own = outs[r0 + r] + ln, ip.it[r].own_g = (unsigned)g;
+                    adds[r] = outs[r0 + r], accs[r] = add ? to[r0 + r] : nullptr;
+                }
+                if (half) launch_rows_ip(ctx, ip, kl.beta, lo, st, lo + 1);
+                else if (n == 4096) launch_inner_product_batch(ctx, ip, kl.beta, lo, st);
+                else launch_inner_product_shared_key(ctx, ip, kl.beta, lo, st);
+                CMCHK(moddown_batch_into(ctx, bu, lo, b, adds, 1, g, accs, to + r0, st, half));
+            }
+            i += m;
+        }
     }
     dst->ntok = add ? std::max(dst->ntok, s->kept_end) : s->kept_end;
     dst->pos = dst->ntok;
