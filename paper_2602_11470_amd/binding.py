@@ -397,7 +397,7 @@ class Context:
         a, b = ((cm_ct * len(scores))(*[c.d for c in cts]) for cts in (scores, outs))
         _chk(lib.cm_relbias_apply(self.h, bias.h, token, first, pass0, len(scores), a, b, _stream()))
         for o, d in zip(outs, b):
-            o.d = cm_ct(d.dev, d.level, d.ncomp, d.scale)
+            o.d = d
         return outs
 
     def vmm_kv(self, evk, kv, which, x):
@@ -561,11 +561,22 @@ class RelBias:
             self.h = None
 
 
-class _Words:
-    """Device memory of a cache as torch reads it; keeps the cache alive."""
+class _KvHandle:
+    """Owns a cache of the library: the last of its KvCache and the tensors over its memory destroys it."""
 
-    def __init__(self, kv, ptr, words):
-        self.kv = kv
+    def __init__(self, h):
+        self.h = h
+
+    def __del__(self):
+        if lib is not None:
+            lib.cm_kv_destroy(self.h)
+
+
+class _Words:
+    """Device memory of a cache as torch reads it."""
+
+    def __init__(self, owner, ptr, words):
+        self.owner = owner
         self.__cuda_array_interface__ = dict(shape=(words,), typestr="<i8", data=(ptr, False), strides=None, version=3)
 
 
@@ -574,10 +585,12 @@ class KvCache:
         self.ctx, self.h, self.level, self.key_index = ctx, _vp(), level, key_index
         t = ctx.S // ((1 << (heads - 1).bit_length()) * dim)
         max_tokens = dim * t if max_tokens is None else max_tokens
+        self._words = {}
         self.dim, self.r_i, self.pages = dim, r_i or dim, -(-max_tokens // t)
         _chk(lib.cm_kv_create_ex(ctx.h, heads, dim, r_i, level, scale, max_tokens,
                                  (CM_KV_UNROLLED_LADDERS if unrolled_ladders else 0) | (CM_KV_KEY_INDEX if key_index else 0),
                                  C.byref(self.h)))
+        self._owner = _KvHandle(self.h)
         if shared_dims != 1:
             self.set_shared_dims(shared_dims)
 
@@ -604,12 +617,15 @@ class KvCache:
 
     def words(self, which):
         """The ciphertexts where they lie, as a tensor: [index][2][level+1][n], the key index [r_o][r_i][2][level+1][n]."""
+        if which in self._words:
+            return self._words[which]
         d = cm_ct()
         _chk(lib.cm_kv_view(self.h, which, 0, C.byref(d)))
         limbs, ct = self.level + 1, 2 * (self.level + 1) * self.ctx.n
         count = self.pages if which == CM_QK else self.dim
-        w = torch.as_tensor(_Words(self, d.dev, count * ct), device="cuda").view(count, 2, limbs, self.ctx.n)
-        return w.unflatten(0, (self.r_i, self.dim // self.r_i)).transpose(0, 1) if which == CM_KV_INDEX else w
+        w = torch.as_tensor(_Words(self._owner, d.dev, count * ct), device="cuda").view(count, 2, limbs, self.ctx.n)
+        self._words[which] = w.unflatten(0, (self.r_i, self.dim // self.r_i)).transpose(0, 1) if which == CM_KV_INDEX else w
+        return self._words[which]
 
     def export(self, which, idx):
         out = np.empty((2, self.level + 1, self.ctx.n), dtype=np.uint64)
@@ -625,11 +641,6 @@ class KvCache:
 
     def append_group(self, evk, k_grp, v_grp):
         _chk(lib.cm_kv_append_group(self.ctx.h, evk.h, self.h, C.byref(k_grp.d), C.byref(v_grp.d), _stream()))
-
-    def __del__(self):
-        if getattr(self, "h", None) and lib is not None:
-            lib.cm_kv_destroy(self.h)
-            self.h = None
 
 
 def config1():

@@ -41,8 +41,12 @@ static bool same_shape(const cm_kv *a, const cm_kv *b) {
 }
 
 // ---- copies -----------------------------------------------------------------------------------------------------------
-// A workgroup moves one piece of PIECE words of a limb to every destination that has the limb, reading it once.
-#define PIECE 4096
+// A lane moves 16 bytes of a limb: to every destination that has the limb, reading them once.  Bound by memory: 2.6 GB read and written
+// once 430 us (6.2 TB/s, the card's own copy 5.85), read once and written four times 13.5 GB 2.3 to 2.4 ms.  More words a lane: 2, 4 and 8 pairs
+// 435, 444 and 485 us; plain instead of non-temporal loads and stores of 8 pairs 505.
+#define LANES 256
+#define LANE_WORDS (2 * LANES)                   // words a workgroup moves
+#define MAX_Y 65534                              // workgroups along y, even: two components a ciphertext
 #define FORK_MAX 8
 struct ForkDst {
     u64 *k, *v, *x;
@@ -50,34 +54,31 @@ struct ForkDst {
 };
 struct ForkArgs {
     const u64 *k, *v, *x;
-    int level, top, pages, E, n, ndst;       // level of the source, highest level of a destination, pages in use
+    int level, top, used, cts, E, n, ndst;       // level of the source, highest level of a destination, pages in use, ciphertexts to copy
     ForkDst d[FORK_MAX];
 };
-__global__ __launch_bounds__(256) void k_fork(ForkArgs a) {
-    const int per = a.n / PIECE, l = blockIdx.x / per, part = blockIdx.x % per;
-    const int c = blockIdx.y & 1, z = blockIdx.y >> 1;              // component, ciphertext: K pages, then V, then X
-    const size_t in = ((size_t)c * (a.level + 1) + l) * a.n + (size_t)part * PIECE, ct = 2 * (size_t)(a.level + 1) * a.n;
-    const int i = z < a.pages ? z : z < a.pages + a.E ? z - a.pages : z - a.pages - a.E;
-    const u64 *src = (z < a.pages ? a.k : z < a.pages + a.E ? a.v : a.x) + i * ct + in;
-    u64x2 w[8];
-#pragma unroll
-    for (int u = 0; u < 8; u++) w[u] = *((const u64x2 *)src + threadIdx.x + 256 * u);
+// grid: x = piece of a limb, y = ciphertext and component from y0 on: pages in use, V, X, then the pages behind the last one, which are cleared
+__global__ __launch_bounds__(LANES) void k_fork(ForkArgs a, int y0) {
+    const int per = a.n / LANE_WORDS, l = blockIdx.x / per, y = blockIdx.y + y0, c = y & 1, z = y >> 1;
+    const size_t at = (size_t)(blockIdx.x % per) * LANE_WORDS + 2 * threadIdx.x, limb = (size_t)c * (a.level + 1) + l;
+    if (z >= a.cts) {
+        const int page = a.used + z - a.cts;
+        for (int d = 0; d < a.ndst; d++) {
+            const ForkDst &t = a.d[d];
+            if (l > t.level || page >= t.pages) continue;
+            __builtin_nontemporal_store(u64x2{0, 0}, (u64x2 *)(t.k + (((size_t)page * 2 + c) * (t.level + 1) + l) * a.n + at));
+        }
+        return;
+    }
+    const int array = z < a.used ? 0 : z < a.used + a.E ? 1 : 2, i = z - (array ? a.used : 0) - (array == 2 ? a.E : 0);
+    const u64 *src = (array == 0 ? a.k : array == 1 ? a.v : a.x) + (2 * (size_t)(a.level + 1) * i + limb) * a.n + at;
+    const u64x2 w = __builtin_nontemporal_load((const u64x2 *)src);
     for (int d = 0; d < a.ndst; d++) {
         const ForkDst &t = a.d[d];
         if (l > t.level) continue;
-        u64 *dst = (z < a.pages ? t.k : z < a.pages + a.E ? t.v : t.x) + i * 2 * (size_t)(t.level + 1) * a.n +
-                   ((size_t)c * (t.level + 1) + l) * a.n + (size_t)part * PIECE;
-#pragma unroll
-        for (int u = 0; u < 8; u++) *((u64x2 *)dst + threadIdx.x + 256 * u) = w[u];
+        u64 *dst = (array == 0 ? t.k : array == 1 ? t.v : t.x) + (((size_t)i * 2 + c) * (t.level + 1) + l) * a.n + at;
+        __builtin_nontemporal_store(w, (u64x2 *)dst);
     }
-}
-__global__ __launch_bounds__(256) void k_zero(u64 *p) {
-    u64x2 *q = (u64x2 *)(p + (size_t)blockIdx.x * PIECE);
-#pragma unroll
-    for (int u = 0; u < 8; u++) q[threadIdx.x + 256 * u] = u64x2{0, 0};
-}
-static void launch_zero(u64 *p, size_t words, hipStream_t st) {
-    if (words) hipLaunchKernelGGL(k_zero, dim3((unsigned)(words / PIECE)), dim3(256), 0, st, p);
 }
 
 extern "C" cm_status cm_kv_view(const cm_kv *kv, int32_t which, int32_t idx, cm_ct *out) {
@@ -103,19 +104,19 @@ extern "C" cm_status cm_kv_fork(cm_ctx *ctx, const cm_kv *src, cm_kv *const *dst
         if (dsts[d]->level > src->level) return CM_E_LEVEL;
     }
     hipStream_t st = (hipStream_t)stream;
-    const int pages = (src->ntok + src->t - 1) / src->t, n = ctx->n;
+    const int used = (src->ntok + src->t - 1) / src->t, n = ctx->n;
     for (int d0 = 0; d0 < ndst; d0 += FORK_MAX) {
-        ForkArgs a{src->d_k, src->d_v, src->d_x, src->level, 0, pages, src->E, n, std::min(ndst - d0, FORK_MAX), {}};
+        ForkArgs a{src->d_k, src->d_v, src->d_x, src->level, 0, used, used + (src->indexed ? 2 : 1) * src->E, src->E, n, std::min(ndst - d0, FORK_MAX), {}};
+        int clear = 0;
         for (int d = 0; d < a.ndst; d++) {
             const cm_kv *t = dsts[d0 + d];
             a.d[d] = {t->d_k, t->d_v, t->d_x, t->level, t->nk_max};
-            a.top = std::max(a.top, t->level);
+            a.top = std::max(a.top, t->level), clear = std::max(clear, t->nk_max - used);
         }
-        const int cts = pages + (src->indexed ? 2 : 1) * src->E;
-        Prof prof_(ctx, CM_K_ELEMENTWISE, (double)cts * 2 * (a.top + 1), st);
-        hipLaunchKernelGGL(k_fork, dim3((a.top + 1) * (n / PIECE), 2 * cts), dim3(256), 0, st, a);
-        for (int d = 0; d < a.ndst; d++)
-            launch_zero(dsts[d0 + d]->d_k + pages * kv_ctw(dsts[d0 + d]), (dsts[d0 + d]->nk_max - pages) * kv_ctw(dsts[d0 + d]), st);
+        const int rows = 2 * (a.cts + clear);
+        Prof prof_(ctx, CM_K_ELEMENTWISE, (double)rows * (a.top + 1), st);
+        for (int y = 0; y < rows; y += MAX_Y)
+            hipLaunchKernelGGL(k_fork, dim3((a.top + 1) * (n / LANE_WORDS), std::min(rows - y, MAX_Y)), dim3(LANES), 0, st, a, y);
     }
     for (int d = 0; d < ndst; d++)
         dsts[d]->ntok = src->ntok, dsts[d]->pos = src->pos, dsts[d]->scale = src->scale, dsts[d]->scale_set = src->scale_set;
@@ -216,26 +217,23 @@ extern "C" int32_t cm_kv_sel_steps(const cm_kv_sel *s, int32_t *steps, int32_t c
     return (int32_t)s->rows.size();
 }
 
-// page blockIdx.y of the result (+)= the page from[blockIdx.y] of the source; zero (nothing added) where there is none
+// K pages of the result, grid as in k_fork: page (+)= the page from[page] of the source, a level above; zero, or nothing added, where there is none
 template <bool ADD>
-__global__ __launch_bounds__(256) void k_pages(u64 *__restrict__ out, const u64 *__restrict__ in, const int *__restrict__ from, const ModC *__restrict__ modc, int E,
-                                               int level, int n) {
-    const int per = n / PIECE, l = blockIdx.x / per, part = blockIdx.x % per, c = blockIdx.y & 1, page = blockIdx.y >> 1;
-    const int src = from && page < E ? from[page] : -1;
-    if (ADD && src < 0) return;
-    const u64 q = modc[l].q;
-    u64x2 *dst = (u64x2 *)(out + (((size_t)page * 2 + c) * (level + 1) + l) * n + (size_t)part * PIECE);
-    const u64x2 *p = (const u64x2 *)(in + (((size_t)std::max(src, 0) * 2 + c) * (level + 2) + l) * n + (size_t)part * PIECE);
-#pragma unroll
-    for (int u = 0; u < 8; u++) {
-        u64x2 w = src < 0 ? u64x2{0, 0} : p[threadIdx.x + 256 * u];
-        if (ADD) {
-            const u64x2 o = dst[threadIdx.x + 256 * u];
-            w = u64x2{addmod(w.x, o.x, q), addmod(w.y, o.y, q)};
-        }
-        dst[threadIdx.x + 256 * u] = w;
+__global__ __launch_bounds__(LANES) void k_pages(u64 *out, const u64 *in, const int *from, const ModC *__restrict__ modc, int level, int n, int y0) {
+    const int per = n / LANE_WORDS, l = blockIdx.x / per, y = blockIdx.y + y0, c = y & 1, page = y >> 1, src = from ? from[page] : -1;
+    const size_t at = (size_t)(blockIdx.x % per) * LANE_WORDS + 2 * threadIdx.x;
+    u64x2 *dst = (u64x2 *)(out + (((size_t)page * 2 + c) * (level + 1) + l) * n + at);
+    u64x2 w = {0, 0};
+    if (src >= 0) w = __builtin_nontemporal_load((const u64x2 *)(in + (((size_t)src * 2 + c) * (level + 2) + l) * n + at));
+    if (ADD) {
+        if (src < 0) return;
+        const u64 q = modc[l].q;
+        const u64x2 o = __builtin_nontemporal_load(dst);
+        w = u64x2{addmod(w.x, o.x, q), addmod(w.y, o.y, q)};
     }
+    __builtin_nontemporal_store(w, dst);
 }
+__global__ __launch_bounds__(LANES) void k_clear(u64 *p) { ((u64x2 *)p)[(size_t)blockIdx.x * LANES + threadIdx.x] = u64x2{0, 0}; }
 
 extern "C" cm_status cm_kv_take(cm_ctx *ctx, const cm_evk *evk, const cm_kv_sel *s, const cm_kv *src, cm_kv *dst, int32_t add, void *stream) {
     (void)hipGetLastError();
@@ -252,16 +250,17 @@ extern "C" cm_status cm_kv_take(cm_ctx *ctx, const cm_evk *evk, const cm_kv_sel 
     const int lv = s->level, lo = lv - 1, n = ctx->n;
     const size_t ctw_in = kv_ctw(src), ctw = kv_ctw(dst);
     // K: pages kept whole are copied, the places without one cleared; then the pages that keep some of their tokens
-    {
-        Prof prof_(ctx, CM_K_ELEMENTWISE, (double)dst->nk_max * 2 * lv, st);
-        const dim3 grid(lv * (n / PIECE), 2 * dst->nk_max);
-        if (add && s->any) hipLaunchKernelGGL(k_pages<true>, grid, dim3(256), 0, st, dst->d_k, src->d_k, s->d_from, ctx->d_modc, s->E, lo, n);
-        else if (!add) hipLaunchKernelGGL(k_pages<false>, grid, dim3(256), 0, st, dst->d_k, src->d_k, s->d_from, ctx->d_modc, s->E, lo, n);
+    if (!add || s->any) {
+        const int rows = 2 * dst->nk_max;
+        Prof prof_(ctx, CM_K_ELEMENTWISE, (double)rows * lv, st);
+        for (int y = 0; y < rows; y += MAX_Y)
+            hipLaunchKernelGGL((add ? k_pages<true> : k_pages<false>), dim3(lv * (n / LANE_WORDS), std::min(rows - y, MAX_Y)), dim3(LANES), 0, st, dst->d_k,
+                               src->d_k, s->d_from, ctx->d_modc, lo, n, y);
     }
     if (!s->any) {
-        if (!add) {
-            launch_zero(dst->d_v, s->E * ctw, st);
-            if (dst->indexed) launch_zero(dst->d_x, s->E * ctw, st);
+        for (int i = 0; i < dst->E && !add; i++) {               // an empty cache
+            hipLaunchKernelGGL(k_clear, dim3((unsigned)(ctw / LANE_WORDS)), dim3(LANES), 0, st, dst->d_v + i * ctw);
+            if (dst->indexed) hipLaunchKernelGGL(k_clear, dim3((unsigned)(ctw / LANE_WORDS)), dim3(LANES), 0, st, dst->d_x + i * ctw);
         }
     } else {
         // K pages kept in part, V and X: masked products, rescaled, as many a batch as the work area has room for; those that turn
