@@ -136,8 +136,10 @@ static u64 brev(u64 x, int bits) {
 
 u64 galois_of_step(const cm_ctx *ctx, int step) {
     int S = ctx->n / 2;
-    int r = ((step % S) + S) % S;
-    return h_powmod(5, (u64)r, 2 * (u64)ctx->n);
+    u64 g = 1, b = 5;                                  // modulo 2n, a power of two: words that wrap
+    for (unsigned r = ((step % S) + S) % S; r; r >>= 1, b *= b)
+        if (r & 1) g *= b;
+    return g & (2 * (u64)ctx->n - 1);
 }
 
 std::vector<std::vector<int>> digits_at(const cm_ctx *ctx, int level) {
