@@ -1143,6 +1143,70 @@ __global__ __launch_bounds__(SMALL_THREADS) void small_rows_inv_mul(u64 *__restr
     else small_rows_inv_mul_body<IntArith>(lds, p, src, m, b.g[z], t, mi, n, chunk);
 }
 
+// The row pass that ends masked rescales of more than SMALL_ROWS limbs: rows256_fwd_body with a tail of its own, which knows no other addends and
+// works on eight words at a time, so that four waves fit a SIMD (124 registers; the general tail's 144 let three in).  The plaintext's words
+// for positions 256 apart: only bits 8 to 11 of the position differ, so their exponents differ by multiples of g that the lanes share.
+// Moves 400 MB of a batch of 32 ciphertexts at level 4 (vector ALU half busy): 7 of 1000 tokens taken back there 1454 -> 1400 us, pages freed at
+// level 10 880 -> 845, decode-step attention at level 3 3160 -> 3095.  Sixteen words at a time 1435, eight with the products' words
+// requested in front of the last exchange 1429.  A wave a row with four words a lane, the tail on them as they are in two 16-byte accesses: 1555
+// (of 1497 with the general tail); the column passes in front in one kernel, so that the last limb's coefficients stay in registers: equal
+// there, +6 to 10 % at level 10 (173 registers); batches of 24, 16 and 8 equal, +5 % and +20 %.
+template <class A>
+__device__ __forceinline__ void masked_rows_body(u64 *lds, const u64 *p, const NttTables &t, int l, int n, unsigned chunk, const FinishBatch &fb, int r, int c) {
+    A ar;
+    ar.init(t, l, n);
+    const int sub = threadIdx.x & 15, blk = threadIdx.x >> 4, logn = 31 - __clz(n);
+    const u64 B = (u64)chunk * 16 + blk;
+    const unsigned pos0 = chunk * 4096 + threadIdx.x;
+    const u64 *up = fb.u[r] + ((size_t)c * fb.ext + l) * n + pos0, *mp = fb.mul_pt + ((size_t)fb.mul_at[r] * fb.ext + l) * n;
+    const size_t at = ((size_t)c * (fb.level + 1) + l) * n + pos0;
+    u64 *op = fb.out[r] + at;
+    const u64 *ac = fb.accum[r] ? fb.accum[r] + at : nullptr;
+    const unsigned g = fb.mul_g[r], eg = ((__brev(pos0) >> (31 - logn)) | 1u) * g;       // perm_src's e g
+    typename A::T v[16];
+    u64 raw[16];
+#pragma unroll
+    for (int k = 0; k < 16; k++) raw[k] = __builtin_nontemporal_load(p + blk * 256 + sub + 16 * k);
+    {
+        const TableTw<A> tw(ar, 256 + B);
+#pragma unroll
+        for (int k = 0; k < 16; k++) v[k] = ar.from_mid(raw[k]);
+        radix16_fwd_tw(v, ar, tw);
+    }
+#pragma unroll
+    for (int k = 0; k < 16; k++) lds[pad(blk * 256 + sub + 16 * k)] = ar.to_mid(v[k]);
+    wave_sync();
+#pragma unroll
+    for (int k = 0; k < 16; k++) v[k] = ar.from_mid(lds[pad(blk * 256 + 16 * sub + k)]);
+    radix16_fwd_last(v, ar, 4096 + B * 16 + sub);
+#pragma unroll
+    for (int k = 0; k < 16; k++) lds[pad(blk * 256 + 16 * sub + k)] = ar.to_tail(v[k]);
+    __syncthreads();
+    const typename A::Tail tl(ar, t, l, fb.pinv[2 * l], fb.pinv[2 * l + 1]);
+#pragma unroll
+    for (int h = 0; h < 16; h += 8) {
+        u64 uu[8], m[8], cc[8];
+#pragma unroll
+        for (int k = 0; k < 8; k++) uu[k] = up[256 * (h + k)];
+#pragma unroll
+        for (int k = 0; k < 8; k++) m[k] = mp[(__brev(eg + g * (__brev(256u * (h + k)) >> (31 - logn))) >> (31 - logn)) & (n - 1u)];
+        if (ac) {
+#pragma unroll
+            for (int k = 0; k < 8; k++) cc[k] = TAIL_LD(ac + 256 * (h + k));
+        }
+#pragma unroll
+        for (int k = 0; k < 8; k++) TAIL_ST(op + 256 * (h + k), tl.masked(ar, uu[k], m[k], lds[pad(threadIdx.x + 256 * (h + k))], ac != nullptr, cc[k]));
+    }
+}
+__global__ __launch_bounds__(NTT_THREADS, 4) void masked_rows(const u64 *__restrict__ red, NttTables t, int n, FinishBatch fb) {
+    __shared__ u64 lds[LDS_WORDS];
+    const int per = n >> 12, limb = blockIdx.x / per, limbs = fb.level + 1, l = limb % limbs, c = limb / limbs & 1, r = limb / (2 * limbs);
+    const unsigned chunk = blockIdx.x % per;
+    const u64 *p = red + (size_t)limb * n + (size_t)chunk * 4096;
+    if (t.fpq[l].q != 0.0) masked_rows_body<FpArith>(lds, p, t, l, n, chunk, fb, r, c);
+    else masked_rows_body<IntArith>(lds, p, t, l, n, chunk, fb, r, c);
+}
+
 // ---- the whole transform of a limb of 4096 words (n = 4096) in one workgroup ---------------------------------
 // 512 lanes with eight words each run the twelve stages as radix 8 x 8 x 8 x 8, all exchanges in LDS.  Bound by the chain of
 // its stages, not by bytes (32 KiB per limb): as a column and a row pass the limb took two launches, and at 2 to 25 limbs
@@ -1948,7 +2012,14 @@ void launch_masked_rescale(cm_ctx *ctx, const FinishBatch &fb, u64 *last, u64 *r
     MulPtBatch mb;
     for (int r = 0; r < fb.items; r++) mb.src[r] = fb.u[r], mb.g[r] = fb.mul_g[r], mb.at[r] = fb.mul_at[r];
     launch_mul_pt_rot_last_inv(ctx, last, mb, fb.items, fb.mul_pt, level + 1, d_last_mods, st);
-    launch_ntt_fwd_finish(ctx, red, d_red_mods, fb, st, last, d_red_src);
+    if (n == 4096 || limbs <= SMALL_ROWS) {
+        launch_ntt_fwd_finish(ctx, red, d_red_mods, fb, st, last, d_red_src);
+        return;
+    }
+    Prof prof_(ctx, CM_K_NTT_FWD, limbs, st);
+    const NttTables t = tables_of(ctx, false, limbs);
+    launch_cols_fwd(red, last, d_red_src, nullptr, d_red_mods, t, n, limbs, st);
+    hipLaunchKernelGGL(masked_rows, dim3(limbs * (n >> 12)), dim3(NTT_THREADS), 0, st, red, t, n, fb);
 }
 void launch_conv_ntt(cm_ctx *ctx, const ConvBatch &b, u64 *out, const u64 *in, hipStream_t st, const int *d_rows, const int *d_mods,
                      int limbs, const FinishBatch *fb) {
