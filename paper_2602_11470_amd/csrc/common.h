@@ -101,6 +101,10 @@ struct FpQ {
 #define CM_KS_BATCH 8      // hoisted rotations whose ModDown runs as one batch
 #define CM_MASK_BATCH 32   // masked products of a cache append in one batch, at most (rescale_masked_batch)
 #define CM_NTT_MAX_LIMBS 1024
+// what the arena holds besides one key switch: key-switch sums of two batches of CM_KS_BATCH and the converted limbs of one; at n = 4096, where a
+// launch of CM_KS_BATCH leaves most of the chip idle, of CM_MASK_BATCH (9 MB more on the 5 + 1 ring): two caches behind one another 362 -> 255 us
+inline int arena_sums(int n) { return n == 4096 ? CM_MASK_BATCH : 2 * CM_KS_BATCH; }
+inline int arena_convs(int n) { return n == 4096 ? CM_MASK_BATCH : CM_KS_BATCH; }
 
 struct ConvTable {            // fast base conversion src -> dst (all indices into the modulus list)
     int ns = 0, nt = 0;

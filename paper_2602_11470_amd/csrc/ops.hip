@@ -29,7 +29,7 @@ static Arena arena_of(const cm_ctx *ctx) {
     a.conv = p, p += 2 * q * n;
     for (int i = 0; i < 3; i++) a.tmp[i] = p, p += 3 * q * n;
     a.misc = p, p += 4 * n;
-    a.bu = p, p += 2 * (size_t)CM_KS_BATCH * 2 * ext * n;      // two batches in flight
+    a.bu = p, p += (size_t)arena_sums(ctx->n) * 2 * ext * n;
     a.bconv = p;
     return a;
 }
@@ -509,10 +509,11 @@ u64 *arena_digits(const cm_ctx *ctx) { return arena_of(ctx).digits; }
 size_t arena_digits_words(const cm_ctx *ctx) { return arena_of(ctx).misc - arena_of(ctx).digits; }
 u64 *arena_batch_sums(const cm_ctx *ctx) { return arena_of(ctx).bu; }
 
-// How many key switches one batch takes at a level: the arena holds the sums of two batches and the converted limbs of one, of CM_KS_BATCH
-// at the top level each, so the low levels, where a batch is short launches, have room for more.
+// How many key switches one batch takes at a level: what the arena holds (arena_sums, arena_convs) is sized for the top level, so the low
+// levels, where a batch is short launches, have room for more.  128 dims moved by 16 pages at level 9 with batches of 8 and as many as
+// fit (17) 9170 and 8490 us, 64 dims at level 4 (32) 2125 and 1905, 128 at level 16 (10) 14400 and 14130.
 int ks_batch_max(const cm_ctx *ctx, int level) {
-    const int sums = 2 * CM_KS_BATCH * (ctx->L + 1 + ctx->K) / (level + 1 + ctx->K), conv = CM_KS_BATCH * (ctx->L + 1) / (level + 1);
+    const int sums = arena_sums(ctx->n) * (ctx->L + 1 + ctx->K) / (level + 1 + ctx->K), conv = arena_convs(ctx->n) * (ctx->L + 1) / (level + 1);
     return std::min(CM_MASK_BATCH, std::min(sums, conv));
 }
 // ModDown of m <= ks_batch_max stacked sums bu[r][2][ext][n] in one batch of launches:

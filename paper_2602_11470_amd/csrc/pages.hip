@@ -264,7 +264,7 @@ extern "C" cm_status cm_kv_take(cm_ctx *ctx, const cm_evk *evk, const cm_kv_sel 
         }
     } else {
         // K pages kept in part, V and X: masked products, rescaled, as many a batch as the work area has room for; those that turn
-        // next to one another and then rotated, CM_KS_BATCH at a time with the key read once
+        // next to one another and then rotated, ks_batch_max at a time
         const KsLevel &kl = ks_level(ctx, lo);
         const size_t ln = (size_t)lv * n, dblk = (size_t)kl.beta * kl.ext * n, ublk = 2 * (size_t)kl.ext * n;
         const u64 *in[3] = {src->d_k, src->d_v, src->d_x};
@@ -307,6 +307,8 @@ extern "C" cm_status cm_kv_take(cm_ctx *ctx, const cm_evk *evk, const cm_kv_sel 
                     ip.it[r].own = outs[r0 + r] + ln, ip.it[r].own_g = (unsigned)g;
                     adds[r] = outs[r0 + r], accs[r] = add ? to[r0 + r] : nullptr;
                 }
+                // one key for all: its words stay in registers over the batch, except at n = 4096, where there are too few lanes for that
+                // (ten ciphertexts 20.4 us against 6.8)
                 if (half) launch_rows_ip(ctx, ip, kl.beta, lo, st, lo + 1);
                 else if (n == 4096) launch_inner_product_batch(ctx, ip, kl.beta, lo, st);
                 else launch_inner_product_shared_key(ctx, ip, kl.beta, lo, st);
