@@ -375,7 +375,8 @@ cm_status cm_vmm_kv(cm_ctx *ctx, const cm_evk *evk, const cm_kv *kv, int32_t whi
  * the other flags may differ. */
 /* Copies of a cache: beams, drafts, a prompt that several continuations share.  dsts: 1 or more different caches other than
  * src (else CM_E_INVAL), each at a level of its own up to src's (else CM_E_LEVEL; a copy at a lower level is a level drop) and
- * with room for its tokens (else CM_E_LAYOUT).  What a dst held is replaced; its pages behind the last token are cleared. */
+ * with room for its tokens and for the place of its next append (else CM_E_LAYOUT).  What a dst held is replaced; its pages
+ * behind the last token are cleared. */
 cm_status cm_kv_fork(cm_ctx *ctx, const cm_kv *src, cm_kv *const *dsts, int32_t ndst, void *stream);
 /* Which tokens of a cache are kept, and where they go.  keep: host, ntok bytes, non-zero = kept; shift: every kept page c goes to
  * page c + shift, |shift| < dim, which has to lie in 0 .. dim - 1 (else CM_E_LAYOUT).  Made for caches of the shape and level of
@@ -384,8 +385,9 @@ cm_status cm_kv_fork(cm_ctx *ctx, const cm_kv *src, cm_kv *const *dsts, int32_t 
  * coefficients, for callers that need bit-identical plaintexts on two implementations: first the kept tokens in the layout of
  * the scores (slots (c, h, tau) of token c t + tau), then, for every different pattern of kept residues among the pages that
  * keep some but not all of their tokens, in the order of their first page, the slots (e, h, tau) of its residues.  Without a
- * kept token none is read.  The object holds 1 + p plaintexts of level + 1 limbs. */
+ * kept token none is read.  The object holds 1 + p plaintexts of level + 1 limbs; cm_kv_sel_masks: 1 + p, 0 without a kept token. */
 typedef struct cm_kv_sel cm_kv_sel;
+int32_t cm_kv_sel_masks(const cm_kv *like, const uint8_t *keep, int32_t ntok);
 cm_status cm_kv_sel_create(cm_ctx *ctx, const cm_kv *like, const uint8_t *keep, int32_t ntok, int32_t shift,
                            const int64_t *coeffs, cm_kv_sel **out);
 void cm_kv_sel_destroy(cm_kv_sel *sel);
@@ -447,7 +449,7 @@ cm_status cm_gqa_sv(cm_ctx *ctx, const cm_evk *evk, const cm_gqa *gqa, const cm_
  * table: host [heads * group][nbuckets], row hk * group + g; bucket: host [cap], a bucket 0 .. nbuckets - 1 for every distance
  * (else CM_E_INVAL).  The largest t_kv - 1 distances are the tokens behind the query in its own page: a bucket
  * whose entries are the mask's value there makes the bias causal.  mask: the value for pages that `first` hides (0: none, and `first` has to
- * be -1).  Every entry and the mask times scale below 2^61 (else CM_E_INVAL), and the padding heads get zeros.  level, scale (0 =
+ * be -1).  Every entry and the mask times scale below 2^61 (else CM_E_INVAL); the padding heads take no entry.  level, scale (0 =
  * the context scale): those of the scores.  coeffs (nullable, host [passes * phases + 1][n]): integer coefficients of
  * plaintext [pass][phase] for a query in page 0 -- at place `phase` (decode, t_kv of them) or with the group's first token
  * at phase * t (prompt, `group` of them) -- and of the mask's value in the slots of row 0; the last is read only with a mask.

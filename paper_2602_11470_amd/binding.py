@@ -109,6 +109,7 @@ _SIGS = {
     "cm_kv_fork": ([_vp, _vp, _vp, _i32, _vp], _i32),
     "cm_kv_sel_create": ([_vp, _vp, _vp, _i32, _i32, _vp, _P(_vp)], _i32),
     "cm_kv_sel_destroy": ([_vp], None),
+    "cm_kv_sel_masks": ([_vp, _vp, _i32], _i32),
     "cm_kv_sel_steps": ([_vp, _vp, _i32], _i32),
     "cm_kv_take": ([_vp, _vp, _vp, _vp, _vp, _i32, _vp], _i32),
     "cm_relbias_create": ([_vp, _i32, _i32, _i32, _i32, _i32, _f64, _i32, _vp, _vp, _f64, _vp, _P(_vp)], _i32),
@@ -528,6 +529,7 @@ class KvSelection:
         self.ctx, self.h = ctx, _vp()
         k = _np(np.asarray(keep) != 0, np.uint8)
         c = _np(coeffs, np.int64) if coeffs is not None else None
+        assert c is None or (c.ndim == 2 and c.shape[1] == ctx.n and len(c) >= lib.cm_kv_sel_masks(like.h, k.ctypes.data, k.size))
         _chk(lib.cm_kv_sel_create(ctx.h, like.h, k.ctypes.data, k.size, shift, c.ctypes.data if c is not None else None, C.byref(self.h)))
 
     def steps(self):
@@ -551,6 +553,7 @@ class RelBias:
         cap = ctx.S // (1 << (heads - 1).bit_length())
         c = _np(coeffs, np.int64) if coeffs is not None else None
         assert t.ndim == 2 and t.shape[0] == heads * group and b.shape == (cap,)
+        assert c is None or (c.ndim == 2 and c.shape[1] == ctx.n and len(c) >= group * (cap // max(dim, 1)) + (mask != 0))
         _chk(lib.cm_relbias_create(ctx.h, heads, dim, group, int(prompt), level, scale, t.shape[1], t.ctypes.data, b.ctypes.data, mask,
                                    c.ctypes.data if c is not None else None, C.byref(self.h)))
         self.passes = lib.cm_relbias_passes(self.h)

@@ -147,8 +147,33 @@ extern "C" void cm_kv_sel_destroy(cm_kv_sel *s) {
     ks_many_tables_destroy(&s->tabs);
     delete s;
 }
+// the kept residues of page c, and how many they are
+static int page_pattern(const cm_kv *like, const uint8_t *keep, int ntok, int c, std::vector<uint8_t> &p) {
+    int kept = 0;
+    p.assign(like->t, 0);
+    for (int r = 0; r < like->t && c * like->t + r < ntok; r++)
+        if (keep[c * like->t + r]) p[r] = 1, kept++;
+    return kept;
+}
+extern "C" int32_t cm_kv_sel_masks(const cm_kv *like, const uint8_t *keep, int32_t ntok) {
+    if (!like || !keep || ntok < 0 || ntok > like->E * like->t) return 0;
+    try {
+        std::vector<std::vector<uint8_t>> patterns;
+        std::vector<uint8_t> p;
+        bool any = false;
+        for (int c = 0; c * like->t < ntok; c++) {
+            const int kept = page_pattern(like, keep, ntok, c, p);
+            any = any || kept;
+            if (kept && kept < std::min(like->t, ntok - c * like->t) && std::find(patterns.begin(), patterns.end(), p) == patterns.end()) patterns.push_back(p);
+        }
+        return any ? 1 + (int32_t)patterns.size() : 0;
+    } catch (...) {
+        return 0;
+    }
+}
 extern "C" cm_status cm_kv_sel_create(cm_ctx *ctx, const cm_kv *like, const uint8_t *keep, int32_t ntok, int32_t shift, const int64_t *coeffs,
                                       cm_kv_sel **out) {
+    (void)hipGetLastError();          // stale errors of earlier calls are not this call's
     if (!ctx || !like || like->ctx != ctx || !out || ntok < 0 || (ntok && !keep)) return CM_E_INVAL;
     if (like->level < 3) return CM_E_LEVEL;                      // the result is a cache, and those begin at level 2
     const int t = like->t, E = like->E, S = like->S;
@@ -164,11 +189,10 @@ extern "C" cm_status cm_kv_sel_create(cm_ctx *ctx, const cm_kv *like, const uint
         std::vector<int> from(E, -1);
         for (int c = 0; c < pages && status == CM_OK; c++) {
             const int stored = std::min(t, ntok - c * t);
-            std::vector<uint8_t> p(t, 0);
-            int kept = 0;
-            for (int r = 0; r < stored; r++)
-                if (keep[c * t + r]) p[r] = 1, kept++, s->kept_end = (c + shift) * t + r + 1;
+            std::vector<uint8_t> p;
+            const int kept = page_pattern(like, keep, ntok, c, p);
             if (!kept) continue;
+            for (int r = 0; r < stored; r++) if (p[r]) s->kept_end = (c + shift) * t + r + 1;
             if (c + shift < 0 || c + shift >= E) { status = CM_E_LAYOUT; break; }
             s->any = true;
             if (kept == stored) {
@@ -199,7 +223,7 @@ extern "C" cm_status cm_kv_sel_create(cm_ctx *ctx, const cm_kv *like, const uint
                 status = coeffs ? cm_pt_from_coeffs(ctx, coeffs + i * n, lv, scale, &pt) : cm_encode(ctx, m.data(), nullptr, S, lv, scale, &pt);
             }
             if (status == CM_OK && !s->rows.empty()) status = ks_many_tables_create(ctx, lv - 1, ks_batch_max(ctx, lv - 1), &s->tabs, 2, 1);
-            if (status == CM_OK) ks_level(ctx, lv), get_qlinv(ctx, lv);      // the per-level tables that a take reads
+            if (status == CM_OK) ks_level(ctx, lv), get_qlinv(ctx, lv), get_pinv(ctx, lv - 1);      // the per-level tables that a take reads
         }
     } catch (...) {
         status = CM_E_NOMEM;

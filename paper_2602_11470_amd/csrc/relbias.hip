@@ -8,6 +8,8 @@
 // sequence, a window) is the sum of rotations of one plaintext row, formed once per number of rows.
 #include <math.h>
 
+#include <algorithm>
+
 #include "kv.h"
 
 typedef u64 u64x2 __attribute__((ext_vector_type(2)));
@@ -72,6 +74,7 @@ extern "C" void cm_relbias_destroy(cm_relbias *rb) {
 extern "C" cm_status cm_relbias_create(cm_ctx *ctx, int32_t heads, int32_t dim, int32_t group, int32_t prompt, int32_t level, double scale,
                                        int32_t nbuckets, const double *table, const int32_t *bucket, double mask, const int64_t *coeffs,
                                        cm_relbias **out) {
+    (void)hipGetLastError();          // stale errors of earlier calls are not this call's
     if (!ctx || !out || heads < 1 || dim < 1 || group < 1 || nbuckets < 1 || !table || !bucket || (prompt != 0 && prompt != 1)) return CM_E_INVAL;
     if (level < 0 || level > ctx->L) return CM_E_LEVEL;
     const int S = ctx->n / 2;
@@ -142,6 +145,23 @@ extern "C" cm_status cm_relbias_create(cm_ctx *ctx, int32_t heads, int32_t dim, 
     *out = rb;
     return CM_OK;
 }
+// whether an output is another pass's input or output
+static bool outputs_shared(const cm_ct *in, const cm_ct *out, int n) {
+    if (n <= 16) {
+        for (int p = 0; p < n; p++)
+            for (int r = 0; r < n; r++) if (r != p && (out[r].dev == in[p].dev || out[r].dev == out[p].dev)) return true;
+        return false;
+    }
+    std::vector<std::pair<const u64 *, int>> o(n);
+    for (int r = 0; r < n; r++) o[r] = {out[r].dev, r};
+    std::sort(o.begin(), o.end());
+    for (int r = 1; r < n; r++) if (o[r].first == o[r - 1].first) return true;
+    for (int p = 0; p < n; p++) {
+        const auto at = std::lower_bound(o.begin(), o.end(), std::make_pair((const u64 *)in[p].dev, 0));
+        if (at != o.end() && at->first == in[p].dev && at->second != p) return true;
+    }
+    return false;
+}
 extern "C" int32_t cm_relbias_passes(const cm_relbias *rb) { return rb ? rb->passes : 0; }
 extern "C" cm_status cm_relbias_apply(cm_ctx *ctx, const cm_relbias *rb, int32_t token, int32_t first, int32_t pass0, int32_t npass, const cm_ct *in,
                                       cm_ct *out, void *stream) {
@@ -153,10 +173,11 @@ extern "C" cm_status cm_relbias_apply(cm_ctx *ctx, const cm_relbias *rb, int32_t
     if (npass > rb->passes - pass0) return CM_E_LAYOUT;
     for (int p = 0; p < npass; p++) {
         if (!in[p].dev || !out[p].dev || in[p].ncomp != 2) return CM_E_INVAL;
-        for (int r = 0; r < npass; r++) if (r != p && (out[r].dev == in[p].dev || out[r].dev == out[p].dev)) return CM_E_INVAL;
         if (in[p].level != rb->level) return CM_E_LEVEL;
         if (!(fabs(in[p].scale / rb->scale - 1) < 1e-9)) return CM_E_SCALE;
     }
+    CM_TRY
+    if (outputs_shared(in, out, npass)) return CM_E_INVAL;
     hipStream_t st = (hipStream_t)stream;
     const int n = ctx->n, limbs = rb->level + 1, S = n / 2, page = token / rb->t_kv, phase = rb->prompt ? token % rb->t_kv / t : token % rb->t_kv;
     const size_t words = (size_t)limbs * n;
@@ -180,4 +201,5 @@ extern "C" cm_status cm_relbias_apply(cm_ctx *ctx, const cm_relbias *rb, int32_t
     }
     for (int p = 0; p < npass; p++) out[p].level = in[p].level, out[p].ncomp = 2, out[p].scale = in[p].scale;
     RETURN_LAUNCH_STATUS();
+    CM_CATCH
 }

@@ -203,6 +203,21 @@ def test_view_shows_what_export_reads(rings):
         assert np.array_equal(ctx.ct_export(_ct(ctx, words)), kv.export(w, idx))
 
 
+def test_words_outlive_the_cache_object(rings):
+    import gc
+    import torch
+    from paper_2602_11470_amd import binding as B
+    ctx = rings(SMALL)
+    kv = _filled(ctx, 4, 16, 4, 3, True, 300, 5)
+    words, copy = kv.words(B.CM_KV_INDEX), kv.words(B.CM_KV_INDEX).clone()
+    assert kv.words(B.CM_KV_INDEX) is words
+    del kv
+    gc.collect()
+    others = [_filled(ctx, 4, 16, 4, 3, True, 300, 6 + i) for i in range(3)]
+    torch.cuda.synchronize()
+    assert torch.equal(words, copy) and len(others) == 3
+
+
 def test_take_matches_the_oracle(rings):
     """Encrypted tokens, a ragged selection moved by three pages: every ciphertext limb for limb the oracle's."""
     from oracle import ckks, packing, params, vmm
@@ -318,6 +333,45 @@ def test_refusals(rings):
     d = B.cm_ct()
     assert B.lib.cm_kv_view(good.h, B.CM_SV, 16, C.byref(d)) == -5 and B.lib.cm_kv_view(good.h, B.CM_SV, -1, C.byref(d)) == -5
     other.close()
+
+
+def test_the_first_call_may_be_captured(rings):
+    """No per-level table is left for the first take to build: captured at once, at a level that nothing has used."""
+    import torch
+    from paper_2602_11470_amd import binding as B
+    ctx = B.Context(4096, 9, 2, 2, 50, 50, 60, 2.0 ** 50)
+    try:
+        src, taken, again = _filled(ctx, 4, 16, 4, 7, True, 300, 1), _filled(ctx, 4, 16, 4, 6, True, 0, 2), _filled(ctx, 4, 16, 4, 6, True, 0, 3)
+        keep = np.arange(300) % 11 != 0
+        sel = ctx.kv_sel(src, keep, 3)
+        keys = ctx.keygen_rotations(ctx.keygen_secret(1), sel.steps(), 2)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            ctx.kv_take(keys, sel, src, taken)
+        graph.replay()
+        ctx.kv_take(keys, sel, src, again)
+        torch.cuda.synchronize()
+        for w in _which(B, True):
+            assert torch.equal(taken.words(w), again.words(w))
+    finally:
+        ctx.close()
+
+
+def test_number_of_masks(rings):
+    from paper_2602_11470_amd import binding as B
+    ctx = rings(SMALL)
+    kv = ctx.kv_create(4, 16, 3)                                             # pages of 32 tokens
+    masks = lambda keep: B.lib.cm_kv_sel_masks(kv.h, np.ascontiguousarray(keep, dtype=np.uint8).ctypes.data, len(keep))  # noqa: E731
+    keep = np.ones(100, dtype=np.uint8)
+    assert masks(keep) == 1                                                  # the last page keeps all of its four tokens
+    assert masks(keep * 0) == 0 and masks(keep[:0]) == 0
+    keep[[3, 35]] = 0
+    assert masks(keep) == 2                                                  # pages 0 and 1 keep the same residues
+    keep[36] = 0
+    assert masks(keep) == 3
+    keep[64:] = 0
+    assert masks(keep) == 3
+    assert masks(np.ones(513)) == 0 and B.lib.cm_kv_sel_masks(None, None, 0) == 0 and B.lib.cm_kv_sel_masks(kv.h, None, 3) == 0
 
 
 @pytest.mark.parametrize("side_stream", [False, True])

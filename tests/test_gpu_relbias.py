@@ -240,6 +240,13 @@ def test_refusals(rings):
     assert status(lambda: apply(bias, 0, [three])) == -1
     assert status(lambda: other.relbias_apply(bias, 0, two)) == -1
     assert all(torch.equal(_words(x), b) for x, b in zip(s, before))
+    many = ctx.relbias(1, 16, np.zeros((1, 3)), np.zeros(2048, dtype=np.int32), 1, prompt=True)
+    m = [_random(ctx, 1, gen) for _ in range(20)]
+    spare = [_random(ctx, 1, gen) for _ in range(20)]
+    assert status(lambda: apply(many, 0, m, outs=spare[:19] + [m[3]])) == -1
+    assert status(lambda: apply(many, 0, m, outs=spare[:19] + [spare[0]])) == -1
+    assert status(lambda: apply(many, 0, m[:19] + [m[0]], outs=m[:19] + [spare[0]])) == -1
+    assert status(lambda: apply(many, 0, m, outs=spare[:10] + m[10:])) == 0
     other.close()
 
 
