@@ -115,8 +115,8 @@ void cm_ctx_destroy(cm_ctx *ctx);
  *     only b_j is kept and the kernels regenerate a_j from its stream.  Same residues either way, hence
  *     bit-identical results.  A key set can only be used while the option has the value it was generated
  *     under (else CM_E_INVAL).
- *   CM_OPT_TWO_STEP_MASKS  value != 0: cm_kv_append(_group) forms its masked products as stored
- *     ciphertexts and rescales them afterwards, instead of forming them inside the rescale's transform
+ *   CM_OPT_TWO_STEP_MASKS  value != 0: cm_kv_append(_group) and cm_kv_take form their masked products as
+ *     stored ciphertexts and rescale them afterwards, instead of forming them inside the rescale's transform
  *     (a cross-check of that fused path, bit-identical results). */
 enum { CM_OPT_EVK_STORED_A = 1, CM_OPT_TWO_STEP_MASKS = 2 };
 cm_status cm_ctx_set_option(cm_ctx *ctx, int32_t option, int32_t value);
@@ -385,7 +385,9 @@ cm_status cm_kv_fork(cm_ctx *ctx, const cm_kv *src, cm_kv *const *dsts, int32_t 
  * coefficients, for callers that need bit-identical plaintexts on two implementations: first the kept tokens in the layout of
  * the scores (slots (c, h, tau) of token c t + tau), then, for every different pattern of kept residues among the pages that
  * keep some but not all of their tokens, in the order of their first page, the slots (e, h, tau) of its residues.  Without a
- * kept token none is read.  The object holds 1 + p plaintexts of level + 1 limbs; cm_kv_sel_masks: 1 + p, 0 without a kept token. */
+ * kept token none is read.  The object holds 1 + p plaintexts of level + 1 limbs; cm_kv_sel_masks: 1 + p, 0 without a kept token.
+ * At n = 4096 the first object of a context that lists steps makes room in the context for larger batches of key switches:
+ * 64 (2 n_q + n_p) limbs, held until the context is destroyed. */
 typedef struct cm_kv_sel cm_kv_sel;
 int32_t cm_kv_sel_masks(const cm_kv *like, const uint8_t *keep, int32_t ntok);
 cm_status cm_kv_sel_create(cm_ctx *ctx, const cm_kv *like, const uint8_t *keep, int32_t ntok, int32_t shift,

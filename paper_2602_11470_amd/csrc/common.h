@@ -101,10 +101,6 @@ struct FpQ {
 #define CM_KS_BATCH 8      // hoisted rotations whose ModDown runs as one batch
 #define CM_MASK_BATCH 32   // masked products of a cache append in one batch, at most (rescale_masked_batch)
 #define CM_NTT_MAX_LIMBS 1024
-// what the arena holds besides one key switch: key-switch sums of two batches of CM_KS_BATCH and the converted limbs of one; at n = 4096, where a
-// launch of CM_KS_BATCH leaves most of the chip idle, of CM_MASK_BATCH (9 MB more on the 5 + 1 ring): two caches behind one another 362 -> 255 us
-inline int arena_sums(int n) { return n == 4096 ? CM_MASK_BATCH : 2 * CM_KS_BATCH; }
-inline int arena_convs(int n) { return n == 4096 ? CM_MASK_BATCH : CM_KS_BATCH; }
 
 struct ConvTable {            // fast base conversion src -> dst (all indices into the modulus list)
     int ns = 0, nt = 0;
@@ -202,6 +198,7 @@ struct cm_ctx {
     bool two_step_masks = false;   // cache appends multiply, store and rescale instead of fusing the product into the rescale
     // scratch arena
     u64 *arena = nullptr;
+    u64 *batch_arena = nullptr;     // sums and converted limbs of CM_MASK_BATCH key switches (ks_batches_grow), or null: those of the arena
     size_t arena_words = 0;
     int *d_idx = nullptr;                          // 0, 1, 2, ...: modulus index lists of consecutive limbs
     int *d_idx_stage = nullptr;                    // [CM_NTT_MAX_LIMBS] staging of a caller's modulus index list (cm_ntt)

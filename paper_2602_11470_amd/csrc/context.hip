@@ -387,7 +387,7 @@ extern "C" cm_status cm_ctx_create(const cm_params *p, cm_ctx **out) {
     const int beta = (ctx->L + ctx->alpha) / ctx->alpha;
     size_t limbs = (size_t)(ctx->L + 1) + (size_t)beta * ext + 2 * (size_t)ext + 2 * (size_t)(ctx->L + 1) +
                    9 * (size_t)(ctx->L + 1) + 4 +
-                   2 * ((size_t)arena_sums(n) * ext + (size_t)arena_convs(n) * (ctx->L + 1));  // batched ModDowns
+                   (size_t)CM_KS_BATCH * 2 * (2 * ext + ctx->L + 1);  // batched ModDown of hoisted rotations
     ctx->arena_words = limbs * n;
     if (hipMalloc((void **)&ctx->arena, ctx->arena_words * sizeof(u64)) != hipSuccess) ctx->arena = nullptr;
     if (!ctx->d_modc || !ctx->d_pmont || !ctx->d_ubound || !ctx->d_tw || !ctx->d_itw || !ctx->d_ninv ||
@@ -433,7 +433,7 @@ extern "C" void cm_ctx_destroy(cm_ctx *ctx) {
     hipFree(ctx->d_idx);
     hipFree(ctx->d_idx_stage);
     hipFree(ctx->d_cdt);
-    hipFree(ctx->arena);
+    hipFree(ctx->arena), hipFree(ctx->batch_arena);
     for (auto &kv : ctx->modup)
         for (auto &t : kv.second) free_conv(t);
     for (auto &kv : ctx->moddown) free_conv(kv.second);

@@ -179,20 +179,23 @@ struct FinishBatch {
     // (same layout) and have in_rows limbs a component (0: level + 1, like out)
     const u64 *ainv = nullptr;
     int in_rows = 0;
-    // u_r is not stored but formed on the fly as u[r] * (mul_pt read through the Galois map mul_g[r]): the masked
-    // products of a cache append, whose rescale is this tail (mul_pt[ext][n], multiplier form; nullable)
+    // u_r is not stored but formed on the fly as u[r] * (a plaintext read through a Galois map): the masked products of a cache append and of
+    // kept tokens, whose rescale is this tail (mul_pt[..][ext][n], multiplier form; nullable).  mul[r]: the plaintext's number above
+    // the low 16 bits, which hold (g - 1) / 2 (g is odd and below 2^17; there are at most 1 + 2^14 masks of pages)
     const u64 *mul_pt = nullptr;
-    unsigned mul_g[CM_MASK_BATCH] = {}, mul_at[CM_MASK_BATCH] = {};
+    unsigned mul[CM_MASK_BATCH] = {};
+    __host__ __device__ unsigned mul_g(int r) const { return 2 * (mul[r] & 0xffffu) + 1; }
+    __host__ __device__ const u64 *mul_row(int r, int l, int n) const { return mul_pt + ((size_t)(mul[r] >> 16) * ext + l) * n; }
 };
 void launch_cols_inv(cm_ctx *ctx, u64 *data, const int *d_rows, const int *d_mod_idx, int limbs, hipStream_t st);
 // forward transform of conv[items*ncomp*(level+1)][n] (mods 0..level repeating) with that tail
 // with src: the first pass reads row d_src_rows[i] of src for limb i (words below twice that limb's modulus) instead of conv
 void launch_ntt_fwd_finish(cm_ctx *ctx, u64 *conv, const int *d_mods, const FinishBatch &fb, hipStream_t st,
                            const u64 *src = nullptr, const int *d_src_rows = nullptr);
-// The masked products of fb rescaled: out_r = (u_r mask_r - the last limb's residues) q_level^-1 (+ accum_r), fb.ext = level + 1.  The residues
-// of the last limb have to fit the other moduli as they are.  scratch: last[2 items][n] and red[2 items][level][n].
-void launch_masked_rescale(cm_ctx *ctx, const FinishBatch &fb, u64 *last, u64 *red, const int *d_last_mods, const int *d_red_mods, const int *d_red_src,
-                           hipStream_t st);
+// The masked products of fb (mul_pt set; mb and pt name them once more) rescaled: out_r = (u_r mask_r - the last limb's residues) q_level^-1
+// (+ accum_r), fb.ext = level + 1.  The residues of the last limb have to fit the other moduli as they are.  scratch: last[2 items][n] and red[2 items][level][n].
+void launch_masked_rescale(cm_ctx *ctx, const MulPtBatch &mb, const u64 *pt, const FinishBatch &fb, u64 *last, u64 *red, const int *d_last_mods,
+                           const int *d_red_mods, const int *d_red_src, hipStream_t st);
 
 // Base conversion of `batch` items and the forward transform of the results.  Item z: table (z % tab_period)*tab_step
 // (tab_period 0 = batch), input (z / in_group)*in_stride, output z*out_stride; own_src: the items' own source rows are
@@ -271,6 +274,8 @@ cm_status moddown_second_keep_many(cm_ctx *ctx, const u64 *Rs, int level, int m,
 cm_status moddown_many(cm_ctx *ctx, u64 *us, int level, int cnt, u64 *const *outs, hipStream_t st);
 // key switches that one moddown_batch_into takes at a level, at least CM_KS_BATCH, at most CM_MASK_BATCH
 int ks_batch_max(const cm_ctx *ctx, int level);
+// room for larger batches where they pay; false: no memory
+bool ks_batches_grow(cm_ctx *ctx);
 // one batch (m <= ks_batch_max): outs[r] = ModDown(us + r*2*ext*n) + perm_g(addends[r]) on the first addend_comps
 // components (+ accums[r]); addends / accums nullable arrays of nullable pointers
 cm_status moddown_batch_into(cm_ctx *ctx, u64 *us, int level, int m, const u64 *const *addends, int addend_comps, u64 g,

@@ -491,19 +491,14 @@ __device__ __forceinline__ void finish_tail(AT at, const A &ar, const u64 *lds, 
     // once instead of one load-wait-use chain per word.
     u64 uu[NW], aa[NW], cc[NW];
     if (fb.mul_pt) {
-        // u = u[r] * (mul_pt through the Galois map mul_g[r]), formed here instead of being read
+        // u = u[r] * (the plaintext through the Galois map), formed here instead of being read
         const typename A::Tail tl(ar, t, l, pi, pis);
-        const u64 *mp = fb.mul_pt + ((size_t)fb.mul_at[r] * fb.ext + l) * n;
-        const unsigned mg = fb.mul_g[r];
+        const u64 *mp = fb.mul_row(r, l, n);
+        const unsigned mg = fb.mul_g(r);
 #pragma unroll
         for (int k = 0; k < NW; k++) uu[k] = up[LANES * k];
-        if (mg) {
 #pragma unroll
-            for (int k = 0; k < NW; k++) aa[k] = mp[perm_src(pos0 + LANES * k, mg, logn)];
-        } else {
-#pragma unroll
-            for (int k = 0; k < NW; k++) aa[k] = mp[pos0 + LANES * k];
-        }
+        for (int k = 0; k < NW; k++) aa[k] = mp[perm_src(pos0 + LANES * k, mg, logn)];
         if (ac) {
 #pragma unroll
             for (int k = 0; k < NW; k++) cc[k] = TAIL_LD(ac + LANES * k);
@@ -1158,11 +1153,11 @@ __device__ __forceinline__ void masked_rows_body(u64 *lds, const u64 *p, const N
     const int sub = threadIdx.x & 15, blk = threadIdx.x >> 4, logn = 31 - __clz(n);
     const u64 B = (u64)chunk * 16 + blk;
     const unsigned pos0 = chunk * 4096 + threadIdx.x;
-    const u64 *up = fb.u[r] + ((size_t)c * fb.ext + l) * n + pos0, *mp = fb.mul_pt + ((size_t)fb.mul_at[r] * fb.ext + l) * n;
+    const u64 *up = fb.u[r] + ((size_t)c * fb.ext + l) * n + pos0, *mp = fb.mul_row(r, l, n);
     const size_t at = ((size_t)c * (fb.level + 1) + l) * n + pos0;
     u64 *op = fb.out[r] + at;
     const u64 *ac = fb.accum[r] ? fb.accum[r] + at : nullptr;
-    const unsigned g = fb.mul_g[r], eg = ((__brev(pos0) >> (31 - logn)) | 1u) * g;       // perm_src's e g
+    const unsigned g = fb.mul_g(r), eg = ((__brev(pos0) >> (31 - logn)) | 1u) * g;       // perm_src's e g
     typename A::T v[16];
     u64 raw[16];
 #pragma unroll
@@ -1378,13 +1373,13 @@ __device__ __forceinline__ void masked_full_last(u64 *lds, u64 (&w)[8], const Nt
     A ar;
     ar.init(ti, lv, n);
     const ModC m = ti.modc[lv];
-    const u64 *src = fb.u[r] + ((size_t)c * fb.ext + lv) * n, *mask = fb.mul_pt + ((size_t)fb.mul_at[r] * fb.ext + lv) * n;
-    const unsigned g = fb.mul_g[r];
+    const u64 *src = fb.u[r] + ((size_t)c * fb.ext + lv) * n, *mask = fb.mul_row(r, lv, n);
+    const unsigned g = fb.mul_g(r);
     typename A::T v[8];
     full_inv_words(lds, v, ar, [&](u64 (&x)[8]) {
         u64 y[8];
 #pragma unroll
-        for (int k = 0; k < 8; k++) x[k] = src[threadIdx.x + 512 * k], y[k] = mask[g ? perm_src(threadIdx.x + 512 * k, g, logn) : threadIdx.x + 512 * k];
+        for (int k = 0; k < 8; k++) x[k] = src[threadIdx.x + 512 * k], y[k] = mask[perm_src(threadIdx.x + 512 * k, g, logn)];
 #pragma unroll
         for (int k = 0; k < 8; k++) x[k] = redc((u128)x[k] * y[k], m.q, m.qinv);
     });
@@ -2003,17 +1998,15 @@ void launch_ntt_fwd_finish(cm_ctx *ctx, u64 *conv, const int *d_mods, const Fini
 // other.
 #define JOIN_TARGETS 512
 bool conv_joins_inv(const cm_ctx *ctx, bool near, int ns, int targets) { return ctx->n == 4096 && near && ns == 1 && targets <= JOIN_TARGETS; }
-void launch_masked_rescale(cm_ctx *ctx, const FinishBatch &fb, u64 *last, u64 *red, const int *d_last_mods, const int *d_red_mods, const int *d_red_src,
-                           hipStream_t st) {
+void launch_masked_rescale(cm_ctx *ctx, const MulPtBatch &mb, const u64 *pt, const FinishBatch &fb, u64 *last, u64 *red, const int *d_last_mods,
+                           const int *d_red_mods, const int *d_red_src, hipStream_t st) {
     const int n = ctx->n, level = fb.level + 1, comps = 2 * fb.items, limbs = comps * level;
     if (n == 4096 && limbs <= JOIN_TARGETS) {
         Prof prof_(ctx, CM_K_NTT_FWD, limbs, st);
         hipLaunchKernelGGL(masked_full, dim3(limbs), dim3(FULL_THREADS), 0, st, fb, tables_of(ctx, false, limbs), tables_of(ctx, true, 0), n);
         return;
     }
-    MulPtBatch mb;
-    for (int r = 0; r < fb.items; r++) mb.src[r] = fb.u[r], mb.g[r] = fb.mul_g[r], mb.at[r] = fb.mul_at[r];
-    launch_mul_pt_rot_last_inv(ctx, last, mb, fb.items, fb.mul_pt, level + 1, d_last_mods, st);
+    launch_mul_pt_rot_last_inv(ctx, last, mb, fb.items, pt, level + 1, d_last_mods, st);
     if (n == 4096 || limbs <= SMALL_ROWS) {
         launch_ntt_fwd_finish(ctx, red, d_red_mods, fb, st, last, d_red_src);
         return;

@@ -29,8 +29,8 @@ static Arena arena_of(const cm_ctx *ctx) {
     a.conv = p, p += 2 * q * n;
     for (int i = 0; i < 3; i++) a.tmp[i] = p, p += 3 * q * n;
     a.misc = p, p += 4 * n;
-    a.bu = p, p += (size_t)arena_sums(ctx->n) * 2 * ext * n;
-    a.bconv = p;
+    a.bu = ctx->batch_arena ? ctx->batch_arena : p;
+    a.bconv = a.bu + (size_t)(ctx->batch_arena ? CM_MASK_BATCH : 2 * CM_KS_BATCH) * 2 * ext * n;      // the arena's: two batches in flight
     return a;
 }
 
@@ -509,12 +509,21 @@ u64 *arena_digits(const cm_ctx *ctx) { return arena_of(ctx).digits; }
 size_t arena_digits_words(const cm_ctx *ctx) { return arena_of(ctx).misc - arena_of(ctx).digits; }
 u64 *arena_batch_sums(const cm_ctx *ctx) { return arena_of(ctx).bu; }
 
-// How many key switches one batch takes at a level: what the arena holds (arena_sums, arena_convs) is sized for the top level, so the low
-// levels, where a batch is short launches, have room for more.  128 dims moved by 16 pages at level 9 with batches of 8 and as many as
+// How many key switches one batch takes at a level: the arena holds the sums of two batches and the converted limbs of one, of CM_KS_BATCH
+// at the top level each, so the low levels, where a batch is short launches, have room for more.  128 dims moved by 16 pages at level 9 with batches of 8 and as many as
 // fit (17) 9170 and 8490 us, 64 dims at level 4 (32) 2125 and 1905, 128 at level 16 (10) 14400 and 14130.
 int ks_batch_max(const cm_ctx *ctx, int level) {
-    const int sums = arena_sums(ctx->n) * (ctx->L + 1 + ctx->K) / (level + 1 + ctx->K), conv = arena_convs(ctx->n) * (ctx->L + 1) / (level + 1);
+    if (ctx->batch_arena) return CM_MASK_BATCH;
+    const int sums = 2 * CM_KS_BATCH * (ctx->L + 1 + ctx->K) / (level + 1 + ctx->K), conv = CM_KS_BATCH * (ctx->L + 1) / (level + 1);
     return std::min(CM_MASK_BATCH, std::min(sums, conv));
+}
+// At n = 4096, where a launch of CM_KS_BATCH leaves most of the chip idle, room for CM_MASK_BATCH (23 MB on the 5 + 1 ring) from the first
+// selection on that rotates: two caches behind one another 362 -> 253 us.  Not in the arena: what is allocated behind a larger one (keys, inputs)
+// lies elsewhere, and there the inner products of a small product take 5.3 instead of 5.0 us (the whole of it 356 instead of 353).
+bool ks_batches_grow(cm_ctx *ctx) {
+    const size_t words = (size_t)CM_MASK_BATCH * 2 * (2 * (ctx->L + 1) + ctx->K) * ctx->n;
+    if (ctx->n == 4096 && !ctx->batch_arena && hipMalloc((void **)&ctx->batch_arena, words * sizeof(u64)) != hipSuccess) ctx->batch_arena = nullptr;
+    return ctx->n != 4096 || ctx->batch_arena;
 }
 // ModDown of m <= ks_batch_max stacked sums bu[r][2][ext][n] in one batch of launches:
 // outs[r] = ModDown(bu[r]) (+ perm_{gs[r]}(addends[r]) on the first addend_comps components) (+ accums[r])
@@ -1111,12 +1120,12 @@ bool rescale_masked_into(cm_ctx *ctx, const MulPtBatch &mb, int cnt, const u64 *
     fb.items = cnt, fb.level = level - 1, fb.ext = level + 1, fb.addend_comps = 0, fb.ncomp = 2, fb.comp0 = 0;
     for (int r = 0; r < CM_MASK_BATCH; r++) fb.addend[r] = nullptr, fb.accum[r] = nullptr, fb.u[r] = nullptr, fb.out[r] = nullptr, fb.g[r] = 0;
     for (int r = 0; r < cnt; r++) {
-        fb.u[r] = mb.src[r], fb.out[r] = outs[r], fb.mul_g[r] = mb.g[r], fb.mul_at[r] = mb.at[r];
+        fb.u[r] = mb.src[r], fb.out[r] = outs[r], fb.mul[r] = mb.at[r] << 16 | mb.g[r] >> 1;
         fb.accum[r] = accumulate ? fb.out[r] : nullptr;
     }
     fb.mul_pt = pt;
     fb.pinv = get_qlinv(ctx, level);
-    launch_masked_rescale(ctx, fb, last, red, k.d_last_mods, k.d_red_mods, k.d_red_src, st);
+    launch_masked_rescale(ctx, mb, pt, fb, last, red, k.d_last_mods, k.d_red_mods, k.d_red_src, st);
     return true;
 }
 extern "C" cm_status cm_rescale(cm_ctx *ctx, const cm_ct *a, cm_ct *out, void *stream) {

@@ -222,6 +222,7 @@ extern "C" cm_status cm_kv_sel_create(cm_ctx *ctx, const cm_kv *like, const uint
                 }
                 status = coeffs ? cm_pt_from_coeffs(ctx, coeffs + i * n, lv, scale, &pt) : cm_encode(ctx, m.data(), nullptr, S, lv, scale, &pt);
             }
+            if (status == CM_OK && !s->rows.empty() && !ks_batches_grow(ctx)) status = CM_E_NOMEM;
             if (status == CM_OK && !s->rows.empty()) status = ks_many_tables_create(ctx, lv - 1, ks_batch_max(ctx, lv - 1), &s->tabs, 2, 1);
             if (status == CM_OK) ks_level(ctx, lv), get_qlinv(ctx, lv), get_pinv(ctx, lv - 1);      // the per-level tables that a take reads
         }

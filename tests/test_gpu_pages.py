@@ -357,6 +357,35 @@ def test_the_first_call_may_be_captured(rings):
         ctx.close()
 
 
+def test_work_from_before_a_rotating_selection_goes_on(rings):
+    """The first selection that rotates makes room for larger batches on the small ring: batched key switches captured before it and
+    called after it give what they gave before."""
+    import torch
+    from paper_2602_11470_amd import binding as B
+    ctx = B.Context(4096, 6, 2, 2, 50, 50, 60, 2.0 ** 50)
+    try:
+        gen = torch.Generator(device="cuda").manual_seed(5)
+        steps = list(range(1, 12))
+        src, dst = _filled(ctx, 4, 16, 4, 4, True, 300, 1), _filled(ctx, 4, 16, 4, 3, True, 0, 2)
+        keys = ctx.keygen_rotations(ctx.keygen_secret(1), steps, 2)
+        x = _ct(ctx, _residues(ctx, (2,), 6, gen))
+        first = [_words(c).clone() for c in ctx.rotate_hoisted(keys, x, steps)]
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            captured = ctx.rotate_hoisted(keys, x, steps)
+        sel = ctx.kv_sel(src, np.ones(300, dtype=bool), 3)
+        assert len(sel.steps()) > 0
+        moved = ctx.keygen_rotations(ctx.keygen_secret(1), sel.steps(), 2)
+        for _ in range(3):
+            ctx.kv_take(moved, sel, src, dst)
+            graph.replay()
+            again = ctx.rotate_hoisted(keys, x, steps)
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, _words(b)) and torch.equal(a, _words(c)) for a, b, c in zip(first, captured, again))
+    finally:
+        ctx.close()
+
+
 def test_number_of_masks(rings):
     from paper_2602_11470_amd import binding as B
     ctx = rings(SMALL)
