@@ -465,7 +465,8 @@ int32_t cm_relbias_passes(const cm_relbias *rb);
 /* out[i] = in[i] + the bias of pass pass0 + i, i < npass.  first = -1: every page is seen; else the place of the first token of
  * a page (a multiple of t_kv): pages outside first's .. token's, in the order of the ring, get the mask's value on top.
  * in, out: arrays of npass ciphertexts at the object's level and scale (else CM_E_LEVEL, CM_E_SCALE); out[i] may be in[i]
- * itself (its second component is then not touched), no other two of them may share memory (CM_E_INVAL). */
+ * itself (its second component is then not touched), else no word of an out[i] may be a word of another of them (CM_E_INVAL).
+ * Inputs may share memory with one another. */
 cm_status cm_relbias_apply(cm_ctx *ctx, const cm_relbias *rb, int32_t token, int32_t first, int32_t pass0, int32_t npass,
                            const cm_ct *in, cm_ct *out, void *stream);
 

@@ -9,6 +9,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <iterator>
 
 #include "kv.h"
 
@@ -145,20 +146,30 @@ extern "C" cm_status cm_relbias_create(cm_ctx *ctx, int32_t heads, int32_t dim, 
     *out = rb;
     return CM_OK;
 }
-// whether an output is another pass's input or output
-static bool outputs_shared(const cm_ct *in, const cm_ct *out, int n) {
+// whether the words that an output is written to are another output's, or an input's other than that the pass's output is its input itself.  Arrays
+// of n ciphertexts of `words` words each; by sorting where they are many.
+bool relbias_outputs_shared(const cm_ct *in, const cm_ct *out, int n, size_t words) {
+    const uintptr_t len = words * sizeof(u64);
+    auto at = [](const cm_ct &c) { return (uintptr_t)c.dev; };
+    auto meet = [len](uintptr_t a, uintptr_t b) { return (a < b ? b - a : a - b) < len; };
     if (n <= 16) {
         for (int p = 0; p < n; p++)
-            for (int r = 0; r < n; r++) if (r != p && (out[r].dev == in[p].dev || out[r].dev == out[p].dev)) return true;
+            for (int r = 0; r < n; r++) {
+                if (r != p && meet(at(out[r]), at(out[p]))) return true;
+                if (!(r == p && out[r].dev == in[p].dev) && meet(at(out[r]), at(in[p]))) return true;
+            }
         return false;
     }
-    std::vector<std::pair<const u64 *, int>> o(n);
-    for (int r = 0; r < n; r++) o[r] = {out[r].dev, r};
+    std::vector<std::pair<uintptr_t, int>> o(n);
+    for (int r = 0; r < n; r++) o[r] = {at(out[r]), r};
     std::sort(o.begin(), o.end());
-    for (int r = 1; r < n; r++) if (o[r].first == o[r - 1].first) return true;
+    for (int r = 1; r < n; r++) if (meet(o[r - 1].first, o[r].first)) return true;
     for (int p = 0; p < n; p++) {
-        const auto at = std::lower_bound(o.begin(), o.end(), std::make_pair((const u64 *)in[p].dev, 0));
-        if (at != o.end() && at->first == in[p].dev && at->second != p) return true;
+        const uintptr_t a = at(in[p]);
+        // the outputs are apart: only the last one that begins in front of the input and the first one that does not can meet it
+        auto next = std::lower_bound(o.begin(), o.end(), std::make_pair(a, -1));
+        if (next != o.begin() && meet(std::prev(next)->first, a)) return true;
+        if (next != o.end() && meet(next->first, a) && !(next->first == a && next->second == p)) return true;
     }
     return false;
 }
@@ -177,7 +188,7 @@ extern "C" cm_status cm_relbias_apply(cm_ctx *ctx, const cm_relbias *rb, int32_t
         if (!(fabs(in[p].scale / rb->scale - 1) < 1e-9)) return CM_E_SCALE;
     }
     CM_TRY
-    if (outputs_shared(in, out, npass)) return CM_E_INVAL;
+    if (relbias_outputs_shared(in, out, npass, 2 * (size_t)(rb->level + 1) * ctx->n)) return CM_E_INVAL;
     hipStream_t st = (hipStream_t)stream;
     const int n = ctx->n, limbs = rb->level + 1, S = n / 2, page = token / rb->t_kv, phase = rb->prompt ? token % rb->t_kv / t : token % rb->t_kv;
     const size_t words = (size_t)limbs * n;

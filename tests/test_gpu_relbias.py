@@ -275,3 +275,29 @@ def test_captured_and_replayed(rings):
         eager = ctx.relbias_apply(bias, 33, ctx.relbias_apply(bias, 100, scores, first=64), first=480)
         torch.cuda.synchronize()
         assert all(torch.equal(a, _words(b)) for a, b in zip(got, eager))
+
+
+def test_scores_that_overlap_are_refused(rings):
+    """Windows of one buffer: an output that begins inside another pass's ciphertext, or inside its own input, is refused; neighbours are not."""
+    import torch
+    from paper_2602_11470_amd import binding as B
+    ctx, level = rings("small"), 2
+    bias = ctx.relbias(4, 16, np.ones((8, 3)), np.zeros(512, dtype=np.int32), level, group=2)
+    words = 2 * (level + 1) * ctx.n
+    buf = torch.zeros(6 * words, dtype=torch.int64, device="cuda")
+
+    def at(word):
+        c = B.Ct(ctx, level)
+        c.buf, c.d = buf, B.cm_ct(buf.data_ptr() + 8 * word, level, 2, ctx.scale)
+        return c
+    for ins, outs in (((0, words), (ctx.n, 3 * words)), ((0, words), (2 * words, 3 * words - 2)), ((0, 2 * words), (4 * words, words + 2)),
+                      ((0, 2 * words), (2, 2 * words)), ((2, 2 * words), (0, 4 * words)), ((0, words), (0, words // 2))):
+        with pytest.raises(B.CachemirError) as e:
+            ctx.relbias_apply(bias, 0, [at(w) for w in ins], outs=[at(w) for w in outs])
+        assert e.value.status == -1
+    torch.cuda.synchronize()
+    assert not buf.any()
+    ctx.relbias_apply(bias, 0, [at(0), at(ctx.n)], outs=[at(2 * words), at(3 * words)])          # inputs may overlap
+    ctx.relbias_apply(bias, 0, [at(4 * words), at(5 * words)], outs=[at(4 * words), at(5 * words)])
+    assert buf[2 * words:].any() and not buf[: 2 * words].any()
+    assert torch.equal(buf[2 * words: 4 * words], buf[4 * words:])
