@@ -449,10 +449,12 @@ cm_status cm_gqa_sv(cm_ctx *ctx, const cm_evk *evk, const cm_gqa *gqa, const cm_
  *     of delta residues (group = 1: CM_QK_GROUP; else cm_gqa_qk with t_kv for its group and the query heads of a KV head side by side,
  *     as everywhere in the layout); the group's first token is at place `token`, a multiple of t.
  * table: host [heads * group][nbuckets], row hk * group + g; bucket: host [cap], a bucket 0 .. nbuckets - 1 for every distance
- * (else CM_E_INVAL).  The largest t_kv - 1 distances are the tokens behind the query in its own page: a bucket
- * whose entries are the mask's value there makes the bias causal.  mask: the value for pages that `first` hides (0: none, and `first` has to
- * be -1).  Every entry and the mask times scale below 2^61 (else CM_E_INVAL); the padding heads take no entry.  level, scale (0 =
- * the context scale): those of the scores.  coeffs (nullable, host [passes * phases + 1][n]): integer coefficients of
+ * (else CM_E_INVAL).  mask: the value for pages that `first` hides and for the places that CM_RELBIAS_CAUSAL hides (0: none; `first` then
+ * has to be -1, and the flag is CM_E_INVAL).  flags: CM_RELBIAS_CAUSAL adds it to the places behind the query in its own page.
+ * Their distances, among the largest t_kv - 1, do not tell them from the first tokens of the page behind the query's, which is the oldest
+ * one once the ring is full: a bucket of the mask's value there hides both.  Every entry and the mask times scale below 2^61 (else
+ * CM_E_INVAL); the padding heads take no entry.  level, scale (0 = the context scale): those of the scores.
+ * coeffs (nullable, host [passes * phases + 1][n]): integer coefficients, with what the flags add, of
  * plaintext [pass][phase] for a query in page 0 -- at place `phase` (decode, t_kv of them) or with the group's first token
  * at phase * t (prompt, `group` of them) -- and of the mask's value in the slots of row 0; the last is read only with a mask.
  * Device memory: group * t_kv plaintexts, and with a mask dim + 1 more, one for every number of visible pages. */
@@ -460,6 +462,11 @@ typedef struct cm_relbias cm_relbias;
 cm_status cm_relbias_create(cm_ctx *ctx, int32_t heads, int32_t dim, int32_t group, int32_t prompt, int32_t level,
                             double scale, int32_t nbuckets, const double *table, const int32_t *bucket, double mask,
                             const int64_t *coeffs, cm_relbias **out);
+enum { CM_RELBIAS_CAUSAL = 1 };
+/* cm_relbias_create with flags (the plain call: 0). */
+cm_status cm_relbias_create_ex(cm_ctx *ctx, int32_t heads, int32_t dim, int32_t group, int32_t prompt, int32_t level,
+                               double scale, int32_t nbuckets, const double *table, const int32_t *bucket, double mask,
+                               uint32_t flags, const int64_t *coeffs, cm_relbias **out);
 void cm_relbias_destroy(cm_relbias *rb);
 int32_t cm_relbias_passes(const cm_relbias *rb);
 /* out[i] = in[i] + the bias of pass pass0 + i, i < npass.  first = -1: every page is seen; else the place of the first token of

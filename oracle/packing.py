@@ -407,10 +407,10 @@ class KvLayout:
         return sorted(r * self.H * self.t for r in rows if r)
 
     # ---- relative position bias: E t places in a ring, distance of a query at p from place a = (p - a) mod E t ---------
-    def bias_slots(self, table, bucket, token, first=None, mask=0.0, group=1, delta=0, prompt=False):
+    def bias_slots(self, table, bucket, token, first=None, mask=0.0, group=1, delta=0, prompt=False, causal=False):
         """What pass delta of the scores takes for a query at place `token` (a prompt's group begins there): in slot (c, hk, j)
         table[hk * group + g][bucket[distance]] of the query head g that meets residue j there, and `mask` in the pages that are
-        not among those from `first`'s to the query's."""
+        not among those from `first`'s to the query's, and, causal, in the places behind the query in its own page."""
         cap, t = self.E * self.t, self.t // group
         out = np.zeros(self.S)
         for c in range(self.E):
@@ -424,7 +424,8 @@ class KvLayout:
                         g, place = (j // t - delta) % group, token
                     d = (place - (c * self.t + j)) % cap
                     v = table[hk * group + g][bucket[d]] if hk < self.heads else 0.0
-                    out[self.slot(c, hk, j)] = v + (mask if hidden else 0.0)
+                    behind = causal and c == place // self.t and c * self.t + j > place
+                    out[self.slot(c, hk, j)] = v + (mask if hidden or behind else 0.0)
         return out
 
     def k_index_steps(self):

@@ -20,6 +20,7 @@ lib = C.CDLL(LIB_PATH)
 CM_QK, CM_SV, CM_QK_GROUP, CM_SV_GROUP, CM_KV_INDEX = 0, 1, 2, 3, 4
 CM_VMM_RAISED_SUMS, CM_VMM_DIRECT_GIANTS, CM_VMM_TOKEN_BATCH, CM_VMM_UNROLLED_LADDERS = 1, 2, 4, 8
 CM_KV_UNROLLED_LADDERS, CM_KV_KEY_INDEX = 1, 2
+CM_RELBIAS_CAUSAL = 1
 CM_OPT_EVK_STORED_A, CM_OPT_TWO_STEP_MASKS = 1, 2
 
 
@@ -113,6 +114,7 @@ _SIGS = {
     "cm_kv_sel_steps": ([_vp, _vp, _i32], _i32),
     "cm_kv_take": ([_vp, _vp, _vp, _vp, _vp, _i32, _vp], _i32),
     "cm_relbias_create": ([_vp, _i32, _i32, _i32, _i32, _i32, _f64, _i32, _vp, _vp, _f64, _vp, _P(_vp)], _i32),
+    "cm_relbias_create_ex": ([_vp, _i32, _i32, _i32, _i32, _i32, _f64, _i32, _vp, _vp, _f64, C.c_uint32, _vp, _P(_vp)], _i32),
     "cm_relbias_destroy": ([_vp], None),
     "cm_relbias_passes": ([_vp], _i32),
     "cm_relbias_apply": ([_vp, _vp, _i32, _i32, _i32, _i32, _vp, _vp, _vp], _i32),
@@ -388,8 +390,9 @@ class Context:
         """dst = (add: +=) the tokens of src that sel keeps; evk may be None where sel has no steps."""
         _chk(lib.cm_kv_take(self.h, evk.h if evk is not None else None, sel.h, src.h, dst.h, int(add), _stream()))
 
-    def relbias(self, heads, dim, table, bucket, level, scale=0.0, group=1, prompt=False, mask=0.0, coeffs=None):
-        return RelBias(self, heads, dim, table, bucket, level, scale, group, prompt, mask, coeffs)
+    def relbias(self, heads, dim, table, bucket, level, scale=0.0, group=1, prompt=False, mask=0.0, coeffs=None,
+                causal=False):
+        return RelBias(self, heads, dim, table, bucket, level, scale, group, prompt, mask, coeffs, causal)
 
     def relbias_apply(self, bias, token, scores, first=-1, pass0=0, outs=None):
         """scores (a list, one for each pass from pass0 on) plus their bias; outs may be scores."""
@@ -545,17 +548,18 @@ class KvSelection:
 
 
 class RelBias:
-    """Relative position bias on scores (cm_relbias_*): table [query heads][buckets], bucket of every distance in the ring."""
+    """Relative position bias on scores (cm_relbias_*): table [query heads][buckets], bucket of every distance in the ring; causal: the
+    mask on the places behind the query in its own page."""
 
-    def __init__(self, ctx, heads, dim, table, bucket, level, scale, group, prompt, mask, coeffs):
+    def __init__(self, ctx, heads, dim, table, bucket, level, scale, group, prompt, mask, coeffs, causal):
         self.ctx, self.h = ctx, _vp()
         t, b = _np(table, np.float64), _np(bucket, np.int32)
         cap = ctx.S // (1 << (heads - 1).bit_length())
         c = _np(coeffs, np.int64) if coeffs is not None else None
         assert t.ndim == 2 and t.shape[0] == heads * group and b.shape == (cap,)
         assert c is None or (c.ndim == 2 and c.shape[1] == ctx.n and len(c) >= group * (cap // max(dim, 1)) + (mask != 0))
-        _chk(lib.cm_relbias_create(ctx.h, heads, dim, group, int(prompt), level, scale, t.shape[1], t.ctypes.data, b.ctypes.data, mask,
-                                   c.ctypes.data if c is not None else None, C.byref(self.h)))
+        _chk(lib.cm_relbias_create_ex(ctx.h, heads, dim, group, int(prompt), level, scale, t.shape[1], t.ctypes.data, b.ctypes.data, mask,
+                                      CM_RELBIAS_CAUSAL if causal else 0, c.ctypes.data if c is not None else None, C.byref(self.h)))
         self.passes = lib.cm_relbias_passes(self.h)
 
     def __del__(self):

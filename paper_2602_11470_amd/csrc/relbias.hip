@@ -75,8 +75,14 @@ extern "C" void cm_relbias_destroy(cm_relbias *rb) {
 extern "C" cm_status cm_relbias_create(cm_ctx *ctx, int32_t heads, int32_t dim, int32_t group, int32_t prompt, int32_t level, double scale,
                                        int32_t nbuckets, const double *table, const int32_t *bucket, double mask, const int64_t *coeffs,
                                        cm_relbias **out) {
+    return cm_relbias_create_ex(ctx, heads, dim, group, prompt, level, scale, nbuckets, table, bucket, mask, 0, coeffs, out);
+}
+extern "C" cm_status cm_relbias_create_ex(cm_ctx *ctx, int32_t heads, int32_t dim, int32_t group, int32_t prompt, int32_t level, double scale,
+                                          int32_t nbuckets, const double *table, const int32_t *bucket, double mask, uint32_t flags,
+                                          const int64_t *coeffs, cm_relbias **out) {
     (void)hipGetLastError();          // stale errors of earlier calls are not this call's
     if (!ctx || !out || heads < 1 || dim < 1 || group < 1 || nbuckets < 1 || !table || !bucket || (prompt != 0 && prompt != 1)) return CM_E_INVAL;
+    if ((flags & ~(uint32_t)CM_RELBIAS_CAUSAL) || ((flags & CM_RELBIAS_CAUSAL) && mask == 0)) return CM_E_INVAL;
     if (level < 0 || level > ctx->L) return CM_E_LEVEL;
     const int S = ctx->n / 2;
     if (heads > S || dim > S) return CM_E_LAYOUT;
@@ -117,7 +123,10 @@ extern "C" cm_status cm_relbias_create(cm_ctx *ctx, int32_t heads, int32_t dim, 
                     const int u = (j - delta + t_kv) % t_kv;                 // prompt: the query's residue in its page
                     const int g = prompt ? u / t : ((j / t - delta) % group + group) % group;
                     const int place = prompt ? phase * t + u % t : phase, d = ((place - j - x * t_kv) % cap + cap) % cap;
-                    for (int h = 0; h < H; h++) m[(size_t)(x * H + h) * t_kv + j] = h < real ? table[(size_t)(h * group + g) * nbuckets + bucket[d]] : 0.0;
+                    // the query's own page: the places behind it have the largest distances, which the oldest page of a full ring has as well
+                    const double behind = (flags & CM_RELBIAS_CAUSAL) && x == 0 && j > place ? mask : 0.0;
+                    for (int h = 0; h < H; h++)
+                        m[(size_t)(x * H + h) * t_kv + j] = (h < real ? table[(size_t)(h * group + g) * nbuckets + bucket[d]] : 0.0) + behind;
                 }
             status = encode(rb->d_pts + p * words, m, p);
         }
