@@ -590,14 +590,14 @@ class _Words:
 class KvCache:
     def __init__(self, ctx, heads, dim, r_i, level, scale, max_tokens, unrolled_ladders=False, shared_dims=1, key_index=False):
         self.ctx, self.h, self.level, self.key_index = ctx, _vp(), level, key_index
-        t = ctx.S // ((1 << (heads - 1).bit_length()) * dim)
+        # tokens a page; of a shape that the library refuses below it may be none
+        t = ctx.S // ((1 << (heads - 1).bit_length()) * dim) if dim > 0 else 0
         max_tokens = dim * t if max_tokens is None else max_tokens
-        self._words = {}
-        self.dim, self.r_i, self.pages = dim, r_i or dim, -(-max_tokens // t)
         _chk(lib.cm_kv_create_ex(ctx.h, heads, dim, r_i, level, scale, max_tokens,
                                  (CM_KV_UNROLLED_LADDERS if unrolled_ladders else 0) | (CM_KV_KEY_INDEX if key_index else 0),
                                  C.byref(self.h)))
-        self._owner = _KvHandle(self.h)
+        self._owner, self._words = _KvHandle(self.h), {}
+        self.dim, self.r_i, self.pages = dim, r_i or dim, -(-max_tokens // t)
         if shared_dims != 1:
             self.set_shared_dims(shared_dims)
 

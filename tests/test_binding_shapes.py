@@ -1,0 +1,33 @@
+"""What the Python binding does in front of the library: shapes that the library refuses arrive there.  No GPU is needed."""
+import types
+
+import pytest
+
+SHAPES = [(4, 1024), (2048, 2), (3, 2048), (4096, 1), (1 << 20, 4), (4, 0), (0, 16), (-3, 16), (4, -16), (4, 24)]
+
+
+@pytest.mark.parametrize("heads,dim", SHAPES)
+@pytest.mark.parametrize("max_tokens", [None, 8, 0, -1])
+def test_a_cache_of_any_shape_is_refused_by_the_library(heads, dim, max_tokens):
+    """Without a context every creation is refused; what is computed from the shape must not end before that."""
+    from paper_2602_11470_amd import binding as B
+    with pytest.raises(B.CachemirError) as e:
+        B.KvCache(types.SimpleNamespace(S=2048, h=None), heads, dim, 0, 3, 0.0, max_tokens)
+    assert e.value.status == -1
+
+
+@pytest.mark.gpu
+def test_shapes_that_do_not_fit_say_so():
+    from paper_2602_11470_amd import binding as B
+    ctx = B.config1()
+    try:
+        for heads, dim, status in ((4, 1024, -5), (2048, 2, -5), (3, 2048, -5), (4, 24, -5), (4, 0, -1), (0, 16, -1), (4, -16, -1)):
+            with pytest.raises(B.CachemirError) as e:
+                ctx.kv_create(heads, dim, 3, max_tokens=8)
+            assert e.value.status == status
+            with pytest.raises(B.CachemirError) as e:
+                ctx.kv_create(heads, dim, 3)
+            assert e.value.status in (-1, -5)
+        assert ctx.kv_create(4, 16, 3).pages == 16 and ctx.kv_create(4, 16, 3, max_tokens=33).pages == 2
+    finally:
+        ctx.close()
