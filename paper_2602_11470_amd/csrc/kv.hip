@@ -63,6 +63,7 @@ extern "C" cm_status cm_kv_create_ex(cm_ctx *ctx, int32_t heads, int32_t dim, in
     if (!ctx || !out || heads < 1 || dim < 1 || max_tokens < 1 || (flags & ~(uint32_t)(CM_KV_UNROLLED_LADDERS | CM_KV_KEY_INDEX))) return CM_E_INVAL;
     if (level < 2 || level > ctx->L) return CM_E_LEVEL;
     const int S = ctx->n / 2;
+    if (heads > S || dim > S) return CM_E_LAYOUT;
     heads = 1 << ilog2(heads);            // a head count that is not a power of two is padded to the next one
     if (!pow2(dim) || heads * dim > S) return CM_E_LAYOUT;
     cm_kv *kv = new (std::nothrow) cm_kv();

@@ -31,3 +31,18 @@ def test_shapes_that_do_not_fit_say_so():
         assert ctx.kv_create(4, 16, 3).pages == 16 and ctx.kv_create(4, 16, 3, max_tokens=33).pages == 2
     finally:
         ctx.close()
+
+
+@pytest.mark.gpu
+def test_head_counts_whose_product_with_the_dims_passes_32_bits():
+    import ctypes as C
+    from paper_2602_11470_amd import binding as B
+    ctx = B.config1()
+    try:
+        h = C.c_void_p()
+        for heads, dim in ((1 << 20, 1 << 12), (1 << 16, 1 << 16), (1 << 30, 4), ((1 << 31) - 1, 2), (2, 1 << 30)):
+            assert B.lib.cm_kv_create_ex(ctx.h, heads, dim, 0, 3, 0.0, 8, 0, C.byref(h)) == -5
+            assert B.lib.cm_rope_create(ctx.h, heads, dim, 3, 0, 0, 10000.0, None, C.byref(h)) == -5
+        assert h.value is None
+    finally:
+        ctx.close()
