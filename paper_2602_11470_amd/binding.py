@@ -180,7 +180,7 @@ class Context:
         torch.cuda.init()
         _chk(lib.cm_ctx_create(C.byref(self.prm), C.byref(h)))
         self.h, self.n, self.S, self.L, self.K = h, n, n // 2, n_q - 1, n_p
-        self.scale = scale
+        self.scale, self.device = scale, torch.device("cuda", torch.cuda.current_device())
 
     def close(self):
         if self.h:
@@ -630,7 +630,7 @@ class KvCache:
         _chk(lib.cm_kv_view(self.h, which, 0, C.byref(d)))
         limbs, ct = self.level + 1, 2 * (self.level + 1) * self.ctx.n
         count = self.pages if which == CM_QK else self.dim
-        w = torch.as_tensor(_Words(self._owner, d.dev, count * ct), device="cuda").view(count, 2, limbs, self.ctx.n)
+        w = torch.as_tensor(_Words(self._owner, d.dev, count * ct), device=self.ctx.device).view(count, 2, limbs, self.ctx.n)
         self._words[which] = w.unflatten(0, (self.r_i, self.dim // self.r_i)).transpose(0, 1) if which == CM_KV_INDEX else w
         return self._words[which]
 

@@ -1,4 +1,4 @@
-"""What the Python binding does in front of the library: shapes that the library refuses arrive there.  No GPU is needed."""
+"""What the Python binding does around the library's calls: shapes that the library refuses arrive there, a cache's words are shown where they lie."""
 import types
 
 import pytest
@@ -14,6 +14,41 @@ def test_a_cache_of_any_shape_is_refused_by_the_library(heads, dim, max_tokens):
     with pytest.raises(B.CachemirError) as e:
         B.KvCache(types.SimpleNamespace(S=2048, h=None), heads, dim, 0, 3, 0.0, max_tokens)
     assert e.value.status == -1
+
+
+def test_words_are_asked_for_on_the_device_of_the_context(monkeypatch):
+    """The memory lies on the context's device; asked for on the current one, another device would silently get a copy."""
+    import torch
+    from paper_2602_11470_amd import binding as B
+    asked = []
+
+    def as_tensor(words, device=None):
+        asked.append(torch.device(device))
+        return torch.zeros(words.__cuda_array_interface__["shape"], dtype=torch.int64)
+    monkeypatch.setattr(B.lib, "cm_kv_view", lambda *a: 0)
+    monkeypatch.setattr(B.torch, "as_tensor", as_tensor)
+    kv = B.KvCache.__new__(B.KvCache)
+    kv.ctx, kv.h, kv.level, kv.dim, kv.r_i, kv.pages = types.SimpleNamespace(n=8, device=torch.device("cuda", 3)), None, 2, 4, 2, 3
+    kv._words, kv._owner = {}, None
+    assert kv.words(B.CM_QK).shape == (3, 2, 3, 8) and kv.words(B.CM_SV).shape == (4, 2, 3, 8) and kv.words(B.CM_KV_INDEX).shape == (2, 2, 2, 3, 8)
+    assert asked == [torch.device("cuda", 3)] * 3
+
+
+@pytest.mark.gpu
+def test_words_lie_where_the_library_says():
+    import ctypes as C
+    import torch
+    from paper_2602_11470_amd import binding as B
+    ctx = B.config1()
+    try:
+        kv = ctx.kv_create(4, 16, 3, key_index=True)
+        assert ctx.device == torch.device("cuda", torch.cuda.current_device())
+        for which in (B.CM_QK, B.CM_SV, B.CM_KV_INDEX):
+            d = B.cm_ct()
+            assert B.lib.cm_kv_view(kv.h, which, 0, C.byref(d)) == 0
+            assert kv.words(which).data_ptr() == d.dev and kv.words(which).device == ctx.device
+    finally:
+        ctx.close()
 
 
 @pytest.mark.gpu
