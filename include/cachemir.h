@@ -454,10 +454,11 @@ cm_status cm_gqa_sv(cm_ctx *ctx, const cm_evk *evk, const cm_gqa *gqa, const cm_
  * Their distances, among the largest t_kv - 1, do not tell them from the first tokens of the page behind the query's, which is the oldest
  * one once the ring is full: a bucket of the mask's value there hides both.  Every entry and the mask times scale below 2^61 (else
  * CM_E_INVAL); the padding heads take no entry.  level, scale (0 = the context scale): those of the scores.
- * coeffs (nullable, host [passes * phases + 1][n]): integer coefficients, with what the flags add, of
+ * coeffs (nullable, host [passes * phases + 1][n]): integer coefficients, with what the flag adds in them, of
  * plaintext [pass][phase] for a query in page 0 -- at place `phase` (decode, t_kv of them) or with the group's first token
- * at phase * t (prompt, `group` of them) -- and of the mask's value in the slots of row 0; the last is read only with a mask.
- * Device memory: group * t_kv plaintexts, and with a mask dim + 1 more, one for every number of visible pages. */
+ * at phase * t (prompt, `group` of them) -- and of the mask's value in the slots of row 0; the last is read only with a mask
+ * and dim > 1.
+ * Device memory: group * t_kv plaintexts, and with a mask dim - 1 more, one for every number of visible pages with hidden ones. */
 typedef struct cm_relbias cm_relbias;
 cm_status cm_relbias_create(cm_ctx *ctx, int32_t heads, int32_t dim, int32_t group, int32_t prompt, int32_t level,
                             double scale, int32_t nbuckets, const double *table, const int32_t *bucket, double mask,

@@ -18,10 +18,10 @@ typedef u64 u64x2 __attribute__((ext_vector_type(2)));
 struct cm_relbias {
     cm_ctx *ctx = nullptr;
     int H, E, t_kv, G, level, passes, phases;
-    bool prompt = false;
+    bool prompt = false, masked = false;
     double scale;
     u64 *d_pts = nullptr;          // [passes][phases][level+1][n]
-    u64 *d_unseen = nullptr;       // [E+1][level+1][n]: entry m < E: the mask's value in the rows m .. E-1, entry E: in row 0; null without a mask
+    u64 *d_unseen = nullptr;       // [E-1][level+1][n]: entry m - 1: the mask's value in the rows m .. E-1; null without a mask or other rows
 };
 
 // out = a + (b through the Galois map g), rows limbs
@@ -102,14 +102,16 @@ extern "C" cm_status cm_relbias_create_ex(cm_ctx *ctx, int32_t heads, int32_t di
     cm_relbias *rb = new (std::nothrow) cm_relbias();
     if (!rb) return CM_E_NOMEM;
     cm_status status = CM_OK;
+    u64 *row = nullptr;            // the mask's value in row 0
     try {
-        rb->ctx = ctx, rb->H = H, rb->E = dim, rb->t_kv = t_kv, rb->G = group, rb->level = level, rb->prompt = prompt != 0, rb->scale = scale;
+        rb->ctx = ctx, rb->H = H, rb->E = dim, rb->t_kv = t_kv, rb->G = group, rb->level = level, rb->prompt = prompt != 0, rb->scale = scale, rb->masked = mask != 0;
         rb->passes = prompt ? t_kv : group, rb->phases = prompt ? group : t_kv;
         const int n = ctx->n, polys = rb->passes * rb->phases;
         const size_t words = (size_t)(level + 1) * n;
-        u64 *row = nullptr;
         if (hipMalloc((void **)&rb->d_pts, polys * words * 8) != hipSuccess) status = CM_E_NOMEM;
-        if (status == CM_OK && mask != 0 && hipMalloc((void **)&rb->d_unseen, (dim + 1) * words * 8) != hipSuccess) status = CM_E_NOMEM;
+        if (status == CM_OK && mask != 0 && dim > 1 &&
+            (hipMalloc((void **)&rb->d_unseen, (dim - 1) * words * 8) != hipSuccess || hipMalloc((void **)&row, words * 8) != hipSuccess))
+            status = CM_E_NOMEM;
         auto encode = [&](u64 *dst, const std::vector<double> &m, int i) {
             cm_pt pt;
             pt.dev = dst, pt.mont = 0;
@@ -130,17 +132,17 @@ extern "C" cm_status cm_relbias_create_ex(cm_ctx *ctx, int32_t heads, int32_t di
                 }
             status = encode(rb->d_pts + p * words, m, p);
         }
-        if (status == CM_OK && mask != 0) {
+        if (status == CM_OK && rb->d_unseen) {
             for (int i = 0; i < S; i++) m[i] = i < H * t_kv ? mask : 0.0;
-            row = rb->d_unseen + dim * words;
             status = encode(row, m, polys);
             if (status == CM_OK) {
-                // entry E - 1: the row turned right by E - 1; entry i: entry i + 1 and the row turned right by i
-                for (int i = dim - 1; i >= 0; i--) {
+                // E - 1 pages visible: the row turned right by E - 1; i pages: those of i + 1 and the row turned right by i
+                for (int i = dim - 1; i > 0; i--) {
                     const u64 g = galois_of_step(ctx, (int)(((long long)S - (long long)i * H * t_kv) % S));
-                    if (i == dim - 1) launch_automorphism(ctx, rb->d_unseen + i * words, row, level + 1, g, 0);
-                    else hipLaunchKernelGGL(k_add_turned, dim3(n / 256, level + 1), dim3(256), 0, 0, rb->d_unseen + i * words,
-                                            rb->d_unseen + (i + 1) * words, row, ctx->d_modc, (unsigned)g, n, ctx->logn);
+                    u64 *entry = rb->d_unseen + (i - 1) * words;
+                    if (i == dim - 1) launch_automorphism(ctx, entry, row, level + 1, g, 0);
+                    else hipLaunchKernelGGL(k_add_turned, dim3(n / 256, level + 1), dim3(256), 0, 0, entry, entry + words, row, ctx->d_modc, (unsigned)g, n,
+                                            ctx->logn);
                 }
                 if (hipDeviceSynchronize() != hipSuccess || hipGetLastError() != hipSuccess) status = CM_E_HIP;
             }
@@ -148,6 +150,7 @@ extern "C" cm_status cm_relbias_create_ex(cm_ctx *ctx, int32_t heads, int32_t di
     } catch (...) {
         status = CM_E_NOMEM;
     }
+    hipFree(row);
     if (status != CM_OK) {
         cm_relbias_destroy(rb);
         return status;
@@ -189,7 +192,7 @@ extern "C" cm_status cm_relbias_apply(cm_ctx *ctx, const cm_relbias *rb, int32_t
     if (!ctx || !rb || rb->ctx != ctx || !in || !out || npass < 1 || pass0 < 0) return CM_E_INVAL;
     const int cap = rb->E * rb->t_kv, t = rb->t_kv / rb->G;
     if (token < 0 || token >= cap || (rb->prompt && token % t) || first < -1 || first >= cap || (first > 0 && first % rb->t_kv)) return CM_E_LAYOUT;
-    if (first >= 0 && !rb->d_unseen) return CM_E_LAYOUT;
+    if (first >= 0 && !rb->masked) return CM_E_LAYOUT;
     if (npass > rb->passes - pass0) return CM_E_LAYOUT;
     for (int p = 0; p < npass; p++) {
         if (!in[p].dev || !out[p].dev || in[p].ncomp != 2) return CM_E_INVAL;
@@ -206,7 +209,7 @@ extern "C" cm_status cm_relbias_apply(cm_ctx *ctx, const cm_relbias *rb, int32_t
     unsigned gr = 0;
     if (first >= 0) {
         const int from = first / rb->t_kv, seen = (page - from + rb->E) % rb->E + 1;
-        if (seen < rb->E) row = rb->d_unseen + seen * words, gr = turn(from);
+        if (seen < rb->E) row = rb->d_unseen + (seen - 1) * words, gr = turn(from);
     }
     for (int p0 = 0; p0 < npass; p0 += BIAS_BATCH) {
         const int m = npass - p0 < BIAS_BATCH ? npass - p0 : BIAS_BATCH;

@@ -101,3 +101,24 @@ def test_refusals(ctx):
     for flags, mask in ((B.CM_RELBIAS_CAUSAL, -9.0), (0, 0.0), (0, -9.0)):
         assert create(flags, mask) == 0
         B.lib.cm_relbias_destroy(h)
+
+
+def test_memory_of_an_object_with_a_mask():
+    """group * t_kv plaintexts, and one for every number of visible pages with hidden ones: less than one more is taken."""
+    import torch
+    from paper_2602_11470_amd import binding as B
+    ctx = B.llama_ring(24, 4)
+    try:
+        heads, dim, level = 32, 64, 21
+        cap = ctx.S // heads
+        make = lambda: ctx.relbias(heads, dim, np.ones((heads, 2)), np.zeros(cap, dtype=np.int32), level, mask=-9.0)  # noqa: E731
+        first = make()                                                       # what the context makes on the way
+        torch.cuda.synchronize()
+        before = torch.cuda.mem_get_info()[0]
+        second = make()
+        used = before - torch.cuda.mem_get_info()[0]
+        pt = (level + 1) * ctx.n * 8
+        assert 0 < used < (cap // dim + dim) * pt                           # memory that the runtime holds from the first counts as used before
+        del first, second
+    finally:
+        ctx.close()
