@@ -32,7 +32,7 @@ __global__ void k_add_turned(u64 *out, const u64 *a, const u64 *b, const ModC *_
 }
 
 #define BIAS_BATCH 32
-#define BIAS_LARGE (128 << 20)      // bytes of the scores of a launch
+#define BIAS_LARGE (128 << 20)
 struct BiasBatch {
     const u64 *in[BIAS_BATCH], *pt[BIAS_BATCH];
     u64 *out[BIAS_BATCH];
@@ -40,8 +40,13 @@ struct BiasBatch {
 // out[z] = in[z] + (pt[z] through g, row through gr, 0).  A lane has two neighbouring words, which the Galois map leaves neighbours: 16-byte
 // accesses, the plaintexts' in another order (its aligned runs of 64 stay together, so they coalesce as well).  Bound by memory: eight passes at
 // level 21 (473 MB with the plaintexts) 73.5 us, 6.4 TB/s, with one word a lane 89.7; a single pass is the launch (6.3 us a call from Python, 3.9 of
-// them the launch).  LARGE: scores read past the caches.  Those of a few passes are still in them: four passes at level 8 (75 MB of scores) 15.4 us
-// read plainly, 17.4 past them; eight at level 21 (369 MB) 81.1 and 73.5.  Stores go past them always (four passes 17.9 us otherwise).
+// them the launch).  Stores go past the caches always (four passes at level 8 17.9 us otherwise).  LARGE: scores are read past them as well, from BIAS_LARGE
+// bytes of scores on (both components, in and out).  Reads past the caches cost where the scores are still in them, as those of a few passes
+// are, and pay where they are not.  Plainly and past them, each call on other scores, window masked: 75 MB (four passes at level 8) 15.4 and 17.4 us, 134 MB (eight
+// at level 7) 29.3 and 27.9, 159 MB 36.5 and 32.5, 167 MB 37.1 and 33.1, 218 MB 47.6 and 42.5, 318 MB 69.6 and 60.6, 369 MB 81.1 and 73.8.  On one set of scores
+// again and again 117 MB 20.8 and 22.7, 134 MB 23.5 and 26.3; on 2.5 GB of them in turn 23.8 and 22.7, 26.6 and 26.1.  In place, where a
+// launch moves half of these bytes, the same line holds: four passes at level 11 (100 MB) 13.4 and 12.1 / 15.1 and 12.3, at level 15 (134 MB) 15.9 and 16.7 /
+// 18.2 and 16.6, eight at level 15 (268 MB) 29.3 and 30.1 / 31.8 and 30.1.
 __device__ __forceinline__ u64x2 turned(const u64 *p, unsigned src) {
     const u64x2 w = *(const u64x2 *)(p + (src & ~1u));
     return src & 1u ? u64x2{w.y, w.x} : w;
