@@ -669,12 +669,11 @@ def _context(ring):
     return _contexts[ring]
 
 
+@functools.lru_cache(4)
 def _own_keys(ring, steps):
-    key = (ring, tuple(sorted(set(steps))))
-    if key not in _contexts:
-        ctx = _context(ring)
-        _contexts[key] = ctx.keygen_rotations(ctx.keygen_secret(1), key[1], 2)
-    return _contexts[key]
+    """The library's key set, as few of them held as of the plain form's (_keys)."""
+    ctx = _context(ring)
+    return ctx.keygen_rotations(ctx.keygen_secret(1), steps, 2)
 
 
 def _own_cache(case, level, room, words=None, tokens=0):
@@ -715,7 +714,7 @@ def _own_state(s, words, coeffs):
         return s
     s["dsts"] = [_own_cache(case, case["level"] - 1, _room(case))]
     s["sel"] = ctx.kv_sel(s["src"], _keep(case), case["shift"], coeffs=coeffs)
-    steps = s["sel"].steps()
+    steps = tuple(sorted(set(s["sel"].steps())))
     s["keys"] = _own_keys(case["ring"], steps) if steps else None
     if case["op"] == "concat":
         s["first"] = _own_cache(case, case["level"], _first_tokens(case), words[1], _first_tokens(case))
