@@ -7,7 +7,7 @@
 // So dropping tokens multiplies every V and X ciphertext by a rotation of ONE 0/1 mask M (the kept tokens, page c in row c): by
 // Rot(M, j B) and Rot(M, -g r_i B).  A rescale follows: the result lies one level below.  A page that moves from c to c' = c + s
 // keeps its dims, which says where it goes:
-//   V: k' = k + s (mod E), its rows by (g' - g) r_i;      X: k' = k - s (mod E), its rows by j - j'.
+//   V: k' = k + s (mod E), its rows by (g' - g) r_i to the right;      X: k' = k - s (mod E), its rows by j - j' to the right.
 // Every ciphertext therefore moves as a whole: to another place, and by one rotation by whole rows where the giant step (V) or
 // the baby step (X) of the place is another one.  K ciphertexts move without any arithmetic, unless a page keeps some of its
 // tokens only (a mask by residues).
