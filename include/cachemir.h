@@ -34,10 +34,10 @@
  *    streams of that seed XOR a 64-bit value derived from the SECRET key's seed, which must
  *    therefore be kept private and must not be reused as a public seed.
  *  - A context's scratch arena is shared by all calls on it: calls on one context must not
- *    overlap in time (enqueue them on one stream, or order the streams).  A plan, a cache and
- *    a rotary-embedding object each hold one work area of their own with the same rule.
- *  - The hot calls (cm_rotate*, cm_vmm_pt*, cm_vmm_kv, cm_kv_append, cm_kv_fork, cm_kv_take, cm_rope_apply, cm_relbias_apply
- *    and the element-wise ones) allocate nothing and only enqueue kernels and device copies once the
+ *    overlap in time (enqueue them on one stream, or order the streams).  A plan, a cache,
+ *    a rotary-embedding object, a table of positions and a tree object each hold one work area of their own with the same rule.
+ *  - The hot calls (cm_rotate*, cm_vmm_pt*, cm_vmm_kv, cm_kv_append*, cm_kv_fork, cm_kv_take, cm_rope_apply, cm_relbias_apply,
+ *    cm_rotary_set, cm_rotary_apply, cm_tree_qk, cm_tree_sv and the element-wise ones) allocate nothing and only enqueue kernels and device copies once the
  *    per-level tables exist (the first call at a level builds them), so they can be captured
  *    into a HIP graph after one eager call.
  */
@@ -505,6 +505,89 @@ cm_status cm_rope_apply(cm_ctx *ctx, const cm_evk *evk, const cm_rope *rope, con
  * plaintext, the mask of the residues >= t - delta and the mask of the residues < t - delta. */
 cm_status cm_inner_rot_create(cm_ctx *ctx, int32_t t, int32_t delta, int32_t level,
                               const int64_t *coeffs, cm_rope **out);
+
+/* ---- rotary positions that are given with the call -------------------------------------------------------
+ * cm_rope_* holds the angles of ONE position, encoded when the object is made.  A cm_rotary holds tables of positions instead: which
+ * token stands at which residue, and at which position, is said by cm_rotary_set, which only enqueues kernels; so one object serves every
+ * step, layer (of one level) and tree of drafts.
+ * What is turned: the first rot_dims dims of a head (even, 2 .. dim; the others leave as they are); pairs of neighbours (2m, 2m+1), or with
+ * CM_ROTARY_HALVES (m, rot_dims/2 + m): at position p by p freq[m] (host, rot_dims/2 of them; null: 10000^(-2m/rot_dims)), cosines and sines
+ * times gain.  Residues without a token come out zero, whatever partial sums a projection left there; so do no other slots.
+ * room: positions 0 .. room - 1 (at most 2^24) can be set.  level: of the ciphertexts to turn; they come out one below, their scale kept.  The
+ * special moduli have to be above 2.1 gain q_level (else CM_E_INVAL).
+ * coeffs (nullable, host [cm_rotary_polys(room)][n]): integer coefficients of the tables.  With position = R high + low (R the power of two at or
+ * above sqrt(room)): for every low part cos of the first dims of the pairs, cos of the second ones, sin of the first, sin of the second (times gain, at
+ * residue 0, scale q_level); ones in the dims that are not turned (residue 0, scale q_level; read only if there are any); for every high part cos (one
+ * in dims not turned) and sin in all slots, scale m2.  m1 = p_0; m2 = p_1, or q_0 where there is one special prime.
+ * Exactly: C, S the sums over the tokens of one high part of the low entries turned to their residues, the plaintexts are
+ *   p0 = [sum C c - S s],  p_up = [-sum (S c + C s)] of the first dims,  p_dn = [sum S c + C s] of the second,   [V] = V / m2, to the nearest integer,
+ *   y = rescale(ModDown(p0 P x + p_up Rot'(x, step) + p_dn Rot'(x, -step))),
+ * Rot' the hoisted rotation in the extended basis (cm_rotate_hoisted before its ModDown), step = heads t or, halves, rot_dims/2 heads t slots; where
+ * 2 step = S both rotations are one, with the plaintext [V_up + V_dn].
+ * Device memory: 8 (R + high parts) polynomials of n words, 9 plaintexts, and the raised digits of up to eight ciphertexts (256 MB of
+ * them at most, one at least). */
+typedef struct cm_rotary cm_rotary;
+enum { CM_ROTARY_HALVES = 1 };
+#define CM_ROTARY_ROOM (1 << 24)
+#define CM_ROTARY_MAX 64
+int32_t cm_rotary_polys(int32_t room);
+cm_status cm_rotary_create(cm_ctx *ctx, int32_t heads, int32_t dim, int32_t level, int32_t rot_dims, const double *freq, double gain, int32_t room,
+                           uint32_t flags, const int64_t *coeffs, cm_rotary **out);
+void cm_rotary_destroy(cm_rotary *rotary);
+/* Rotation steps it needs: returns their number (2, or 1), writes up to cap of them (host). */
+int32_t cm_rotary_steps(const cm_rotary *rotary, int32_t *steps, int32_t cap);
+/* host out[rot_dims/2]: base^(-2m/rot_dims), scaled for contexts longer than the model's own:
+ *   CM_ROTARY_LINEAR  par = {factor}: every frequency over factor;
+ *   CM_ROTARY_BASE    par = {factor}: base factor^(rot_dims/(rot_dims-2)) in the place of base;
+ *   CM_ROTARY_BANDS   par = {factor, low, high, context}: those that turn at least `high` times over `context` positions as they are, those that turn
+ *                     at most `low` times over factor, in between a mean of both, linear in the turns. */
+enum { CM_ROTARY_PLAIN = 0, CM_ROTARY_LINEAR = 1, CM_ROTARY_BASE = 2, CM_ROTARY_BANDS = 3 };
+cm_status cm_rotary_freqs(int32_t rot_dims, double base, int32_t scaling, const double *par, double *out);
+/* pos: host [t] (t = S / (heads dim), heads padded), the position of the token at every residue, -1 where there is none (read before the call
+ * returns); outside -1 .. room - 1: CM_E_LAYOUT.  Enqueued: calls on the object that follow on the stream see it.  split: the residues below it belong
+ * to the next page (cm_kv_append_run); 0: there is none.  cm_rotary_apply does not look at it. */
+cm_status cm_rotary_set(cm_ctx *ctx, cm_rotary *rotary, const int32_t *pos, int32_t split, void *stream);
+/* y[i] = x[i] turned, i < count <= CM_ROTARY_MAX (the queries and keys of a token, a group, a tree).  No y may share memory with an x or another y
+ * (CM_E_INVAL); x may.  Before the first cm_rotary_set: CM_E_LAYOUT. */
+cm_status cm_rotary_apply(cm_ctx *ctx, const cm_evk *evk, const cm_rotary *rotary, int32_t count, const cm_ct *x, cm_ct *y, void *stream);
+
+/* Append a run of ntok tokens, 1 <= ntok <= t, at the place of the next append: the last tokens of a prompt, drafted tokens.  k, v hold the token of
+ * place a at residue a mod t; what stands at other residues does not matter.  The run may pass into the next page.  v one level above the cache.
+ * rotary (nullable): the keys take their positions on the way.  Made for the cache's heads and dim, at k's level; its positions are set for exactly the
+ * residues of the run, with split = the number of residues in the next page (else CM_E_LAYOUT).  The rotation's plaintexts are the mask
+ * of the K ciphertexts, so k then is one level above the cache, as without (where the rotation and cm_kv_append take two levels); for a cache with the key
+ * index, whose masks meet rotations of the rotated key, two.
+ * Exactly: as cm_kv_append with, in the place of its masks, the sums of the masks of the run's tokens (K: those of one page for each page; V and index:
+ * all, each token's V mask at its page's row); with rotary K ciphertexts are added cm_rotary_apply's result from the plaintexts of the page's residues. */
+cm_status cm_kv_append_run(cm_ctx *ctx, const cm_evk *evk, cm_kv *kv, const cm_rotary *rotary, int32_t ntok, const cm_ct *k, const cm_ct *v, void *stream);
+
+/* ---- attention of a tree of drafted tokens ----------------------------------------------------------------
+ * `nodes` drafted tokens stand in the cache at places base .. base + nodes - 1, behind what was committed (appended by cm_kv_append_run, say; the
+ * rejected ones are dropped by cm_kv_take); token i follows parent[i] (host, -1 <= parent[i] < i; -1: the last committed token).  Its query sees the
+ * committed tokens from `first` on (a multiple of t_kv, at most base), the drafted tokens it follows, and itself.
+ * Queries stand in the layout of H = group heads heads (t = t_kv / group tokens a ciphertext, as for cm_gqa_qk; group = 1: the cache's own heads): that
+ * of the token at place a at residue a mod t, tokens node0 .. node0 + t - 1 in one ciphertext, one level above the cache.  At residues without one
+ * of them stand the scores of a query that sees no drafted token.
+ * There are t_kv passes (cm_tree_passes, at most 64): scores[delta] holds at slot (c, hk, j) the score of the query in slot (j - delta) mod t_kv of
+ * its block against the token of place c t_kv + j, plus the mask's value (-24 leaves 4e-11 of an exponential) where it is not seen; all pages
+ * outside first's .. the last drafted token's among it.  One level below the cache with the key index, else two.  Exactly: the query moved by delta
+ * residues, formed as cm_rotary_apply does from the rotations by -delta and t_kv - delta and the plaintexts of the residues from delta on and of those below (delta = 0: a level drop), then cm_vmm_kv(CM_QK_GROUP), then the masks added.
+ * cm_tree_sv: t_kv score ciphertexts in that layout at the cache's level times the values (cm_vmm_kv(CM_SV_GROUP)), moved back by t_kv - delta residues and
+ * summed: the attention output in the queries' layout, two levels below.  The moved results are summed in the extended basis, with
+ * one ModDown and rescale; the first one, which does not move, is dropped a level and added.
+ * cm_tree_create: kv gives the shape and level only.  mask: the value; scale: that of the scores (0: of a query at the context's scale); |mask| scale below
+ * 2^61 (else CM_E_INVAL).  coeffs (nullable, host [2 (t_kv - 1) + 2][n]): the residues from 1, 2, .. t_kv - 1 on, scale q_{level+1}, the same at scale
+ * q_{level-1} (the residues below are that scale in all slots, less these), the mask's value in slots (0, h, 0) and in slots (0, h, r), both at the scores' scale.
+ * cm_tree_steps: the rotations needed beyond those of the cache's product (cm_kv_steps; of those only the steps that are multiples of t_kv).
+ * The calls use the work areas of the cache and of the object.  No score may share memory with q or another score (CM_E_INVAL). */
+typedef struct cm_tree cm_tree;
+cm_status cm_tree_create(cm_ctx *ctx, const cm_kv *kv, int32_t group, double mask, double scale, const int64_t *coeffs, cm_tree **out);
+void cm_tree_destroy(cm_tree *tree);
+int32_t cm_tree_passes(const cm_tree *tree);
+int32_t cm_tree_steps(const cm_tree *tree, int32_t *steps, int32_t cap);
+cm_status cm_tree_qk(cm_ctx *ctx, const cm_evk *evk, const cm_tree *tree, const cm_kv *kv, const int32_t *parent, int32_t nodes, int32_t base, int32_t node0,
+                     int32_t first, const cm_ct *q, cm_ct *scores, void *stream);
+cm_status cm_tree_sv(cm_ctx *ctx, const cm_evk *evk, const cm_tree *tree, const cm_kv *kv, const cm_ct *scores, cm_ct *out, void *stream);
 
 /* ---- building blocks exposed for measurement and parity -------------------------------- */
 /* Forward / inverse negacyclic NTT of `limbs` limbs in place (device), limb i under modulus

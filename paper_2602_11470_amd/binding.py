@@ -21,6 +21,8 @@ CM_QK, CM_SV, CM_QK_GROUP, CM_SV_GROUP, CM_KV_INDEX = 0, 1, 2, 3, 4
 CM_VMM_RAISED_SUMS, CM_VMM_DIRECT_GIANTS, CM_VMM_TOKEN_BATCH, CM_VMM_UNROLLED_LADDERS = 1, 2, 4, 8
 CM_KV_UNROLLED_LADDERS, CM_KV_KEY_INDEX = 1, 2
 CM_RELBIAS_CAUSAL = 1
+CM_ROTARY_HALVES = 1
+CM_ROTARY_PLAIN, CM_ROTARY_LINEAR, CM_ROTARY_BASE, CM_ROTARY_BANDS = 0, 1, 2, 3
 CM_OPT_EVK_STORED_A, CM_OPT_TWO_STEP_MASKS = 1, 2
 
 
@@ -118,6 +120,20 @@ _SIGS = {
     "cm_relbias_destroy": ([_vp], None),
     "cm_relbias_passes": ([_vp], _i32),
     "cm_relbias_apply": ([_vp, _vp, _i32, _i32, _i32, _i32, _vp, _vp, _vp], _i32),
+    "cm_rotary_polys": ([_i32], _i32),
+    "cm_rotary_create": ([_vp, _i32, _i32, _i32, _i32, _vp, _f64, _i32, C.c_uint32, _vp, _P(_vp)], _i32),
+    "cm_rotary_destroy": ([_vp], None),
+    "cm_rotary_steps": ([_vp, _vp, _i32], _i32),
+    "cm_rotary_freqs": ([_i32, _f64, _i32, _vp, _vp], _i32),
+    "cm_rotary_set": ([_vp, _vp, _vp, _i32, _vp], _i32),
+    "cm_rotary_apply": ([_vp, _vp, _vp, _i32, _vp, _vp, _vp], _i32),
+    "cm_kv_append_run": ([_vp, _vp, _vp, _vp, _i32, _P(cm_ct), _P(cm_ct), _vp], _i32),
+    "cm_tree_create": ([_vp, _vp, _i32, _f64, _f64, _vp, _P(_vp)], _i32),
+    "cm_tree_destroy": ([_vp], None),
+    "cm_tree_passes": ([_vp], _i32),
+    "cm_tree_steps": ([_vp, _vp, _i32], _i32),
+    "cm_tree_qk": ([_vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _P(cm_ct), _vp, _vp], _i32),
+    "cm_tree_sv": ([_vp, _vp, _vp, _vp, _vp, _P(cm_ct), _vp], _i32),
     "cm_profile_enable": ([_vp, _i32], _i32),
     "cm_profile_get": ([_vp, _i32, _P(_f64), _P(_f64), _P(_f64)], _i32),
     "cm_ntt": ([_vp, _vp, _vp, _i32, _i32, _vp], _i32),
@@ -404,6 +420,46 @@ class Context:
             o.d = d
         return outs
 
+    def rotary(self, heads, dim, level, room, rot_dims=None, freq=None, gain=1.0, halves=False, coeffs=None):
+        return Rotary(self, heads, dim, level, room, rot_dims, freq, gain, halves, coeffs)
+
+    def rotary_set(self, rotary, positions, split=0):
+        """The position of the token at every residue, -1 where there is none."""
+        p = _np(positions, np.int32)
+        assert p.shape == (rotary.residues,)
+        _chk(lib.cm_rotary_set(self.h, rotary.h, p.ctypes.data, split, _stream()))
+
+    def rotary_apply(self, evk, rotary, xs, outs=None):
+        """xs (a list) with the positions that were set."""
+        outs = outs or [Ct(self, x.level - 1) for x in xs]
+        assert len(outs) == len(xs)
+        a, b = ((cm_ct * len(xs))(*[c.d for c in cts]) for cts in (xs, outs))
+        _chk(lib.cm_rotary_apply(self.h, evk.h, rotary.h, len(xs), a, b, _stream()))
+        for o, d in zip(outs, b):
+            o.d = d
+        return outs
+
+    def tree(self, kv, group=1, mask=-24.0, scale=0.0, coeffs=None):
+        return Tree(self, kv, group, mask, scale, coeffs)
+
+    def tree_qk(self, evk, tree, kv, parents, base, q, node0=0, first=0, outs=None):
+        """The score ciphertexts of the passes (pass delta at index delta)."""
+        p = _np(parents, np.int32)
+        outs = outs or [Ct(self, q.level - (2 if kv.key_index else 3)) for _ in range(tree.passes)]
+        assert len(outs) == tree.passes
+        arr = (cm_ct * len(outs))(*[o.d for o in outs])
+        _chk(lib.cm_tree_qk(self.h, evk.h, tree.h, kv.h, p.ctypes.data, p.size, base, node0, first, C.byref(q.d), arr, _stream()))
+        for o, d in zip(outs, arr):
+            o.d = d
+        return outs
+
+    def tree_sv(self, evk, tree, kv, scores, out=None):
+        assert len(scores) == tree.passes
+        out = out or Ct(self, scores[0].level - 2)
+        arr = (cm_ct * len(scores))(*[s.d for s in scores])
+        _chk(lib.cm_tree_sv(self.h, evk.h, tree.h, kv.h, arr, C.byref(out.d), _stream()))
+        return out
+
     def vmm_kv(self, evk, kv, which, x):
         out = Ct(self, x.level - (1 if which in (CM_SV, CM_SV_GROUP) or kv.key_index else 2))
         _chk(lib.cm_vmm_kv(self.h, evk.h, kv.h, which, C.byref(x.d), C.byref(out.d), _stream()))
@@ -568,6 +624,52 @@ class RelBias:
             self.h = None
 
 
+class Rotary:
+    """Tables of rotary positions (cm_rotary_*): positions 0 .. room - 1, the first rot_dims dims of a head (all of them), freq: angles a position of the
+    pairs (rotary_freqs)."""
+
+    def __init__(self, ctx, heads, dim, level, room, rot_dims, freq, gain, halves, coeffs):
+        self.ctx, self.h, self.level = ctx, _vp(), level
+        rot_dims = dim if rot_dims is None else rot_dims
+        f = _np(freq, np.float64) if freq is not None else None
+        c = _np(coeffs, np.int64) if coeffs is not None else None
+        assert f is None or f.shape == (rot_dims // 2,)
+        assert c is None or (c.ndim == 2 and c.shape[1] == ctx.n and len(c) >= lib.cm_rotary_polys(room))
+        _chk(lib.cm_rotary_create(ctx.h, heads, dim, level, rot_dims, f.ctypes.data if f is not None else None, gain, room,
+                                  CM_ROTARY_HALVES if halves else 0, c.ctypes.data if c is not None else None, C.byref(self.h)))
+        self.residues = ctx.S // ((1 << (heads - 1).bit_length()) * dim)
+
+    def steps(self):
+        out = np.empty(2, dtype=np.int32)
+        return out[: lib.cm_rotary_steps(self.h, out.ctypes.data, 2)].tolist()
+
+    def __del__(self):
+        if getattr(self, "h", None) and lib is not None:
+            lib.cm_rotary_destroy(self.h)
+            self.h = None
+
+
+class Tree:
+    """Attention of drafted tokens on caches of the shape and level of kv (cm_tree_*)."""
+
+    def __init__(self, ctx, kv, group, mask, scale, coeffs):
+        self.ctx, self.h = ctx, _vp()
+        c = _np(coeffs, np.int64) if coeffs is not None else None
+        _chk(lib.cm_tree_create(ctx.h, kv.h, group, mask, scale, c.ctypes.data if c is not None else None, C.byref(self.h)))
+        self.passes = lib.cm_tree_passes(self.h)
+
+    def steps(self):
+        n = lib.cm_tree_steps(self.h, None, 0)
+        out = np.empty(n, dtype=np.int32)
+        lib.cm_tree_steps(self.h, out.ctypes.data, n)
+        return out.tolist()
+
+    def __del__(self):
+        if getattr(self, "h", None) and lib is not None:
+            lib.cm_tree_destroy(self.h)
+            self.h = None
+
+
 class _KvHandle:
     """Owns a cache of the library: the last of its KvCache and the tensors over its memory destroys it."""
 
@@ -648,6 +750,17 @@ class KvCache:
 
     def append_group(self, evk, k_grp, v_grp):
         _chk(lib.cm_kv_append_group(self.ctx.h, evk.h, self.h, C.byref(k_grp.d), C.byref(v_grp.d), _stream()))
+
+    def append_run(self, evk, k, v, ntok, rotary=None):
+        """ntok tokens, that of place a at residue a mod t of k and v; rotary: with positions set, the keys take them."""
+        _chk(lib.cm_kv_append_run(self.ctx.h, evk.h, self.h, rotary.h if rotary is not None else None, ntok, C.byref(k.d), C.byref(v.d), _stream()))
+
+
+def rotary_freqs(rot_dims, base=10000.0, scaling=CM_ROTARY_PLAIN, par=()):
+    """Angles a position of the pairs, scaled for long contexts (cm_rotary_freqs)."""
+    out, p = np.empty(rot_dims // 2), _np(list(par) + [0.0] * 4, np.float64)
+    _chk(lib.cm_rotary_freqs(rot_dims, base, scaling, p.ctypes.data, out.ctypes.data))
+    return out
 
 
 def config1():

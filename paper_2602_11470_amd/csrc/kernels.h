@@ -25,6 +25,34 @@ __device__ __forceinline__ u64 redc_raw(u128 T, const ModC &m) {
     return redc((u128)redc(T, m.q, m.qinv) * m.r2, m.q, m.qinv);
 }
 
+// Where the two words of a_j for positions (i, i + 1) of limb mi come from.  Keys generated with both halves stored
+// carry a_j in multiplier form like b_j (word offset a_off inside the key): the kernels read it, one REDC per sum.
+// Otherwise it is regenerated from its stream (raw draws, two REDCs per sum).  Both give the same residues.
+struct EvkA {
+    size_t a_off;     // 0: regenerate
+    int kdig;         // digits of a full key: the stream keys start at kdig * nmod * n
+};
+template <bool SA>
+__device__ __forceinline__ ulonglong2 evk_a_words(const u64 *__restrict__ key, const EvkA ea, int nmod, int n, int j, int mi,
+                                                  unsigned i, u64 cg0, u64 cg1, u64 bound) {
+    ulonglong2 r;
+    if (SA) {
+        const u64 *ka = key + ea.a_off + ((size_t)j * nmod + mi) * n + i;
+        r.x = __builtin_nontemporal_load(ka), r.y = __builtin_nontemporal_load(ka + 1);
+    } else {
+        const u64 sk_ = key[(size_t)ea.kdig * nmod * n + (size_t)j * nmod + mi];
+        r.x = evk_a_draw(sk_, cg0, i, bound), r.y = evk_a_draw(sk_, cg1, i + 1, bound);
+    }
+    return r;
+}
+template <bool SA>
+__device__ __forceinline__ u64 evk_a_reduce(u128 T, const ModC &m) {
+    return SA ? redc(T, m.q, m.qinv) : redc_raw(T, m);
+}
+inline EvkA evk_a_of(const cm_ctx *ctx) {
+    return EvkA{ctx->evk_stored_a ? evk_a_offset(ctx) : 0, (ctx->L + ctx->alpha) / ctx->alpha};
+}
+
 void launch_set_idx(int *d_dst, const int *h_src, int count, hipStream_t st);
 void launch_reduce_i64(cm_ctx *ctx, u64 *out, const long long *d_coeffs, const int *d_mod_idx, int limbs, hipStream_t st);
 void launch_to_mont(cm_ctx *ctx, u64 *data, const int *d_mod_idx, int limbs, hipStream_t st);
@@ -127,6 +155,22 @@ struct IpFan {
 };
 bool launch_inner_product_fanout(cm_ctx *ctx, const IpFan &f, const u64 *dig, const u64 *c0, bool c0_ext, int beta, int level,
                                  hipStream_t st);
+// Rotations that share their digits, times plaintexts, on the extended basis (rotary.hip): output z < nz (out[z] = [2][ext][n]) is
+// extra[z] (nullable, may be out[z] itself) + here[z] P c_here[z] (here nullable) + the sum of items z*nsum .. z*nsum + nsum - 1, each
+// pt ((sum_j perm_g(dig_j) key_j) + (P perm_g(c's first component), 0)); plaintexts [ext][n] in multiplier form, c [2][level+1][n].
+#define WR_ITEMS 32
+#define WR_OUTS CM_KS_BATCH
+struct WrItem {
+    const u64 *dig = nullptr, *c = nullptr, *key = nullptr, *pt = nullptr;
+    unsigned g = 0;
+};
+struct WrBatch {
+    int nz = 0, nsum = 1;
+    WrItem it[WR_ITEMS];
+    const u64 *here[WR_OUTS] = {}, *c_here[WR_OUTS] = {}, *extra[WR_OUTS] = {};
+    u64 *out[WR_OUTS] = {};
+};
+void launch_weighted(cm_ctx *ctx, const WrBatch &b, int beta, int level, hipStream_t st);
 #define IP_MULTI_KEYS 3
 struct IpKeys {
     const u64 *key[IP_MULTI_KEYS] = {};
@@ -294,10 +338,10 @@ size_t arena_digits_words(const cm_ctx *ctx);
 // us + r*2*ext'*n, ext' = level + 1 + sets*K, whose special limbs of s = 0 .. sets-1 follow each other and whose ciphertext limbs
 // are summed over s; add_r = add + r*add_stride (on the first add_comps components), acc_r = acc + r*acc_stride ([2][level+1][n],
 // nullable).  One forward transform per output limb instead of two, and four launches fewer than one after the other.  Rows
-// level .. of us are overwritten.  ks_drop_fits: whether the kernels cover this level and count (otherwise: two steps).
+// level .. of us are overwritten.  outs: the results' places, where they do not follow each other.  ks_drop_fits: whether the kernels cover this level and count (otherwise: two steps).
 bool ks_drop_fits(cm_ctx *ctx, int level, int sets, int m);
 cm_status ks_drop(cm_ctx *ctx, u64 *us, int level, int sets, int m, const u64 *add, size_t add_stride, int add_comps, u64 g,
-                  const u64 *acc, size_t acc_stride, u64 *out, hipStream_t st, bool rows_done = false);
+                  const u64 *acc, size_t acc_stride, u64 *out, hipStream_t st, bool rows_done = false, u64 *const *outs = nullptr);
 // what joins row `level` of a ks_drop (launch_rows_ip does it where it does the inverse row pass: inv_from = level)
 FoldIn ks_drop_fold(cm_ctx *ctx, int level, int sets, const u64 *add, size_t add_stride, int add_comps, u64 g, const u64 *acc, size_t acc_stride);
 // out[2][level][n] = rescale(ModDown(u[2][ext][n])), in one where ks_drop_fits, through tmp[2][level+1][n] otherwise

@@ -468,33 +468,6 @@ void launch_automorphism(cm_ctx *ctx, u64 *out, const u64 *in, int rows, u64 g, 
 // rotations).  Two adjacent coefficients per lane (16-byte accesses); the permutation keeps
 // aligned pairs together (it maps i^1 to src^1).
 // `extra` may be the output itself (a running sum): every lane reads its own words before it writes them.
-// Where the two words of a_j for positions (i, i + 1) of limb mi come from.  Keys generated with both halves stored
-// carry a_j in multiplier form like b_j (word offset a_off inside the key): the kernels read it, one REDC per sum.
-// Otherwise it is regenerated from its stream (raw draws, two REDCs per sum).  Both give the same residues.
-struct EvkA {
-    size_t a_off;     // 0: regenerate
-    int kdig;         // digits of a full key: the stream keys start at kdig * nmod * n
-};
-template <bool SA>
-__device__ __forceinline__ ulonglong2 evk_a_words(const u64 *__restrict__ key, const EvkA ea, int nmod, int n, int j, int mi,
-                                                  unsigned i, u64 cg0, u64 cg1, u64 bound) {
-    ulonglong2 r;
-    if (SA) {
-        const u64 *ka = key + ea.a_off + ((size_t)j * nmod + mi) * n + i;
-        r.x = __builtin_nontemporal_load(ka), r.y = __builtin_nontemporal_load(ka + 1);
-    } else {
-        const u64 sk_ = key[(size_t)ea.kdig * nmod * n + (size_t)j * nmod + mi];
-        r.x = evk_a_draw(sk_, cg0, i, bound), r.y = evk_a_draw(sk_, cg1, i + 1, bound);
-    }
-    return r;
-}
-template <bool SA>
-__device__ __forceinline__ u64 evk_a_reduce(u128 T, const ModC &m) {
-    return SA ? redc(T, m.q, m.qinv) : redc_raw(T, m);
-}
-static EvkA evk_a_of(const cm_ctx *ctx) {
-    return EvkA{ctx->evk_stored_a ? evk_a_offset(ctx) : 0, (ctx->L + ctx->alpha) / ctx->alpha};
-}
 template <bool SA>
 __global__ __launch_bounds__(TPB) void k_inner_product(u64 *u0, u64 *u1,
                                                        const u64 *__restrict__ dig, const u64 *__restrict__ evk,

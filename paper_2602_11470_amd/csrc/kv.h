@@ -53,3 +53,12 @@ inline u64 rot_g(const cm_kv *kv, long long step) {
     long long S = kv->S;
     return galois_of_step(kv->ctx, (int)(((step % S) + S) % S));
 }
+// the products of a cache (kv.hip) that others build on; sums: the tensor sums of all r_o <= CM_KS_BATCH groups, where they are formed already
+cm_status kv_qk_keys(const cm_evk *evk, const cm_kv *kv, bool replicate);
+cm_status kv_qk(cm_ctx *ctx, const cm_evk *evk, const cm_kv *kv, const cm_ct *in, cm_ct *out, hipStream_t st, bool replicate);
+cm_status kv_sv_keys(const cm_evk *evk, const cm_kv *kv, bool reduce, bool replicate);
+cm_status kv_sv_babies(cm_ctx *ctx, const cm_evk *evk, const cm_kv *kv, const cm_ct *in, u64 *babies, u64 *tmp, hipStream_t st, bool replicate);
+cm_status kv_sv(cm_ctx *ctx, const cm_evk *evk, const cm_kv *kv, const cm_ct *in, cm_ct *out, hipStream_t st, bool reduce, const u64 *array,
+                bool replicate, const u64 *sums = nullptr);
+// entries[m - 1][limbs][n], m = 1 .. E - 1: the sum of `row` (a plaintext of row 0, B slots) turned right by m .. E - 1 rows (relbias.hip)
+cm_status rows_from_on(cm_ctx *ctx, u64 *entries, const u64 *row, int B, int E, int limbs);

@@ -11,9 +11,11 @@
 // scale of the prime the following rescale removes, so masking leaves the scale unchanged.
 #include <math.h>
 
+#include <algorithm>
 #include <utility>
 
 #include "kv.h"
+#include "rotary.h"
 
 // ceil(L/3) runs of as equal length as possible, the longer ones first; a run lists its non-empty subset sums
 static std::vector<std::vector<long long>> ladder_groups(const std::vector<long long> &steps) {
@@ -288,19 +290,11 @@ extern "C" cm_status cm_kv_export(cm_ctx *ctx, const cm_kv *kv, int32_t which, i
     return cm_ct_export(ctx, &ct, out);
 }
 
-// One token (k_new / v_new hold it at residue ntok mod t), or, group = true, the t tokens of the
-// next K ciphertext at once (Sec. 5.4: token c*t + tau at residue tau, which is already the layout
-// of K ciphertext c; the V masks take whole block rows, all residues together).
-static cm_status kv_append(cm_ctx *ctx, const cm_evk *evk, cm_kv *kv, const cm_ct *k_new, const cm_ct *v_new,
-                           bool group, void *stream) {
-    (void)hipGetLastError();          // stale errors of earlier calls are not this call's
-    if (!ctx || !evk || !kv || kv->ctx != ctx || !k_new || !v_new || !k_new->dev || !v_new->dev || !evk_fits(ctx, evk)) return CM_E_INVAL;
-    if (k_new->ncomp != 2 || v_new->ncomp != 2) return CM_E_INVAL;
-    CM_TRY
+// What an append asks for apart from its key's ciphertext: `room` more tokens at the place of the next append, v and the rotation keys
+static cm_status kv_append_checks(cm_ctx *ctx, const cm_evk *evk, const cm_kv *kv, const cm_ct *k_new, const cm_ct *v_new, int room) {
     const int lv = kv->level + 1;
-    if (lv > ctx->L || k_new->level != lv || v_new->level != lv) return CM_E_LEVEL;
-    if (kv->pos >= kv->max_tokens) return CM_E_LAYOUT;
-    if (group && (kv->pos % kv->t || kv->pos + kv->t > kv->max_tokens)) return CM_E_LAYOUT;
+    if (lv > ctx->L || v_new->level != lv) return CM_E_LEVEL;
+    if (kv->pos >= kv->max_tokens || kv->pos + room > kv->max_tokens) return CM_E_LAYOUT;
     if (kv->scale_set && (fabs(k_new->scale / kv->scale - 1) > 1e-9 || fabs(v_new->scale / kv->scale - 1) > 1e-9))
         return CM_E_SCALE;
     if (fabs(k_new->scale / v_new->scale - 1) > 1e-9) return CM_E_SCALE;
@@ -308,18 +302,18 @@ static cm_status kv_append(cm_ctx *ctx, const cm_evk *evk, cm_kv *kv, const cm_c
         if (!find_key(evk, rot_g(kv, -(long long)g * kv->r_i * kv->H * kv->t))) return CM_E_NOKEY;
     for (int j = 1; j < kv->r_i && kv->indexed; j++)
         if (!find_key(evk, rot_g(kv, (long long)j * kv->H * kv->t))) return CM_E_NOKEY;
-    hipStream_t st = (hipStream_t)stream;
+    return CM_OK;
+}
+// The value and index part of an append to page c: vmask holds the slots (0, h, tau) of the new tokens (page c in row 0, the next one in row 1),
+// turned right by tau slots more; k_new, v_new [2][level+2][n]; shifted: room for the shifted inputs and what follows in the work area
+static cm_status kv_put(cm_ctx *ctx, const cm_evk *evk, cm_kv *kv, const u64 *k_new, const u64 *v_new, const u64 *vmask, int c, int tau, u64 *shifted,
+                        hipStream_t st) {
+    const int lv = kv->level + 1;
     const size_t n = ctx->n, ctw_up = 2 * (size_t)(lv + 1) * n, ctw = kv_ctw(kv);
-    const int tok = kv->pos, c = tok / kv->t, tau = tok % kv->t;
-    u64 *mask = kv->d_work, *prod = mask + (size_t)(lv + 1) * n, *res = prod + ctw_up, *shifted = res + ctw_up;
-    // K: K_c += rescale(k_new * mask_tau), mask_tau = residue-0 mask rotated right by tau (a group: all ones)
-    if (!group) launch_automorphism(ctx, mask, kv->d_mask_k, lv + 1, rot_g(kv, -tau), st);
-    launch_mul_pt(ctx, prod, k_new->dev, group ? kv->d_mask_kg : mask, 2, lv + 1, st);
-    CMCHK(rescale_into(ctx, prod, 2, lv, kv->d_k + (size_t)c * ctw, st, nullptr, nullptr, true));
     // V: the new vector shifted right by each giant step, then one masked product per V ciphertext
     if (kv->r_o > 1) {                                       // rotations of one ciphertext: one raise for all of them
         u64 *digits = arena_digits(ctx);
-        CMCHK(ks_raise(ctx, v_new->dev + (size_t)(lv + 1) * n, lv, digits, st));
+        CMCHK(ks_raise(ctx, v_new + (size_t)(lv + 1) * n, lv, digits, st));
         std::vector<const u64 *> keys;
         std::vector<u64> gs;
         std::vector<u64 *> dst;
@@ -327,12 +321,11 @@ static cm_status kv_append(cm_ctx *ctx, const cm_evk *evk, cm_kv *kv, const cm_c
             const u64 gal = rot_g(kv, -(long long)g * kv->r_i * kv->H * kv->t);
             keys.push_back(find_key(evk, gal)), gs.push_back(gal), dst.push_back(shifted + (size_t)(g - 1) * ctw_up);
         }
-        CMCHK(ks_apply_many(ctx, digits, lv, kv->r_o - 1, keys.data(), gs.data(), v_new->dev, dst.data(), st));
+        CMCHK(ks_apply_many(ctx, digits, lv, kv->r_o - 1, keys.data(), gs.data(), v_new, dst.data(), st));
     }
     // dst[k] += rescale(mask through the Galois map g(k) * src(k)) for the E ciphertexts of dst (contiguous: the rescale adds
     // its result onto a run of them), as many per launch as the work area has room for, or, where the rescale does not
     // form the products itself, CM_KS_BATCH in two steps
-    const u64 *vmask = group ? kv->d_mask_vg : kv->d_mask_v;
     auto add_masked = [&](u64 *dst, u64 *work, auto src, auto g) -> cm_status {
         const int fused = rescale_masked_batch(ctx, lv, kv->d_work + kv->work_words - work), B = fused ? fused : CM_KS_BATCH;
         u64 *last = work, *red = last + (size_t)B * 2 * n, *prods = red + (size_t)B * 2 * lv * n;
@@ -348,7 +341,7 @@ static cm_status kv_append(cm_ctx *ctx, const cm_evk *evk, cm_kv *kv, const cm_c
         return CM_OK;
     };
     CMCHK(add_masked(kv->d_v, shifted + (size_t)(kv->r_o > 1 ? kv->r_o - 1 : 0) * ctw_up,
-                     [&](int k) { return k < kv->r_i ? v_new->dev : shifted + (size_t)(k / kv->r_i - 1) * ctw_up; },
+                     [&](int k) { return k < kv->r_i ? v_new : shifted + (size_t)(k / kv->r_i - 1) * ctw_up; },
                      [&](int k) {
                          return rot_g(kv, -((long long)(((c - k) % kv->E + kv->E) % kv->E) * kv->H * kv->t + tau +
                                             (long long)(k / kv->r_i) * kv->r_i * kv->H * kv->t));
@@ -358,7 +351,7 @@ static cm_status kv_append(cm_ctx *ctx, const cm_evk *evk, cm_kv *kv, const cm_c
         // whole copy); the baby rotations of the new key are hoisted
         if (kv->r_i > 1) {
             u64 *digits = arena_digits(ctx);
-            CMCHK(ks_raise(ctx, k_new->dev + (size_t)(lv + 1) * n, lv, digits, st));
+            CMCHK(ks_raise(ctx, k_new + (size_t)(lv + 1) * n, lv, digits, st));
             std::vector<const u64 *> keys;
             std::vector<u64> gs;
             std::vector<u64 *> dst;
@@ -366,13 +359,37 @@ static cm_status kv_append(cm_ctx *ctx, const cm_evk *evk, cm_kv *kv, const cm_c
                 const u64 gal = rot_g(kv, (long long)j * kv->H * kv->t);
                 keys.push_back(find_key(evk, gal)), gs.push_back(gal), dst.push_back(shifted + (size_t)(j - 1) * ctw_up);
             }
-            CMCHK(ks_apply_many(ctx, digits, lv, kv->r_i - 1, keys.data(), gs.data(), k_new->dev, dst.data(), st));
+            CMCHK(ks_apply_many(ctx, digits, lv, kv->r_i - 1, keys.data(), gs.data(), k_new, dst.data(), st));
         }
         // place j r_o + g holds index ciphertext g r_i + j
         CMCHK(add_masked(kv->d_x, shifted + (size_t)(kv->r_i > 1 ? kv->r_i - 1 : 0) * ctw_up,
-                         [&](int k) { return k < kv->r_o ? k_new->dev : shifted + (size_t)(k / kv->r_o - 1) * ctw_up; },
+                         [&](int k) { return k < kv->r_o ? k_new : shifted + (size_t)(k / kv->r_o - 1) * ctw_up; },
                          [&](int k) { return rot_g(kv, -((long long)((c + k % kv->r_o * kv->r_i) % kv->E) * kv->H * kv->t + tau)); }));
     }
+    return CM_OK;
+}
+// One token (k_new / v_new hold it at residue ntok mod t), or, group = true, the t tokens of the
+// next K ciphertext at once (Sec. 5.4: token c*t + tau at residue tau, which is already the layout
+// of K ciphertext c; the V masks take whole block rows, all residues together).
+static cm_status kv_append(cm_ctx *ctx, const cm_evk *evk, cm_kv *kv, const cm_ct *k_new, const cm_ct *v_new,
+                           bool group, void *stream) {
+    (void)hipGetLastError();          // stale errors of earlier calls are not this call's
+    if (!ctx || !evk || !kv || kv->ctx != ctx || !k_new || !v_new || !k_new->dev || !v_new->dev || !evk_fits(ctx, evk)) return CM_E_INVAL;
+    if (k_new->ncomp != 2 || v_new->ncomp != 2) return CM_E_INVAL;
+    CM_TRY
+    const int lv = kv->level + 1;
+    if (k_new->level != lv) return CM_E_LEVEL;
+    if (group && kv->pos % kv->t) return CM_E_LAYOUT;
+    CMCHK(kv_append_checks(ctx, evk, kv, k_new, v_new, group ? kv->t : 1));
+    hipStream_t st = (hipStream_t)stream;
+    const size_t n = ctx->n, ctw_up = 2 * (size_t)(lv + 1) * n, ctw = kv_ctw(kv);
+    const int tok = kv->pos, c = tok / kv->t, tau = tok % kv->t;
+    u64 *mask = kv->d_work, *prod = mask + (size_t)(lv + 1) * n, *res = prod + ctw_up, *shifted = res + ctw_up;
+    // K: K_c += rescale(k_new * mask_tau), mask_tau = residue-0 mask rotated right by tau (a group: all ones)
+    if (!group) launch_automorphism(ctx, mask, kv->d_mask_k, lv + 1, rot_g(kv, -tau), st);
+    launch_mul_pt(ctx, prod, k_new->dev, group ? kv->d_mask_kg : mask, 2, lv + 1, st);
+    CMCHK(rescale_into(ctx, prod, 2, lv, kv->d_k + (size_t)c * ctw, st, nullptr, nullptr, true));
+    CMCHK(kv_put(ctx, evk, kv, k_new->dev, v_new->dev, group ? kv->d_mask_vg : kv->d_mask_v, c, tau, shifted, st));
     kv->pos += group ? kv->t : 1;
     if (kv->ntok < kv->pos) kv->ntok = kv->pos;
     kv->scale = k_new->scale * (double)ctx->mod[lv] / (double)ctx->mod[lv];
@@ -389,8 +406,89 @@ extern "C" cm_status cm_kv_append_group(cm_ctx *ctx, const cm_evk *evk, cm_kv *k
     return kv_append(ctx, evk, kv, k_grp, v_grp, true, stream);
 }
 
+
+// out = the sum of a mask's turns: entry k through the Galois map g[k]
+#define RUN_TURNS 64
+struct MaskTurns {
+    unsigned g[RUN_TURNS];
+};
+__global__ __launch_bounds__(256) void k_mask_turns(u64 *out, const u64 *__restrict__ mask, MaskTurns t, int count, const ModC *__restrict__ modc, int n,
+                                                    int logn, int accumulate) {
+    const unsigned i = blockIdx.x * 256 + threadIdx.x;
+    const size_t row = (size_t)blockIdx.y * n;
+    const u64 q = modc[blockIdx.y].q;
+    u64 v = accumulate ? out[row + i] : 0;
+    for (int k = 0; k < count; k++) v = addmod(v, mask[row + perm_src(i, t.g[k], logn)], q);
+    out[row + i] = v;
+}
+static void launch_mask_turns(cm_ctx *ctx, u64 *out, const u64 *mask, const std::vector<u64> &gs, int limbs, hipStream_t st) {
+    for (size_t k0 = 0; k0 < gs.size(); k0 += RUN_TURNS) {
+        MaskTurns t;
+        const int m = (int)std::min<size_t>(RUN_TURNS, gs.size() - k0);
+        for (int k = 0; k < RUN_TURNS; k++) t.g[k] = k < m ? (unsigned)gs[k0 + k] : 1;
+        Prof prof_(ctx, CM_K_ELEMENTWISE, limbs, st);
+        hipLaunchKernelGGL(k_mask_turns, dim3(ctx->n / 256, limbs), dim3(256), 0, st, out, mask, t, m, ctx->d_modc, ctx->n, ctx->logn, k0 > 0);
+    }
+}
+// A run of tokens from the place of the next append on.  Its masks are sums of turns of the masks that single appends use: of one residue for the
+// page it begins in and the next one (K), of one slot row (V and the index, where a run that passes into the next page has two rows).
+// With rotary positions the K ciphertexts take the rotated key as it leaves its ModDown and rescale: the plaintexts of the rotation hold nothing at other
+// residues, so they are the mask, and the key needs no level for it.  The index masks rotations of the rotated key: there it is formed first, a level above.
+extern "C" cm_status cm_kv_append_run(cm_ctx *ctx, const cm_evk *evk, cm_kv *kv, const cm_rotary *rotary, int32_t ntok, const cm_ct *k_new, const cm_ct *v_new,
+                                      void *stream) {
+    (void)hipGetLastError();          // stale errors of earlier calls are not this call's
+    if (!ctx || !evk || !kv || kv->ctx != ctx || !k_new || !v_new || !k_new->dev || !v_new->dev || (rotary && rotary->ctx != ctx) || !evk_fits(ctx, evk)) return CM_E_INVAL;
+    if (k_new->ncomp != 2 || v_new->ncomp != 2) return CM_E_INVAL;
+    CM_TRY
+    const int lv = kv->level + 1, t = kv->t, lk = rotary && kv->indexed ? lv + 1 : lv;
+    if (lk > ctx->L || k_new->level != lk || (rotary && rotary->level != lk)) return CM_E_LEVEL;
+    if (ntok < 1 || ntok > t) return CM_E_LAYOUT;
+    const int c = kv->pos / t, begin = kv->pos % t, end = begin + ntok, pages = end > t ? 2 : 1;
+    if (rotary) {
+        if (rotary->H != kv->H || rotary->E != kv->E || !rotary->set || rotary->split != (pages > 1 ? end - t : 0)) return CM_E_LAYOUT;
+        for (int r = 0; r < t; r++) if ((rotary->pos[r] >= 0) != ((r >= begin && r < end) || r + t < end)) return CM_E_LAYOUT;
+        for (int s = 0; s < rotary->parts - 1; s++) if (!find_key(evk, galois_of_step(ctx, s ? -rotary->step : rotary->step))) return CM_E_NOKEY;
+    }
+    CMCHK(kv_append_checks(ctx, evk, kv, k_new, v_new, ntok));
+    hipStream_t st = (hipStream_t)stream;
+    const size_t n = ctx->n, ctw_up = 2 * (size_t)(lv + 1) * n, ctw = kv_ctw(kv);
+    u64 *vmask = kv->d_work, *prod = vmask + (size_t)(lv + 1) * n, *res = prod + ctw_up, *shifted = res + ctw_up, *us = arena_batch_sums(ctx);
+    std::vector<u64> rows, residues[2];
+    for (int i = begin; i < end; i++) {
+        rows.push_back(rot_g(kv, -((long long)(i / t) * kv->H * t + i % t)));
+        residues[i / t].push_back(rot_g(kv, -(i % t)));
+    }
+    const u64 *k_src = k_new->dev;
+    if (rotary && !kv->indexed) {
+        const u64 *x = k_new->dev;
+        u64 *outs[2] = {prod, res};
+        CMCHK(rotary_sums(ctx, evk, rotary, 1, &x, pages > 1 ? 1 : 0, pages, us, st));
+        CMCHK(weighted_down(ctx, us, lk, pages, outs, rotary->d_work, st));
+        for (int p = 0; p < pages; p++) launch_add(ctx, kv->d_k + (size_t)(c + p) * ctw, kv->d_k + (size_t)(c + p) * ctw, outs[p], 2, lv, st);
+    } else {
+        if (rotary) {
+            u64 *turned = rotary->d_work + 2 * (size_t)(lk + 1) * n;              // the raise is done with what it held there
+            CMCHK(rotary_sums(ctx, evk, rotary, 1, &k_src, 0, 1, us, st));
+            CMCHK(weighted_down(ctx, us, lk, 1, &turned, rotary->d_work, st));
+            k_src = turned;
+        }
+        for (int p = 0; p < pages; p++) {
+            launch_mask_turns(ctx, res, kv->d_mask_k, residues[p], lv + 1, st);
+            launch_mul_pt(ctx, prod, k_src, res, 2, lv + 1, st);
+            CMCHK(rescale_into(ctx, prod, 2, lv, kv->d_k + (size_t)(c + p) * ctw, st, nullptr, nullptr, true));
+        }
+    }
+    launch_mask_turns(ctx, vmask, kv->d_mask_v, rows, lv + 1, st);
+    CMCHK(kv_put(ctx, evk, kv, k_src, v_new->dev, vmask, c, 0, shifted, st));
+    kv->pos += ntok;
+    if (kv->ntok < kv->pos) kv->ntok = kv->pos;
+    kv->scale = k_new->scale, kv->scale_set = true;
+    RETURN_LAUNCH_STATUS();
+    CM_CATCH
+}
+
 // every key query-times-K needs is there (checked before anything is enqueued)
-static cm_status kv_qk_keys(const cm_evk *evk, const cm_kv *kv, bool replicate) {
+cm_status kv_qk_keys(const cm_evk *evk, const cm_kv *kv, bool replicate) {
     if (kv->level < 2) return CM_E_LEVEL;
     if (!find_key(evk, 0)) return CM_E_NOKEY;
     for (int i = 0; i < ilog2(kv->t) && replicate; i++) if (!find_key(evk, rot_g(kv, -(1 << i)))) return CM_E_NOKEY;
@@ -403,7 +501,7 @@ static cm_status kv_qk_keys(const cm_evk *evk, const cm_kv *kv, bool replicate) 
     }
     return (kv->ntok + kv->t - 1) / kv->t < 1 ? CM_E_LAYOUT : CM_OK;
 }
-static cm_status kv_qk(cm_ctx *ctx, const cm_evk *evk, const cm_kv *kv, const cm_ct *in, cm_ct *out, hipStream_t st,
+cm_status kv_qk(cm_ctx *ctx, const cm_evk *evk, const cm_kv *kv, const cm_ct *in, cm_ct *out, hipStream_t st,
                        bool replicate) {
     const int lv = kv->level, limbs = lv + 1;
     CMCHK(kv_qk_keys(evk, kv, replicate));
@@ -553,7 +651,7 @@ static cm_status kv_qk(cm_ctx *ctx, const cm_evk *evk, const cm_kv *kv, const cm
 
 // array = the value ciphertexts, or the key index with the query in the place of the scores (replicate: the query is
 // first copied to all residues, as query-times-K does)
-static cm_status kv_sv_keys(const cm_evk *evk, const cm_kv *kv, bool reduce, bool replicate) {
+cm_status kv_sv_keys(const cm_evk *evk, const cm_kv *kv, bool reduce, bool replicate) {
     for (int i = 0; i < ilog2(kv->t) && replicate; i++) if (!find_key(evk, rot_g(kv, -(1 << i)))) return CM_E_NOKEY;
     if (!find_key(evk, 0)) return CM_E_NOKEY;
     const long long Ht = (long long)kv->H * kv->t;
@@ -569,7 +667,7 @@ static cm_status kv_sv_keys(const cm_evk *evk, const cm_kv *kv, bool reduce, boo
     return CM_OK;
 }
 // the baby steps of in; tmp: a ciphertext
-static cm_status kv_sv_babies(cm_ctx *ctx, const cm_evk *evk, const cm_kv *kv, const cm_ct *in, u64 *babies, u64 *tmp, hipStream_t st, bool replicate) {
+cm_status kv_sv_babies(cm_ctx *ctx, const cm_evk *evk, const cm_kv *kv, const cm_ct *in, u64 *babies, u64 *tmp, hipStream_t st, bool replicate) {
     const int lv = kv->level;
     const size_t ctw = kv_ctw(kv), ln = (size_t)(lv + 1) * ctx->n;
     const long long Ht = (long long)kv->H * kv->t;
@@ -599,8 +697,8 @@ static cm_status kv_sv_babies(cm_ctx *ctx, const cm_evk *evk, const cm_kv *kv, c
     return CM_OK;
 }
 // sums: the tensor sums of all r_o <= CM_KS_BATCH groups, where they are formed already (in is then its scale alone)
-static cm_status kv_sv(cm_ctx *ctx, const cm_evk *evk, const cm_kv *kv, const cm_ct *in, cm_ct *out, hipStream_t st,
-                       bool reduce, const u64 *array, bool replicate, const u64 *sums = nullptr) {
+cm_status kv_sv(cm_ctx *ctx, const cm_evk *evk, const cm_kv *kv, const cm_ct *in, cm_ct *out, hipStream_t st,
+                       bool reduce, const u64 *array, bool replicate, const u64 *sums) {
     const int lv = kv->level, limbs = lv + 1;
     CMCHK(kv_sv_keys(evk, kv, reduce, replicate));
     const size_t n = ctx->n, ctw = kv_ctw(kv), ln = (size_t)limbs * n;

@@ -439,7 +439,7 @@ FoldIn ks_drop_fold(cm_ctx *ctx, int level, int sets, const u64 *add, size_t add
     return fi;
 }
 cm_status ks_drop(cm_ctx *ctx, u64 *us, int level, int sets, int m, const u64 *add, size_t add_stride, int add_comps, u64 g,
-                  const u64 *acc, size_t acc_stride, u64 *out, hipStream_t st, bool rows_done) {
+                  const u64 *acc, size_t acc_stride, u64 *out, hipStream_t st, bool rows_done, u64 *const *outs) {
     if (!ks_drop_fits(ctx, level, sets, m)) return CM_E_INVAL;
     const KsLevelFull &k = ks_level_full(ctx, level);
     Arena A = arena_of(ctx);
@@ -453,7 +453,7 @@ cm_status ks_drop(cm_ctx *ctx, u64 *us, int level, int sets, int m, const u64 *a
     fb.items = m, fb.level = level - 1, fb.ext = ext, fb.addend_comps = add ? add_comps : 0, fb.in_rows = level + 1;
     for (int r = 0; r < CM_MASK_BATCH; r++) fb.addend[r] = nullptr, fb.accum[r] = nullptr, fb.u[r] = nullptr, fb.out[r] = nullptr, fb.g[r] = 0;
     for (int r = 0; r < m; r++) {
-        fb.u[r] = us + (size_t)r * 2 * ext * n, fb.out[r] = out + (size_t)r * 2 * level * n, fb.g[r] = (unsigned)g;
+        fb.u[r] = us + (size_t)r * 2 * ext * n, fb.out[r] = outs ? outs[r] : out + (size_t)r * 2 * level * n, fb.g[r] = (unsigned)g;
         fb.addend[r] = add ? add + r * add_stride : nullptr, fb.accum[r] = acc ? acc + r * acc_stride : nullptr;
     }
     fb.pinv = k.d_pqinv, fb.ainv = get_qlinv(ctx, level);

@@ -72,6 +72,18 @@ __global__ __launch_bounds__(256) void k_relbias(BiasBatch b, const u64 *row, un
     if (out != in) store(c1, out + at + cs);
 }
 
+cm_status rows_from_on(cm_ctx *ctx, u64 *entries, const u64 *row, int B, int E, int limbs) {
+    const int n = ctx->n;
+    const size_t words = (size_t)limbs * n;
+    // E - 1 pages visible: the row turned right by E - 1; i pages: those of i + 1 and the row turned right by i
+    for (int i = E - 1; i > 0; i--) {
+        const u64 g = galois_of_step(ctx, (int)(((long long)n / 2 - (long long)i * B) % (n / 2)));
+        u64 *entry = entries + (i - 1) * words;
+        if (i == E - 1) launch_automorphism(ctx, entry, row, limbs, g, 0);
+        else hipLaunchKernelGGL(k_add_turned, dim3(n / 256, limbs), dim3(256), 0, 0, entry, entry + words, row, ctx->d_modc, (unsigned)g, n, ctx->logn);
+    }
+    return CM_OK;
+}
 extern "C" void cm_relbias_destroy(cm_relbias *rb) {
     if (!rb) return;
     hipFree(rb->d_pts), hipFree(rb->d_unseen);
@@ -141,14 +153,7 @@ extern "C" cm_status cm_relbias_create_ex(cm_ctx *ctx, int32_t heads, int32_t di
             for (int i = 0; i < S; i++) m[i] = i < H * t_kv ? mask : 0.0;
             status = encode(row, m, polys);
             if (status == CM_OK) {
-                // E - 1 pages visible: the row turned right by E - 1; i pages: those of i + 1 and the row turned right by i
-                for (int i = dim - 1; i > 0; i--) {
-                    const u64 g = galois_of_step(ctx, (int)(((long long)S - (long long)i * H * t_kv) % S));
-                    u64 *entry = rb->d_unseen + (i - 1) * words;
-                    if (i == dim - 1) launch_automorphism(ctx, entry, row, level + 1, g, 0);
-                    else hipLaunchKernelGGL(k_add_turned, dim3(n / 256, level + 1), dim3(256), 0, 0, entry, entry + words, row, ctx->d_modc, (unsigned)g, n,
-                                            ctx->logn);
-                }
+                rows_from_on(ctx, rb->d_unseen, row, H * t_kv, dim, level + 1);
                 if (hipDeviceSynchronize() != hipSuccess || hipGetLastError() != hipSuccess) status = CM_E_HIP;
             }
         }
