@@ -524,3 +524,67 @@ class GqaLayout:
         for back in range(1, self.G):
             s += self.kv.inner_rotation_steps(self.inner_delta(back))
         return s + [1 << l for l in range(_log2(self.t))]
+
+
+class RotaryTables:
+    """Rotary positions by tables: position = low * (high part) + low part, low the power of two at or above sqrt(room).  The first `rot` dims of a
+    head turn, pairs of neighbours or (halves) of its two halves, pair m by freq[m] a position, cosines and sines times gain."""
+
+    def __init__(self, S, heads, dim, room, rot=None, freq=None, gain=1.0, halves=False):
+        self.lay, self.rot, self.gain, self.halves, self.room = KvLayout(S, heads, dim), dim if rot is None else rot, gain, halves, room
+        self.freq = np.asarray(freq if freq is not None else [10000.0 ** (-2.0 * m / self.rot) for m in range(self.rot // 2)])
+        self.low = 1
+        while self.low * self.low < room:
+            self.low *= 2
+        self.high = -(-room // self.low)
+        self.step = (self.rot // 2 if halves else 1) * self.lay.H * self.lay.t
+
+    def pair(self, e):
+        """(pair, first or second dim of it) of dim e; None where it does not turn."""
+        if e >= self.rot:
+            return None
+        return (e % (self.rot // 2), e // (self.rot // 2)) if self.halves else (e // 2, e % 2)
+
+    def _rows(self, value, everywhere):
+        out = np.zeros((self.lay.E, self.lay.H, self.lay.t))
+        for e in range(self.lay.E):
+            out[e, :, slice(None) if everywhere else slice(0, 1)] = value(e)
+        return out.reshape(-1)
+
+    def slots(self):
+        """Slot vectors of the tables, in the order of cm_rotary_create's coefficients."""
+        out = []
+        for i in range(self.low):
+            for f in (np.cos, np.sin):
+                for side in (0, 1):
+                    out.append(self._rows(lambda e: self.gain * f(i * self.freq[self.pair(e)[0]]) if self.pair(e) and self.pair(e)[1] == side else 0.0, False))
+        out.append(self._rows(lambda e: 0.0 if self.pair(e) else 1.0, False))
+        for h in range(self.high):
+            for f in (np.cos, np.sin):
+                out.append(self._rows(lambda e: f(h * self.low * self.freq[self.pair(e)[0]]) if self.pair(e) else f(0.0), True))
+        return out
+
+    def turn(self, v, p):
+        """v[h, e] at position p."""
+        out = np.array(v, dtype=float)
+        for m in range(self.rot // 2):
+            a, b = (m, m + self.rot // 2) if self.halves else (2 * m, 2 * m + 1)
+            c, s = self.gain * np.cos(p * self.freq[m]), self.gain * np.sin(p * self.freq[m])
+            out[:, a], out[:, b] = v[:, a] * c - v[:, b] * s, v[:, b] * c + v[:, a] * s
+        return out
+
+
+def tree_hidden(lay, group, parents, base, node0, first, delta):
+    """Slots (c, h, j) of pass delta's scores that take the mask's value: the query in slot (j - delta) mod t against place c t + j."""
+    t, per = lay.t, lay.t // group
+    follows = []
+    for i, p in enumerate(parents):
+        follows.append({i} | (follows[p] if p >= 0 else set()))
+    out, last = np.zeros((lay.E, lay.H, t)), (base + len(parents) - 1) // t
+    for c in range(lay.E):
+        for j in range(t):
+            place, u = c * t + j, (j - delta) % t % per
+            node = node0 + (u - base - node0) % per
+            seen = follows[node] if node < len(parents) else set()
+            out[c, :, j] = not (first // t <= c <= last and (place < base or place - base in seen))
+    return out

@@ -5,6 +5,8 @@ Sec. 5.1-5.3 (query times K cache, scores times V cache, cache append), written 
 small operation set so that the same steps run on plain slot vectors (`SlotOps`, no
 cryptography) and on oracle ciphertexts (`CkksOps`).
 """
+import functools
+
 import numpy as np
 
 from .packing import GqaLayout, KvLayout, VmmPlan, _log2
@@ -547,3 +549,126 @@ def gqa_score_times_v(ops, glay: GqaLayout, cs_list, v_cts, rot_plaintexts, sv=N
     for l in range(_log2(glay.t)):
         acc = ops.add(acc, ops.rotate(acc, 1 << l))
     return acc
+
+
+# ---- drafted tokens: rotary positions by tables, appended runs, attention of a tree ----------------------------------------
+def weighted_rotations(ctx, keys, x, terms, here=None):
+    """here x + sum over (r, pt) of pt Rot(x, r) in the extended basis: hoisted rotations, each multiplied before any ModDown."""
+    ext, hoisted = ctx.ext_idx(x.level), ctx.hoist(x) if terms else None
+    acc = [np.zeros((len(ext), ctx.n), dtype=np.uint64) for _ in range(2)]
+    if here is not None:
+        ctx.mac_pt_raised(acc, ctx.raise_ct(x), here, x.level)
+    for r, pt in terms:
+        ctx.mac_pt_raised(acc, ctx.rotate_hoisted_raised(x, hoisted, r, keys), pt, x.level)
+    return acc
+
+
+def rotary_plaintexts(ctx, tables, coeffs, positions, level):
+    """Plaintexts (extended basis) of the positions at every residue (-1: none) from the tables' integer coefficients: what stays, the
+    rotation up, the rotation down, or both rotations in one where they are the same."""
+    L, K = ctx.prm.L, ctx.prm.K
+    idx = [L + 1, L + 2 if K > 1 else 0]
+    m1, m2 = (int(ctx.mod[i]) for i in idx)
+
+    def entry(i, residue=0):
+        e = ctx.ntt(ctx.from_i64(coeffs[i], idx), idx)
+        return ctx.automorphism(e, idx, ctx.galois(-residue)) if residue else e
+    parts = [np.zeros((2, ctx.n), dtype=np.uint64) for _ in range(3)]
+    for r, p in enumerate(positions):
+        if p < 0:
+            continue
+        c1, c2, s1, s2 = (entry(4 * (p % tables.low) + k, r) for k in range(4))
+        c, s = (entry(4 * tables.low + 1 + 2 * (p // tables.low) + k) for k in range(2))
+        ctx.mac(parts[0], ctx.add(ctx.add(c1, c2, idx), entry(4 * tables.low, r), idx), c, idx)
+        parts[0] = ctx.sub(parts[0], ctx.mul(ctx.add(s1, s2, idx), s, idx), idx)
+        parts[1] = ctx.sub(parts[1], ctx.add(ctx.mul(s1, c, idx), ctx.mul(c1, s, idx), idx), idx)
+        parts[2] = ctx.add(parts[2], ctx.add(ctx.mul(s2, c, idx), ctx.mul(c2, s, idx), idx), idx)
+    if 2 * tables.step == ctx.S:
+        parts = [parts[0], ctx.add(parts[1], parts[2], idx)]
+    out = []
+    for v in parts:
+        a, b = ctx.intt(v, idx).astype(object)
+        value = (b + m2 * ((a - b) * pow(m2, -1, m1) % m1)) % (m1 * m2)
+        value = np.where(2 * value > m1 * m2, value - m1 * m2, value)
+        out.append(ctx.pt_from_coeffs_ext(((2 * value + m2) // (2 * m2)).astype(np.int64), level, float(ctx.mod[level])))
+    return out
+
+
+def rotary(ctx, keys, tables, x, plaintexts):
+    """A ciphertext with its positions, one level below."""
+    steps = [tables.step, -tables.step][: len(plaintexts) - 1]
+    acc = weighted_rotations(ctx, keys, x, list(zip(steps, plaintexts[1:])), plaintexts[0])
+    return ctx.rescale(ctx.moddown_ct(acc, x.level, x.scale * float(ctx.mod[x.level])))
+
+
+def _turned_sum(ctx, pt, steps):
+    """The sum of a plaintext's slot rotations (exact permutations of its polynomial)."""
+    idx = ctx.q_idx(pt.level)
+    m = functools.reduce(lambda a, b: ctx.add(a, b, idx), (ctx.automorphism(pt.m, idx, ctx.galois(s)) for s in steps))
+    return type(pt)(m, pt.level, pt.scale)
+
+
+def kv_append_run(ctx, keys, lay: KvLayout, k_cts, v_cts, place, ntok, ck, cv, residue_mask, row_mask, turned=None, x_cts=None):
+    """Append ntok <= t tokens from `place` on, that of place a at residue a mod t of ck and cv.  residue_mask, row_mask: the plaintexts of
+    the slots of residue 0 and of the slots (0, h, 0).  turned: what is added to the K ciphertexts, one a page (keys with rotary
+    positions); k_cts: a list by page (None: nothing yet)."""
+    t, B = lay.t, lay.H * lay.t
+    tokens = [(place % t + i) for i in range(ntok)]
+    for p in sorted({i // t for i in tokens}):
+        c = place // t + p
+        new = turned[p] if turned is not None else ctx.rescale(ctx.mul_pt(ck, _turned_sum(ctx, residue_mask, [-(i % t) for i in tokens if i // t == p])))
+        k_cts[c] = new if k_cts[c] is None else ctx.ct_add(k_cts[c], new)
+    rows = _turned_sum(ctx, row_mask, [-(i // t * B + i % t) for i in tokens])
+
+    def put(cts, k, src, row):
+        new = ctx.rescale(ctx.mul_pt(src, _turned_sum(ctx, rows, [-row * B])))
+        cts[k] = new if cts[k] is None else ctx.ct_add(cts[k], new)
+    h = ctx.hoist(cv)
+    for k in range(lay.E):
+        g = k // lay.r_i
+        put(v_cts, k, ctx.rotate_hoisted(cv, h, -g * lay.r_i * B, keys) if g else cv, (place // t - k) % lay.E + g * lay.r_i)
+    if x_cts is not None:
+        h = ctx.hoist(ck)
+        for k in range(lay.E):
+            j, g = k % lay.r_i, k // lay.r_i
+            put(x_cts, k, ctx.rotate_hoisted(ck, h, j * B, keys) if j else ck, (place // t + g * lay.r_i) % lay.E)
+
+
+def tree_moved(ctx, keys, lay: KvLayout, x, delta, masks):
+    """Residue r of every block moved to (r + delta) mod t, in the extended basis; masks[delta - 1]: the integer coefficients of the
+    residues from delta on, at the scale of the level's prime."""
+    q = int(ctx.mod[x.level])
+    rest = -np.asarray(masks[delta - 1])
+    rest[0] += q
+    pts = [ctx.pt_from_coeffs_ext(c, x.level, float(q)) for c in (masks[delta - 1], rest)]
+    return weighted_rotations(ctx, keys, x, list(zip((-delta, lay.t - delta), pts)))
+
+
+def tree_qk(ctx, keys, lay: KvLayout, q, masks, product, mask_pts):
+    """Scores of a tree: pass delta is the query group moved by delta residues, its un-replicated product with the keys, and mask_pts[delta] added."""
+    out = []
+    for delta in range(lay.t):
+        x = ctx.level_drop(q, q.level - 1) if delta == 0 else \
+            ctx.rescale(ctx.moddown_ct(tree_moved(ctx, keys, lay, q, delta, masks), q.level, q.scale * float(ctx.mod[q.level])))
+        y = product(x)
+        y.c[0] = ctx.add(y.c[0], mask_pts[delta][: y.level + 1], ctx.q_idx(y.level))
+        out.append(y)
+    return out
+
+
+def tree_sv(ctx, keys, lay: KvLayout, scores, masks, product):
+    """Such scores times the values: the products moved back and summed, one ModDown and rescale."""
+    acc = None
+    for delta in range(lay.t):
+        part = product(scores[delta])
+        if delta == 0:
+            out = ctx.level_drop(part, part.level - 1)
+            continue
+        u = tree_moved(ctx, keys, lay, part, lay.t - delta, masks)
+        ext = ctx.ext_idx(part.level)
+        acc = u if acc is None else [ctx.add(a, b, ext) for a, b in zip(acc, u)]
+    if acc is None:
+        return out
+    moved = ctx.rescale(ctx.moddown_ct(acc, part.level, part.scale * float(ctx.mod[part.level])))
+    moved.scale = out.scale
+    return ctx.ct_add(out, moved)
