@@ -324,6 +324,9 @@ bool ks_batches_grow(cm_ctx *ctx);
 // components (+ accums[r]); addends / accums nullable arrays of nullable pointers
 cm_status moddown_batch_into(cm_ctx *ctx, u64 *us, int level, int m, const u64 *const *addends, int addend_comps, u64 g,
                              const u64 *const *accums, u64 *const *outs, hipStream_t st, bool rows_done = false);
+// the same with a Galois element for each addend
+cm_status moddown_batch_turned(cm_ctx *ctx, u64 *us, int level, int m, const u64 *const *addends, int addend_comps, const u64 *gs, u64 *const *outs,
+                               hipStream_t st);
 // raised[r][2][ext][n] = sum_j perm_{g_r}(digits_j) * key_r + P * perm_{g_r}(in.c0): hoisted rotations left in the
 // extended basis
 cm_status ks_apply_many_raised(cm_ctx *ctx, const u64 *digits, int level, int cnt, const u64 *const *keys,

@@ -554,6 +554,12 @@ cm_status moddown_batch_into(cm_ctx *ctx, u64 *us, int level, int m, const u64 *
     moddown_batch(ctx, ks_level_full(ctx, level), us, m, addends, addend_comps, gs, accums, outs, st, rows_done);
     return CM_OK;
 }
+cm_status moddown_batch_turned(cm_ctx *ctx, u64 *us, int level, int m, const u64 *const *addends, int addend_comps, const u64 *gs, u64 *const *outs,
+                               hipStream_t st) {
+    if (m < 1 || m > ks_batch_max(ctx, level)) return CM_E_INVAL;
+    moddown_batch(ctx, ks_level_full(ctx, level), us, m, addends, addend_comps, gs, nullptr, outs, st);
+    return CM_OK;
+}
 cm_status moddown_many(cm_ctx *ctx, u64 *us, int level, int cnt, u64 *const *outs, hipStream_t st) {
     const KsLevelFull &k = ks_level_full(ctx, level);
     const size_t ublk = 2 * (size_t)k.ext * ctx->n;

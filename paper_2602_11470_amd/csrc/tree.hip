@@ -13,7 +13,7 @@
 
 #include <algorithm>
 
-#include "kv.h"
+#include "passes.h"
 #include "rotary.h"
 
 #define TREE_ROWS 4
@@ -27,6 +27,7 @@ struct cm_tree {
     u64 *d_unseen = nullptr;                  // [E - 1][level][n]: entry m - 1: in the rows m .. E - 1
     u64 *d_work = nullptr;
     KsManyTables tabs;                        // raise of the second components of CM_KS_BATCH results
+    KvPasses passes;                          // for caches with the creating one's baby steps; others' passes run one at a time
 };
 
 struct TreeMask {
@@ -49,9 +50,19 @@ __global__ __launch_bounds__(256) void k_tree_mask(TreeMask m, int rows, const u
     *p = v;
 }
 
+// out[c][limbs][n] = a[c][limbs][n] + the first limbs of b[c][limbs + 1][n]
+__global__ __launch_bounds__(256) void k_add_dropped(u64 *__restrict__ out, const u64 *__restrict__ a, const u64 *__restrict__ b, const ModC *__restrict__ modc,
+                                                     int limbs, int n) {
+    const size_t i = blockIdx.x * 256 + threadIdx.x;
+    const int l = blockIdx.y, c = blockIdx.z;
+    const size_t at = ((size_t)c * limbs + l) * n + i;
+    out[at] = addmod(a[at], b[at + (size_t)c * n], modc[l].q);
+}
+
 extern "C" void cm_tree_destroy(cm_tree *tr) {
     if (!tr) return;
     ks_many_tables_destroy(&tr->tabs);
+    kv_passes_destroy(&tr->passes);
     hipFree(tr->d_q), hipFree(tr->d_v), hipFree(tr->d_one), hipFree(tr->d_unseen), hipFree(tr->d_work);
     delete tr;
 }
@@ -133,6 +144,8 @@ extern "C" cm_status cm_tree_create(cm_ctx *ctx, const cm_kv *kv, int32_t group,
             rows_from_on(ctx, tr->d_unseen, row, H * t, E, level);
             if (hipDeviceSynchronize() != hipSuccess || hipGetLastError() != hipSuccess) status = CM_E_HIP;
         }
+        // last, so that what the object cannot do without has its memory
+        if (status == CM_OK) kv_passes_create(ctx, kv, t, &tr->passes);
     } catch (...) {
         status = CM_E_NOMEM;
     }
@@ -205,11 +218,16 @@ extern "C" cm_status cm_tree_qk(cm_ctx *ctx, const cm_evk *evk, const cm_tree *t
         const int from = first / t, many = page + rows - from;                // pages that are seen
         if (many < tr->E) unseen = tr->d_unseen + (size_t)(many - 1) * lv * n, gu = (unsigned)rot_g(kv, -(long long)from * kv->H * t);
     }
-    for (int d0 = 0; d0 < t; d0 += CM_KS_BATCH) {
-        const int m = std::min(CM_KS_BATCH, t - d0), skip = d0 == 0;
-        if (skip) {
-            cm_ct x0{x, lv, 2, q->scale};
-            CMCHK(cm_level_drop(ctx, q, lv, &x0, stream));
+    const bool joint = kv->indexed && kv_passes_fit(tr->passes, kv);
+    const int turn = joint ? tr->passes.P : CM_KS_BATCH;
+    const size_t xw = joint ? tr->passes.r_i * ctw : ctw;                     // from one pass's ciphertext to the next one's
+    if (joint) x = tr->passes.babies;
+    for (int d0 = 0; d0 < t; d0 += turn) {
+        const int m = std::min(turn, t - d0), skip = d0 == 0;
+        if (skip) {                                                          // pass 0 does not move: a level drop
+            u64 *dst[2] = {x, x + ctw / 2};
+            const u64 *src[2] = {q->dev, q->dev + (size_t)(lv + 2) * n};
+            launch_copies(dst, src, 2, ctw / 2, st);
         }
         if (m > skip) {
             WrBatch b;
@@ -217,15 +235,21 @@ extern "C" cm_status cm_tree_qk(cm_ctx *ctx, const cm_evk *evk, const cm_tree *t
             u64 *outs[CM_KS_BATCH];
             for (int z = 0; z < b.nz; z++) {
                 tree_moves(evk, tr, b.it + 2 * z, tr->d_q, (size_t)up.ext * n, d0 + skip + z, digits, q->dev);
-                b.out[z] = us + z * 2 * (size_t)up.ext * n, outs[z] = x + (skip + z) * ctw;
+                b.out[z] = us + z * 2 * (size_t)up.ext * n, outs[z] = x + (skip + z) * xw;
             }
             launch_weighted(ctx, b, up.beta, lv + 1, st);
             CMCHK(weighted_down(ctx, us, lv + 1, b.nz, outs, tmp, st));
         }
+        if (joint) {
+            u64 *outs[CM_KS_BATCH];
+            for (int z = 0; z < m; z++) outs[z] = scores[d0 + z].dev;
+            CMCHK(kv_passes_run(ctx, evk, kv, tr->passes, kv->d_x, m, outs, st));
+        }
         for (int z = 0; z < m; z++) {
-            cm_ct in{x + z * ctw, lv, 2, q->scale};
-            if (kv->indexed) CMCHK(kv_sv(ctx, evk, kv, &in, &scores[d0 + z], st, false, kv->d_x, false));
-            else CMCHK(kv_qk(ctx, evk, kv, &in, &scores[d0 + z], st, false));
+            cm_ct in{x + z * xw, lv, 2, q->scale}, &out = scores[d0 + z];
+            if (joint) out.level = lv - 1, out.ncomp = 2, out.scale = in.scale * kv->scale / (double)ctx->mod[lv];
+            else if (kv->indexed) CMCHK(kv_sv(ctx, evk, kv, &in, &out, st, false, kv->d_x, false));
+            else CMCHK(kv_qk(ctx, evk, kv, &in, &out, st, false));
         }
         for (int r0 = 0; r0 < rows; r0 += TREE_ROWS) {
             TreeMask mk;
@@ -269,25 +293,33 @@ extern "C" cm_status cm_tree_sv(cm_ctx *ctx, const cm_evk *evk, const cm_tree *t
     const size_t n = ctx->n, B = CM_KS_BATCH, pw = 2 * (size_t)lv * n, dblk = (size_t)dn.beta * dn.ext * n, ublk = 2 * (size_t)dn.ext * n;
     u64 *parts = tr->d_work, *ksin = parts + B * pw, *digits = ksin + B * (size_t)lv * n, *acc = digits + B * dblk, *nxt = acc + ublk, *own = nxt + ublk,
         *res = own + pw, *tmp = res + pw;
-    double scale = 0;
+    const double scale = scores[0].scale * kv->scale / (double)ctx->mod[lv];
+    const bool joint = kv_passes_fit(tr->passes, kv);
+    const int turn = joint ? tr->passes.P : CM_KS_BATCH;
     bool any = false;
-    for (int d0 = 0; d0 < t; d0 += CM_KS_BATCH) {
-        const int m = std::min(CM_KS_BATCH, t - d0), skip = d0 == 0;
-        for (int z = 0; z < m; z++) {
-            cm_ct part{parts + z * pw, lp, 2, 0.0};
-            CMCHK(kv_sv(ctx, evk, kv, &scores[d0 + z], &part, st, false, kv->d_v, false));
-            scale = part.scale;
-            if (d0 + z == 0) {
-                cm_ct first{own, lp - 1, 2, 0.0};
-                CMCHK(cm_level_drop(ctx, &part, lp - 1, &first, stream));
+    for (int d0 = 0; d0 < t; d0 += turn) {
+        const int m = std::min(turn, t - d0), skip = d0 == 0;
+        // the results, the one that does not move in a place of its own
+        u64 *to[CM_KS_BATCH];
+        for (int z = 0; z < m; z++) to[z] = d0 + z == 0 ? own : parts + (z - skip) * pw;
+        if (joint) {
+            u64 *dst[CM_KS_BATCH];
+            const u64 *src[CM_KS_BATCH];
+            for (int z = 0; z < m; z++) dst[z] = tr->passes.babies + z * tr->passes.r_i * kv_ctw(kv), src[z] = scores[d0 + z].dev;
+            launch_copies(dst, src, m, kv_ctw(kv), st);
+            CMCHK(kv_passes_run(ctx, evk, kv, tr->passes, kv->d_v, m, to, st));
+        } else {
+            for (int z = 0; z < m; z++) {
+                cm_ct part{to[z], lp, 2, 0.0};
+                CMCHK(kv_sv(ctx, evk, kv, &scores[d0 + z], &part, st, false, kv->d_v, false));
             }
         }
         if (m == skip) continue;
-        CMCHK(ks_raise_many(ctx, tr->tabs, parts + skip * pw, ksin, digits, st, m - skip));
+        CMCHK(ks_raise_many(ctx, tr->tabs, parts, ksin, digits, st, m - skip));
         WrBatch b;
         b.nz = 1, b.nsum = 2 * (m - skip);
         for (int z = skip; z < m; z++)
-            tree_moves(evk, tr, b.it + 2 * (z - skip), tr->d_v, (size_t)dn.ext * n, t - (d0 + z), digits + (z - skip) * dblk, parts + z * pw);
+            tree_moves(evk, tr, b.it + 2 * (z - skip), tr->d_v, (size_t)dn.ext * n, t - (d0 + z), digits + (z - skip) * dblk, parts + (z - skip) * pw);
         b.extra[0] = any ? acc : nullptr, b.out[0] = nxt;
         launch_weighted(ctx, b, dn.beta, lp, st);
         std::swap(acc, nxt);
@@ -295,9 +327,11 @@ extern "C" cm_status cm_tree_sv(cm_ctx *ctx, const cm_evk *evk, const cm_tree *t
     }
     if (any) {
         CMCHK(weighted_down(ctx, acc, lp, 1, &res, tmp, st));
-        launch_add(ctx, out->dev, own, res, 2, lp, st);
+        hipLaunchKernelGGL(k_add_dropped, dim3(n / 256, lp, 2), dim3(256), 0, st, out->dev, res, own, ctx->d_modc, lp, (int)n);
     } else {
-        HIPCHK(hipMemcpyAsync(out->dev, own, 2 * (size_t)lp * n * 8, hipMemcpyDeviceToDevice, st));
+        u64 *dst[2] = {out->dev, out->dev + (size_t)lp * n};
+        const u64 *src[2] = {own, own + (size_t)lv * n};
+        launch_copies(dst, src, 2, (size_t)lp * n, st);
     }
     out->level = lp - 1, out->ncomp = 2, out->scale = scale;
     RETURN_LAUNCH_STATUS();
