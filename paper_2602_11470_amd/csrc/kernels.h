@@ -171,6 +171,9 @@ struct WrBatch {
     u64 *out[WR_OUTS] = {};
 };
 void launch_weighted(cm_ctx *ctx, const WrBatch &b, int beta, int level, hipStream_t st);
+// the same from half-transformed digits (ConvBatch::half), with the row pass of the inverse transform of the rows from inv_from on (0: none), as
+// launch_rows_ip; only where it applies (rows_weighted_fits)
+void launch_rows_weighted(cm_ctx *ctx, const WrBatch &b, int beta, int level, hipStream_t st, int inv_from);
 #define IP_MULTI_KEYS 3
 struct IpKeys {
     const u64 *key[IP_MULTI_KEYS] = {};
@@ -232,6 +235,19 @@ struct FinishBatch {
     __host__ __device__ const u64 *mul_row(int r, int l, int n) const { return mul_pt + ((size_t)(mul[r] >> 16) * ext + l) * n; }
 };
 void launch_cols_inv(cm_ctx *ctx, u64 *data, const int *d_rows, const int *d_mod_idx, int limbs, hipStream_t st);
+// Plaintexts of rotary positions (rotary.hip).  v[set][part][2][n]: the products of up to ROT_ENTRIES entries of the tables under the moduli ma, mb, in coefficients
+#define ROT_ENTRIES 64
+struct RotEntry {
+    unsigned short low, high;
+    unsigned g, sets;              // Galois element that takes residue 0 to the token's; the sets (bits) it belongs to
+};
+struct RotBatch {
+    RotEntry e[ROT_ENTRIES];       // in the order of their high parts
+};
+void launch_rotary_inv(cm_ctx *ctx, u64 *v, const RotBatch &b, int count, const u64 *low, const u64 *still, const u64 *high, int ma, int mb, int parts, int sets,
+                       const int *d_mods, hipStream_t st);
+// p[poly][ext][n]: v over the second modulus, to the nearest integer, in multiplier form and transformed; inv: that modulus' inverse under the first
+void launch_rotary_fwd(cm_ctx *ctx, u64 *p, const u64 *v, int ma, int mb, u64 inv, int level, int polys, const int *d_mods, hipStream_t st);
 // forward transform of conv[items*ncomp*(level+1)][n] (mods 0..level repeating) with that tail
 // with src: the first pass reads row d_src_rows[i] of src for limb i (words below twice that limb's modulus) instead of conv
 void launch_ntt_fwd_finish(cm_ctx *ctx, u64 *conv, const int *d_mods, const FinishBatch &fb, hipStream_t st,
@@ -341,10 +357,10 @@ size_t arena_digits_words(const cm_ctx *ctx);
 // us + r*2*ext'*n, ext' = level + 1 + sets*K, whose special limbs of s = 0 .. sets-1 follow each other and whose ciphertext limbs
 // are summed over s; add_r = add + r*add_stride (on the first add_comps components), acc_r = acc + r*acc_stride ([2][level+1][n],
 // nullable).  One forward transform per output limb instead of two, and four launches fewer than one after the other.  Rows
-// level .. of us are overwritten.  outs: the results' places, where they do not follow each other.  ks_drop_fits: whether the kernels cover this level and count (otherwise: two steps).
+// level .. of us are overwritten.  outs: the results' places, where they do not follow each other; onto: added there (no add, no acc).  ks_drop_fits: whether the kernels cover this level and count (otherwise: two steps).
 bool ks_drop_fits(cm_ctx *ctx, int level, int sets, int m);
 cm_status ks_drop(cm_ctx *ctx, u64 *us, int level, int sets, int m, const u64 *add, size_t add_stride, int add_comps, u64 g,
-                  const u64 *acc, size_t acc_stride, u64 *out, hipStream_t st, bool rows_done = false, u64 *const *outs = nullptr);
+                  const u64 *acc, size_t acc_stride, u64 *out, hipStream_t st, bool rows_done = false, u64 *const *outs = nullptr, bool onto = false);
 // what joins row `level` of a ks_drop (launch_rows_ip does it where it does the inverse row pass: inv_from = level)
 FoldIn ks_drop_fold(cm_ctx *ctx, int level, int sets, const u64 *add, size_t add_stride, int add_comps, u64 g, const u64 *acc, size_t acc_stride);
 // out[2][level][n] = rescale(ModDown(u[2][ext][n])), in one where ks_drop_fits, through tmp[2][level+1][n] otherwise

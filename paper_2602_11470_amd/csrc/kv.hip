@@ -459,17 +459,17 @@ extern "C" cm_status cm_kv_append_run(cm_ctx *ctx, const cm_evk *evk, cm_kv *kv,
         residues[i / t].push_back(rot_g(kv, -(i % t)));
     }
     const u64 *k_src = k_new->dev;
+    bool rows_done;
     if (rotary && !kv->indexed) {
         const u64 *x = k_new->dev;
-        u64 *outs[2] = {prod, res};
-        CMCHK(rotary_sums(ctx, evk, rotary, 1, &x, pages > 1 ? 1 : 0, pages, us, st));
-        CMCHK(weighted_down(ctx, us, lk, pages, outs, rotary->d_work, st));
-        for (int p = 0; p < pages; p++) launch_add(ctx, kv->d_k + (size_t)(c + p) * ctw, kv->d_k + (size_t)(c + p) * ctw, outs[p], 2, lv, st);
+        u64 *outs[2] = {kv->d_k + (size_t)c * ctw, kv->d_k + (size_t)(c + 1) * ctw};
+        CMCHK(rotary_sums(ctx, evk, rotary, 1, &x, pages > 1 ? 1 : 0, pages, us, &rows_done, st));
+        CMCHK(weighted_down(ctx, us, lk, pages, outs, rotary->d_work, st, rows_done, true));
     } else {
         if (rotary) {
-            u64 *turned = rotary->d_work + 2 * (size_t)(lk + 1) * n;              // the raise is done with what it held there
-            CMCHK(rotary_sums(ctx, evk, rotary, 1, &k_src, 0, 1, us, st));
-            CMCHK(weighted_down(ctx, us, lk, 1, &turned, rotary->d_work, st));
+            u64 *turned = rotary->d_work + 2 * (size_t)(lk + 1) * n;
+            CMCHK(rotary_sums(ctx, evk, rotary, 1, &k_src, 0, 1, us, &rows_done, st));
+            CMCHK(weighted_down(ctx, us, lk, 1, &turned, rotary->d_work, st, rows_done));
             k_src = turned;
         }
         for (int p = 0; p < pages; p++) {

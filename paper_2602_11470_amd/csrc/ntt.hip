@@ -945,9 +945,14 @@ __device__ __forceinline__ void rip_out(u64 *lds, u64 *out, const u64 (&x)[4], c
 }
 // SHARED: one key for all outputs (one item each, no Galois element): the wave runs over outputs z0 .. z1-1, draws the uniform half
 // of its key words once into LDS and keeps the twiddles.
-template <class A, class S, bool SHARED>
+// WEIGHTED: every item's sum times its plaintext (w.pt), and here P c on top (WrBatch); an item ends its own sums.
+struct RipWeights {
+    const u64 *pt[WR_ITEMS];
+    const u64 *here[WR_OUTS], *c_here[WR_OUTS];
+};
+template <class A, class S, bool SHARED, bool WEIGHTED = false>
 __device__ __forceinline__ void rip_body(u64 *lds, const IpBatch &b, const RipArgs &p, const FoldIn &fi, const NttTables &t, const NttTables &ti,
-                                         int r, int mi, unsigned R, int z0, int z1) {
+                                         int r, int mi, unsigned R, int z0, int z1, const RipWeights *w = nullptr) {
     const ModC m = t.modc[mi];
     const int n = p.n, sub = threadIdx.x & 63, special = p.ext - p.level - 1, out_rows = b.apart ? p.ext + (b.nsum - 1) * special : p.ext;
     const unsigned pos = 256 * R + 4 * sub;
@@ -1052,7 +1057,18 @@ __device__ __forceinline__ void rip_body(u64 *lds, const IpBatch &b, const RipAr
 #pragma unroll
                 for (int k = 0; k < 4; k++) acc[k].mac_b(*word_at(it.c0 + (size_t)r * n, g ? perm_src(pos + k, g, p.logn) : pos + k), w);
             }
-            if (!S::LAZY || apart || s + 1 == b.nsum) {
+            if (WEIGHTED) {
+                const u64 *pt = w->pt[z * b.nsum + s] + (size_t)r * n + 256 * R;
+                u64 f[4];
+#pragma unroll
+                for (int k = 0; k < 4; k++) f[k] = *word_at(pt, 4 * sub + k);
+#pragma unroll
+                for (int k = 0; k < 4; k++) {
+                    r0[k] = addmod(r0[k], redc((u128)acc[k].sum_b(m) * f[k], m.q, m.qinv), m.q);
+                    r1[k] = addmod(r1[k], redc((u128)acc[k].sum_a(m) * f[k], m.q, m.qinv), m.q);
+                    acc[k] = S();
+                }
+            } else if (!S::LAZY || apart || s + 1 == b.nsum) {
 #pragma unroll
                 for (int k = 0; k < 4; k++) {
                     const u64 x = acc[k].sum_b(m), y = acc[k].sum_a(m);
@@ -1069,6 +1085,15 @@ __device__ __forceinline__ void rip_body(u64 *lds, const IpBatch &b, const RipAr
             }
         }
         if (apart) continue;
+        if (WEIGHTED && w->here[z] && r <= p.level) {
+            const u64 *h = w->here[z] + (size_t)r * n, *c = w->c_here[z] + (size_t)r * n, pm = p.pmont[r];
+#pragma unroll
+            for (int k = 0; k < 4; k++) {
+                const u64 f = redc((u128)*word_at(h, pos + k) * pm, m.q, m.qinv);
+                r0[k] = addmod(r0[k], redc((u128)*word_at(c, pos + k) * f, m.q, m.qinv), m.q);
+                r1[k] = addmod(r1[k], redc((u128)*word_at(c + (size_t)(p.level + 1) * n, pos + k) * f, m.q, m.qinv), m.q);
+            }
+        }
         if (b.extra[z]) {
             const u64 *e = b.extra[z] + (size_t)r * n;
 #pragma unroll
@@ -1106,6 +1131,15 @@ __global__ CODE_ALIGN __launch_bounds__(64 * RIP_WAVES, 2) void k_rows_ip(IpBatc
     const int z0 = blockIdx.z * per, z1 = min(z0 + per, b.nz);
     if (t.fpq[mi].q != 0.0) rip_body<FpArith, RipFp, SHARED>(l, b, p, fi, t, ti, r, mi, R, z0, z1);
     else rip_body<IntArith, RipInt, SHARED>(l, b, p, fi, t, ti, r, mi, R, z0, z1);
+}
+__global__ CODE_ALIGN __launch_bounds__(64 * RIP_WAVES, 2) void k_rows_ip_weighted(IpBatch b, RipWeights w, RipArgs p, NttTables t, NttTables ti) {
+    extern __shared__ u64 lds[];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = p.ext - 1 - (int)blockIdx.y;
+    const int mi = r <= p.level ? r : p.L + 1 + (r - p.level - 1);
+    u64 *l = lds + wave * RIP_ROW;
+    const unsigned R = blockIdx.x * RIP_WAVES + wave;
+    if (t.fpq[mi].q != 0.0) rip_body<FpArith, RipFp, false, true>(l, b, p, FoldIn(), t, ti, r, mi, R, blockIdx.z, blockIdx.z + 1, &w);
+    else rip_body<IntArith, RipInt, false, true>(l, b, p, FoldIn(), t, ti, r, mi, R, blockIdx.z, blockIdx.z + 1, &w);
 }
 
 // Row pass of the inverse transform of the last limbs of a cache append's masked products, formed on load: limb 2 z + c is
@@ -1403,6 +1437,144 @@ __global__ __launch_bounds__(FULL_THREADS) void masked_full(FinishBatch fb, NttT
     else masked_full_last<IntArith>(lds, w, ti, fb, r, c, n);
     if (t.fpq[l].q != 0.0) masked_full_limb<FpArith>(lds, w, t, fb, l, limb, n);
     else masked_full_limb<IntArith>(lds, w, t, fb, l, limb, n);
+}
+
+// ---- plaintexts of rotary positions (rotary.hip) ----------------------------------------------------------------------
+// The products of the tables' entries are formed as the inverse transform loads them (n = 65536), the rounded quotients as the forward one does, under
+// the modulus of each of its limbs.  One token at level 3: 5.1 + 5.8 -> 8.5 us and 6.1 + 9.6 -> 12.7.  At n = 4096, where a workgroup has a whole
+// limb and its lanes eight words, the products there take as long as a launch of their own and spill (3.6 + 7.3 -> 15), the quotients as long as theirs.
+struct RotaryTabs {
+    const u64 *low, *still, *high;
+    int count, parts, logn;
+};
+// words pos(k) of part `part` under one of the two moduli; at: word offset of its limb in an entry of two limbs.  An entry's words are all
+// requested before the first is used.
+template <int NW, class P>
+__device__ __forceinline__ void rotary_words(u64 (&sum)[NW], const RotBatch &b, const RotaryTabs &r, int part, int set, P pos, size_t at, size_t poly, const ModC &m) {
+    u64 x[NW], y[NW], x2[NW], y2[NW];                       // sums of one high part: the factors of its cosine and of its sine
+    auto mul = [&](u64 a, u64 c) { return redc((u128)a * c, m.q, m.qinv); };
+    const bool both = part == 1 && r.parts == 2;            // both rotations in one plaintext
+#pragma unroll
+    for (int k = 0; k < NW; k++) sum[k] = x[k] = y[k] = x2[k] = y2[k] = 0;
+    for (int k = 0; k < r.count; k++) {
+        const RotEntry e = b.e[k];
+        if (e.sets >> set & 1u) {
+            const u64 *p = r.low + (size_t)e.low * 4 * poly + at, *c1 = p, *c2 = p + poly, *s1 = p + 2 * poly, *s2 = p + 3 * poly;
+            u64 w1[NW], w2[NW], w3[NW], w4[NW], w5[NW];
+#pragma unroll
+            for (int i = 0; i < NW; i++) {
+                const unsigned src = perm_src(pos(i), e.g, r.logn);
+                if (part != 2) w1[i] = c1[src], w3[i] = s1[src];
+                if (part != 1 || both) w2[i] = c2[src], w4[i] = s2[src];
+                if (part == 0 && r.still) w5[i] = r.still[at + src];
+            }
+#pragma unroll
+            for (int i = 0; i < NW; i++) {
+                if (part == 0) {
+                    x[i] = addmod(x[i], addmod(w1[i], w2[i], m.q), m.q), y[i] = addmod(y[i], addmod(w3[i], w4[i], m.q), m.q);
+                    if (r.still) x[i] = addmod(x[i], w5[i], m.q);
+                } else {
+                    if (part == 1) x[i] = addmod(x[i], w3[i], m.q), y[i] = addmod(y[i], w1[i], m.q);
+                    if (part == 2 || both) x2[i] = addmod(x2[i], w4[i], m.q), y2[i] = addmod(y2[i], w2[i], m.q);
+                }
+            }
+        }
+        if (k + 1 < r.count && b.e[k + 1].high == e.high) continue;
+        const u64 *h = r.high + (size_t)e.high * 2 * poly + at;
+        u64 c[NW], w[NW];
+#pragma unroll
+        for (int i = 0; i < NW; i++) c[i] = h[pos(i)], w[i] = h[poly + pos(i)];
+#pragma unroll
+        for (int i = 0; i < NW; i++) {
+            if (part == 0) sum[i] = addmod(sum[i], submod(mul(x[i], c[i]), mul(y[i], w[i]), m.q), m.q);
+            else sum[i] = addmod(sum[i], submod(addmod(mul(x2[i], c[i]), mul(y2[i], w[i]), m.q), addmod(mul(x[i], c[i]), mul(y[i], w[i]), m.q), m.q), m.q);
+            x[i] = y[i] = x2[i] = y2[i] = 0;
+        }
+    }
+}
+// limb = (set parts + part) 2 + which of the moduli
+template <class A>
+__device__ __forceinline__ void rotary_rows_inv_body(u64 *lds, u64 *p, const RotBatch &b, const RotaryTabs &r, const NttTables &ti, int mi, int n, int chunk, int limb) {
+    A ar;
+    ar.init(ti, mi, n);
+    const ModC m = ti.modc[mi];
+    const int sub = threadIdx.x & 63, row = threadIdx.x >> 6, poly = limb >> 1, part = poly % r.parts, set = poly / r.parts;
+    const unsigned pos0 = (unsigned)chunk * SMALL_CHUNK + row * 256 + 4 * sub;
+    u64 w[4];
+    typename A::T v[4];
+    rotary_words(w, b, r, part, set, [&](int k) { return pos0 + k; }, (size_t)(limb & 1) * n, 2 * (size_t)n, m);
+#pragma unroll
+    for (int k = 0; k < 4; k++) v[k] = ar.from_rest(w[k]);
+    small_inv(lds, v, ar, 256 + 8 * chunk + row, sub, SmallRow{row * 256}, WaveSync());
+#pragma unroll
+    for (int k = 0; k < 4; k++) ntt_store(0, p + row * 256 + 64 * k + sub, ar.to_mid(v[k]));
+}
+__global__ __launch_bounds__(SMALL_THREADS) void rotary_rows_inv(u64 *__restrict__ v, RotBatch b, RotaryTabs r, NttTables ti, int ma, int mb, int n) {
+    __shared__ u64 lds[SMALL_CHUNK + SMALL_CHUNK / 16];
+    const int per = n / SMALL_CHUNK, limb = blockIdx.x / per, chunk = blockIdx.x % per, mi = limb & 1 ? mb : ma;
+    u64 *p = v + (size_t)limb * n + (size_t)chunk * SMALL_CHUNK;
+    if (ti.fpq[mi].q != 0.0) rotary_rows_inv_body<FpArith>(lds, p, b, r, ti, mi, n, chunk, limb);
+    else rotary_rows_inv_body<IntArith>(lds, p, b, r, ti, mi, n, chunk, limb);
+}
+// round((a, b) / m2) under q in multiplier form, (a, b) the residues of a coefficient under m1 and m2; inv: m2^-1 mod m1 in multiplier form
+__device__ __forceinline__ u64 rotary_rounded(u64 a, u64 b, const ModC &m1, u64 m2, u64 inv, const ModC &m) {
+    const bool above = b > m2 / 2;                         // the residue under m2 nearest to zero: b or b - m2
+    const u64 x = redc((u128)a * inv, m1.q, m1.qinv), y = redc((u128)(above ? m2 - b : b) * inv, m1.q, m1.qinv);
+    const u64 w = above ? addmod(x, y, m1.q) : submod(x, y, m1.q);
+    const bool negative = w > m1.q / 2;
+    const u64 z = to_mont(negative ? m1.q - w : w, m);
+    return negative && z ? m.q - z : z;
+}
+struct RotaryRound {
+    int ma, mb, level, L, ext;
+    u64 inv;
+};
+template <class A>
+__device__ __forceinline__ void rotary_full_fwd_body(u64 *lds, u64 *p, const u64 *v, const RotaryRound &r, const NttTables &t, int mi, int n) {
+    A ar;
+    ar.init(t, mi, n);
+    const ModC m1 = t.modc[r.ma], m = t.modc[mi];
+    const u64 m2 = t.modc[r.mb].q;
+    u64 a[8], b[8];
+    typename A::T x[8];
+#pragma unroll
+    for (int k = 0; k < 8; k++) a[k] = v[threadIdx.x + 512 * k], b[k] = v[n + threadIdx.x + 512 * k];
+#pragma unroll
+    for (int k = 0; k < 8; k++) x[k] = ar.from_lazy(rotary_rounded(a[k], b[k], m1, m2, r.inv, m));
+    full_fwd_body<A, false>(lds, p, x, ar, t, n, 0, FinishBatch());
+}
+// limb = poly ext + limb of the extended basis
+__global__ __launch_bounds__(FULL_THREADS) void rotary_full_fwd(u64 *__restrict__ p, const u64 *__restrict__ v, RotaryRound r, NttTables t, int n) {
+    __shared__ u64 lds[FULL_LDS];
+    const int poly = blockIdx.x / r.ext, l = blockIdx.x % r.ext, mi = l <= r.level ? l : r.L + l - r.level;
+    if (t.fpq[mi].q != 0.0) rotary_full_fwd_body<FpArith>(lds, p + (size_t)blockIdx.x * n, v + 2 * (size_t)poly * n, r, t, mi, n);
+    else rotary_full_fwd_body<IntArith>(lds, p + (size_t)blockIdx.x * n, v + 2 * (size_t)poly * n, r, t, mi, n);
+}
+template <class A>
+__device__ __forceinline__ void rotary_cols_fwd_body(u64 *lds, u64 *p, const u64 *v, const RotaryRound &r, const NttTables &t, int mi, int n) {
+    A ar;
+    ar.init(t, mi, n);
+    const ModC m1 = t.modc[r.ma], m = t.modc[mi];
+    const u64 m2 = t.modc[r.mb].q;
+    const int n2 = n >> 8, c = threadIdx.x % SMALL_CW, sub = threadIdx.x / SMALL_CW;
+    u64 a[4], b[4];
+    typename A::T x[4];
+#pragma unroll
+    for (int k = 0; k < 4; k++) a[k] = v[(64 * k + sub) * n2 + c], b[k] = v[n + (64 * k + sub) * n2 + c];
+#pragma unroll
+    for (int k = 0; k < 4; k++) x[k] = ar.from_lazy(rotary_rounded(a[k], b[k], m1, m2, r.inv, m));
+    small_fwd(lds, x, ar, SmallTw<A>(ar, 1, sub), sub, SmallCol{c}, GroupSync());
+#pragma unroll
+    for (int k = 0; k < 4; k++) ntt_store(0, p + (4 * sub + k) * n2 + c, ar.to_mid(x[k]));
+}
+__global__ __launch_bounds__(64 * SMALL_CW) void rotary_cols_fwd(u64 *__restrict__ p, const u64 *__restrict__ v, RotaryRound r, NttTables t, int n) {
+    __shared__ u64 lds[256 * SMALL_CW];
+    const int per = n / (256 * SMALL_CW), limb = blockIdx.x / per, c0 = (blockIdx.x % per) * SMALL_CW;
+    const int poly = limb / r.ext, l = limb % r.ext, mi = l <= r.level ? l : r.L + l - r.level;
+    u64 *dst = p + (size_t)limb * n + c0;
+    const u64 *src = v + 2 * (size_t)poly * n + c0;
+    if (t.fpq[mi].q != 0.0) rotary_cols_fwd_body<FpArith>(lds, dst, src, r, t, mi, n);
+    else rotary_cols_fwd_body<IntArith>(lds, dst, src, r, t, mi, n);
 }
 
 // ---- fast base conversion, fused into the first pass of the forward transform of its results --------------------------
@@ -1979,6 +2151,29 @@ void launch_mul_pt_rot_last_inv(cm_ctx *ctx, u64 *out, const MulPtBatch &b, int 
     }
     launch_cols_inv(ctx, out, nullptr, d_mods, 2 * cnt, st);
 }
+void launch_rotary_inv(cm_ctx *ctx, u64 *v, const RotBatch &b, int count, const u64 *low, const u64 *still, const u64 *high, int ma, int mb, int parts, int sets,
+                       const int *d_mods, hipStream_t st) {
+    const int limbs = 2 * parts * sets, n = ctx->n;
+    const RotaryTabs r{low, still, high, count, parts, ctx->logn};
+    const NttTables ti = tables_of(ctx, true, limbs);
+    {
+        Prof prof_(ctx, CM_K_NTT_INV, 0, st);              // the limbs are counted with their second pass
+        hipLaunchKernelGGL(rotary_rows_inv, dim3(limbs * (n / SMALL_CHUNK)), dim3(SMALL_THREADS), 0, st, v, b, r, ti, ma, mb, n);
+    }
+    launch_cols_inv(ctx, v, nullptr, d_mods, limbs, st);
+}
+void launch_rotary_fwd(cm_ctx *ctx, u64 *p, const u64 *v, int ma, int mb, u64 inv, int level, int polys, const int *d_mods, hipStream_t st) {
+    const int n = ctx->n, ext = level + 1 + ctx->K, limbs = polys * ext;
+    Prof prof_(ctx, CM_K_NTT_FWD, limbs, st);
+    const RotaryRound r{ma, mb, level, ctx->L, ext, inv};
+    const NttTables t = tables_of(ctx, false, limbs);
+    if (n == 4096) {
+        hipLaunchKernelGGL(rotary_full_fwd, dim3(limbs), dim3(FULL_THREADS), 0, st, p, v, r, t, n);
+        return;
+    }
+    hipLaunchKernelGGL(rotary_cols_fwd, dim3(limbs * (256 / SMALL_CW)), dim3(64 * SMALL_CW), 0, st, p, v, r, t, n);
+    launch_rows_fwd<false>(p, nullptr, d_mods, t, n, limbs, FinishBatch(), st);
+}
 void launch_ntt_fwd_finish(cm_ctx *ctx, u64 *conv, const int *d_mods, const FinishBatch &fb, hipStream_t st, const u64 *src,
                            const int *d_src_rows) {
     const int limbs = fb.items * fb.ncomp * (fb.level + 1), n = ctx->n;
@@ -2123,6 +2318,24 @@ void launch_rows_ip(cm_ctx *ctx, const IpBatch &b, int beta, int level, hipStrea
     }
     hipLaunchKernelGGL(k_rows_ip<false>, dim3(ctx->n / (256 * RIP_WAVES), ext, b.nz), dim3(64 * RIP_WAVES), RIP_WAVES * RIP_ROW * 8, st, b, p, fi, t,
                        ti, 1);
+}
+void launch_rows_weighted(cm_ctx *ctx, const WrBatch &b, int beta, int level, hipStream_t st, int inv_from) {
+    const int ext = level + 1 + ctx->K;
+    Prof prof_(ctx, CM_K_INNER_PRODUCT, b.nz * b.nsum, st);
+    RipArgs p;
+    p.beta = beta, p.ext = ext, p.level = level, p.alpha = ctx->alpha, p.L = ctx->L, p.nmod = ctx->nmod, p.n = ctx->n, p.logn = ctx->logn;
+    p.kdig = (ctx->L + ctx->alpha) / ctx->alpha, p.inv_from = inv_from, p.ubound = ctx->d_ubound, p.pmont = ctx->d_pmont;
+    IpBatch ip;
+    RipWeights w;
+    ip.nz = b.nz, ip.nsum = b.nsum;
+    for (int i = 0; i < WR_ITEMS; i++) {
+        w.pt[i] = b.it[i].pt;
+        ip.it[i].dig = b.it[i].dig, ip.it[i].key = b.it[i].key, ip.it[i].g = b.it[i].g, ip.it[i].c0 = b.it[i].c;
+        ip.it[i].own = b.it[i].c ? b.it[i].c + (size_t)(level + 1) * ctx->n : nullptr;
+    }
+    for (int z = 0; z < WR_OUTS; z++) w.here[z] = b.here[z], w.c_here[z] = b.c_here[z], ip.out[z] = b.out[z], ip.extra[z] = b.extra[z];
+    hipLaunchKernelGGL(k_rows_ip_weighted, dim3(ctx->n / (256 * RIP_WAVES), ext, b.nz), dim3(64 * RIP_WAVES), RIP_WAVES * RIP_ROW * 8, st, ip, w, p,
+                       tables_of(ctx, false, 0), tables_of(ctx, true, 0));
 }
 void launch_ntt_rows(cm_ctx *ctx, u64 *data, const int *d_rows, const int *d_mod_idx, int limbs,
                      bool inverse, hipStream_t st) {

@@ -439,7 +439,7 @@ FoldIn ks_drop_fold(cm_ctx *ctx, int level, int sets, const u64 *add, size_t add
     return fi;
 }
 cm_status ks_drop(cm_ctx *ctx, u64 *us, int level, int sets, int m, const u64 *add, size_t add_stride, int add_comps, u64 g,
-                  const u64 *acc, size_t acc_stride, u64 *out, hipStream_t st, bool rows_done, u64 *const *outs) {
+                  const u64 *acc, size_t acc_stride, u64 *out, hipStream_t st, bool rows_done, u64 *const *outs, bool onto) {
     if (!ks_drop_fits(ctx, level, sets, m)) return CM_E_INVAL;
     const KsLevelFull &k = ks_level_full(ctx, level);
     Arena A = arena_of(ctx);
@@ -457,6 +457,9 @@ cm_status ks_drop(cm_ctx *ctx, u64 *us, int level, int sets, int m, const u64 *a
         fb.addend[r] = add ? add + r * add_stride : nullptr, fb.accum[r] = acc ? acc + r * acc_stride : nullptr;
     }
     fb.pinv = k.d_pqinv, fb.ainv = get_qlinv(ctx, level);
+    // what is added behind the rescale has the results' layout and no factor
+    if (onto) fb.ainv = nullptr, fb.in_rows = 0;
+    for (int r = 0; r < m && onto; r++) fb.accum[r] = fb.out[r];
     ConvBatch cb;
     cb.tabs = k.d_drop[sets - 1], cb.batch = 2 * m, cb.ns = ns, cb.max_nt = level, cb.fold = true, cb.near = k.near_drop[sets - 1] && k.pays_drop[sets - 1];
     cb.in_stride = (size_t)ext * n, cb.out_stride = (size_t)level * n;

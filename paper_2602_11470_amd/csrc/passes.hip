@@ -7,7 +7,7 @@
 #include <algorithm>
 
 #define PS_TPB 256
-#define PS_KEYS 8                  // keys of a workgroup
+#define PS_KEYS 16                 // keys of a launch
 #define PS_GROUP 4                 // passes of a lane
 typedef u64 u64x2 __attribute__((ext_vector_type(2)));
 
@@ -25,21 +25,21 @@ void launch_copies(u64 *const *dst, const u64 *const *src, int m, size_t words, 
     hipLaunchKernelGGL(k_copies, dim3(words / (2 * PS_TPB), m), dim3(PS_TPB), 0, st, b);
 }
 
-// Rotations of several ciphertexts by the same steps, before their ModDown: out[a][p] = sum_j sigma_a(dig_p,j) key_a,j for up to PS_KEYS keys a
+// Rotations of several ciphertexts by the same steps, before their ModDown: out[a][p] = sum_j sigma_a(dig_p,j) key_a,j for `per` keys a
 // a workgroup and PS_GROUP passes p.  As in k_inner_product_fanout a lane keeps the digit words of two source positions and writes each result
 // where the key's Galois map sends them; here it keeps those of PS_GROUP passes, so a key's words are read and drawn once for all.
 struct FanPasses {
-    int n;                              // keys
-    const u64 *key[2 * PS_KEYS];
-    unsigned ginv[2 * PS_KEYS];
+    int n, per;                         // keys, of a workgroup
+    const u64 *key[PS_KEYS];
+    unsigned ginv[PS_KEYS];
 };
 template <bool SA, int NB>
 __global__ __launch_bounds__(PS_TPB) void k_fan_passes(FanPasses f, u64 *__restrict__ out, const u64 *__restrict__ dig, int passes, const ModC *__restrict__ modc,
                                                        int beta, int ext, int level, int L, int nmod, int n, int logn, EvkA eva, const u64 *__restrict__ ubound) {
-    const int chunks = (f.n + PS_KEYS - 1) / PS_KEYS;
+    const int chunks = (f.n + f.per - 1) / f.per;
     const unsigned s2 = (blockIdx.x * PS_TPB + threadIdx.x) * 2;
     const int r = blockIdx.y, mi = r <= level ? r : L + 1 + (r - level - 1), p0 = (int)(blockIdx.z / chunks) * PS_GROUP;
-    const int first = (int)(blockIdx.z % chunks) * PS_KEYS, end = min(f.n, first + PS_KEYS);
+    const int first = (int)(blockIdx.z % chunks) * f.per, end = min(f.n, first + f.per);
     const ModC m = modc[mi];
     const u64 bound = ubound[mi];
     const bool small = m.q < (1ULL << 50);
@@ -94,7 +94,7 @@ __global__ __launch_bounds__(PS_TPB) void k_fan_passes(FanPasses f, u64 *__restr
 static void launch_fan_passes(cm_ctx *ctx, const FanPasses &f, u64 *out, const u64 *dig, int passes, int beta, int level, hipStream_t st) {
     Prof prof_(ctx, CM_K_INNER_PRODUCT, f.n * passes, st);
     const int ext = level + 1 + ctx->K;
-    const dim3 grid(ctx->n / (2 * PS_TPB), ext, (f.n + PS_KEYS - 1) / PS_KEYS * ((passes + PS_GROUP - 1) / PS_GROUP));
+    const dim3 grid(ctx->n / (2 * PS_TPB), ext, (f.n + f.per - 1) / f.per * ((passes + PS_GROUP - 1) / PS_GROUP));
 #define FANP(SA_, NB_)                                                                                                                                  \
     hipLaunchKernelGGL((k_fan_passes<SA_, NB_>), grid, dim3(PS_TPB), 0, st, f, out, dig, passes, ctx->d_modc, beta, ext, level, ctx->L, ctx->nmod, ctx->n, \
                        ctx->logn, evk_a_of(ctx), ctx->d_ubound)
@@ -145,13 +145,13 @@ cm_status kv_passes_run(cm_ctx *ctx, const cm_evk *evk, const cm_kv *kv, const K
     // rotations by rows: keys in groups whose results one ModDown takes
     if (r_i > 1) {
         CMCHK(ks_raise_many(ctx, kp.baby_tabs, kp.babies, kp.ksin, kp.digits, st, m));
-        const int most = std::max(1, std::min({ks_batch_max(ctx, lv) / m, 2 * PS_KEYS, CM_MASK_BATCH / m}));
+        const int most = std::max(1, std::min({ks_batch_max(ctx, lv) / m, PS_KEYS, CM_MASK_BATCH / m}));
         for (int j0 = 1; j0 < r_i; j0 += most) {
             FanPasses f;
-            f.n = std::min(most, r_i - j0);
+            f.n = std::min(most, r_i - j0), f.per = n == 4096 ? 1 : 8;
             u64 gs[CM_MASK_BATCH], *to[CM_MASK_BATCH];
             const u64 *adds[CM_MASK_BATCH];
-            for (int a = 0; a < 2 * PS_KEYS; a++) {
+            for (int a = 0; a < PS_KEYS; a++) {
                 const u64 g = rot_g(kv, (j0 + (a < f.n ? a : 0)) * Ht);
                 f.key[a] = find_key(evk, g), f.ginv[a] = (unsigned)rot_g(kv, -(j0 + (a < f.n ? a : 0)) * Ht);
                 for (int p = 0; p < m && a < f.n; p++)
@@ -191,6 +191,7 @@ cm_status kv_passes_run(cm_ctx *ctx, const cm_evk *evk, const cm_kv *kv, const K
             ip.it[r].dig = kp.digits + r * dblk, ip.it[r].key = relin, ip.it[r].own = adds[r] + 2 * ln, ip.out[r] = us + r * ublk;
         }
         if (half) launch_rows_ip(ctx, ip, kl.beta, lv, st, lv + 1);
+        else if (n == 4096) launch_inner_product_batch(ctx, ip, kl.beta, lv, st);       // lanes that walk over all items are too few to fill the chip
         else launch_inner_product_shared_key(ctx, ip, kl.beta, lv, st);
         CMCHK(moddown_batch_into(ctx, us, lv, cnt, adds, 2, 0, nullptr, to, st, half));
     }

@@ -16,16 +16,22 @@ struct cm_rotary {
     u64 *d_still = nullptr;           // [2][n], null where the whole head turns
     u64 *d_high = nullptr;            // [high][cos, sin][2][n], multiplier form
     u64 *d_v = nullptr, *d_p = nullptr;      // [set][part][2][n], [set][part][ext][n] (multiplier form)
-    u64 *d_work = nullptr;            // a ciphertext, then the second components, coefficients and digits of a batch
+    u64 *d_work = nullptr;            // two ciphertexts, then the second components, coefficients and digits of a batch
     int *d_mods = nullptr, *d_ext_mods = nullptr;
     KsManyTables tabs;
     std::vector<int32_t> pos;         // set last
     int split = 0;
     bool set = false;
 };
-cm_status rotary_sums(cm_ctx *ctx, const cm_evk *evk, const cm_rotary *r, int m, const u64 *const *xs, int first, int sets, u64 *us, hipStream_t st);
-// outs[z][2][level][n] = rescale(ModDown(us[z][2][ext][n])) for z < m <= CM_KS_BATCH; tmp: a ciphertext of the level, used where it takes two steps
-cm_status weighted_down(cm_ctx *ctx, u64 *us, int level, int m, u64 *const *outs, u64 *tmp, hipStream_t st);
+// of up to r->batch ciphertexts, each with the plaintexts of `sets` sets from the first on: sums on the extended basis, us[z][set]; *rows_done: what
+// weighted_down takes
+cm_status rotary_sums(cm_ctx *ctx, const cm_evk *evk, const cm_rotary *r, int m, const u64 *const *xs, int first, int sets, u64 *us, bool *rows_done,
+                      hipStream_t st);
+// outs[z][2][level][n] = rescale(ModDown(us[z][2][ext][n])) for z < m <= CM_KS_BATCH; tmp: a ciphertext of the level (onto: two), used where it takes
+// two steps; rows_done: the row pass of the inverse transforms has been done (launch_rows_weighted); onto: outs += instead
+cm_status weighted_down(cm_ctx *ctx, u64 *us, int level, int m, u64 *const *outs, u64 *tmp, hipStream_t st, bool rows_done = false, bool onto = false);
+// whether launch_rows_weighted applies, and is the faster form, for outputs of nsum items, m ModDowns following
+bool weighted_rows(cm_ctx *ctx, int beta, int level, int nsum, int m);
 // whether na words at a and nb at b share one
 inline bool words_meet(const u64 *a, size_t na, const u64 *b, size_t nb) {
     const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;

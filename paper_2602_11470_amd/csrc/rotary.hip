@@ -19,15 +19,10 @@
 #include "kernels.h"
 #include "rotary.h"
 
-#define ROT_ENTRIES 64
 #define ROT_TPB 256
-struct RotEntry {
-    unsigned short low, high;
-    unsigned g, sets;              // Galois element that takes residue 0 to the token's; the sets (bits) it belongs to
-};
-struct RotBatch {
-    RotEntry e[ROT_ENTRIES];       // in the order of their high parts
-};
+// Tokens up to which the products are formed inside the inverse transform's row pass (launch_rotary_inv), whose lanes each do four words of them: one
+// token 8.5 us joined, 10.9 apart; eight 24 and 18.
+#define ROT_JOINED 4
 static bool rot_pow2(int x) { return x > 0 && (x & (x - 1)) == 0; }
 
 // v[set][part][2][n] (+)= the products of the tables' entries; limb blockIdx.y under modulus ma or mb
@@ -64,25 +59,6 @@ __global__ __launch_bounds__(ROT_TPB) void k_rotary_products(u64 *__restrict__ v
     out[0] = here, out[poly] = up;
     if (parts == 3) out[2 * poly] = dn;
 }
-// p[poly][ext][n] = round(v / m2) as residues in multiplier form: v[poly][2][n] in coefficients under m1 and m2; inv: m2^-1 mod m1 in
-// multiplier form
-__global__ __launch_bounds__(ROT_TPB) void k_rotary_round(u64 *__restrict__ p, const u64 *__restrict__ v, const ModC *__restrict__ modc, int ma, int mb,
-                                                          u64 inv, int level, int L, int ext, int n) {
-    const size_t i = blockIdx.x * ROT_TPB + threadIdx.x;
-    const ModC m1 = modc[ma];
-    const u64 m2 = modc[mb].q, a = v[(size_t)blockIdx.y * 2 * n + i], b = v[((size_t)blockIdx.y * 2 + 1) * n + i];
-    const bool above = b > m2 / 2;                         // the residue under m2 nearest to zero: b or b - m2
-    const u64 r = (above ? m2 - b : b) % m1.q;
-    const u64 w = redc((u128)(above ? addmod(a, r, m1.q) : submod(a, r, m1.q)) * inv, m1.q, m1.qinv);
-    const bool negative = w > m1.q / 2;
-    const u64 size = negative ? m1.q - w : w;
-    u64 *out = p + (size_t)blockIdx.y * ext * n + i;
-    for (int l = 0; l < ext; l++) {
-        const ModC m = modc[l <= level ? l : L + l - level];
-        const u64 x = to_mont(size, m);
-        out[(size_t)l * n] = negative && x ? m.q - x : x;
-    }
-}
 // out[z][limbs][n] = the second components of b.c[z]
 struct SecondBatch {
     const u64 *c[CM_KS_BATCH];
@@ -93,65 +69,107 @@ __global__ __launch_bounds__(ROT_TPB) void k_second(u64 *__restrict__ out, Secon
 }
 
 // ---- weighted rotations -----------------------------------------------------------------------------------------------
-// A lane has two neighbouring words of an output and runs over its items: the item's digits through the Galois map, its key's
-// words, the sums reduced and multiplied by the item's plaintext.
-template <bool SA>
+// A lane has W neighbouring words of an output and runs over its items: the item's digits through the Galois map, its key's
+// words, the sums reduced and multiplied by the item's plaintext.  All loads of an item are requested before the first is used (NB bounds its
+// digits); one word a lane at n = 4096, where a launch is as long as a lane's chain.
+template <bool SA, int NB, int W>
 __global__ __launch_bounds__(ROT_TPB) void k_weighted(WrBatch b, const ModC *__restrict__ modc, int beta, int ext, int level, int L, int nmod, int n,
                                                       int logn, const u64 *__restrict__ pmont, EvkA eva, const u64 *__restrict__ ubound) {
-    const unsigned i2 = (blockIdx.x * ROT_TPB + threadIdx.x) * 2;
+    typedef u64 words __attribute__((ext_vector_type(W)));
+    const unsigned i0 = (blockIdx.x * ROT_TPB + threadIdx.x) * W;
     const int r = blockIdx.y, z = blockIdx.z, mi = r <= level ? r : L + 1 + (r - level - 1);
     const ModC m = modc[mi];
-    const size_t o = (size_t)r * n + i2;
-    const u64 bound = ubound[mi], cg0 = ((u64)i2 + 1) * GOLD, cg1 = cg0 + GOLD, pm = r <= level ? pmont[r] : 0;
-    ulonglong2 r0 = make_ulonglong2(0, 0), r1 = make_ulonglong2(0, 0);
+    const size_t o = (size_t)r * n + i0;
+    const u64 bound = ubound[mi], pm = r <= level ? pmont[r] : 0;
+    u64 r0[W] = {}, r1[W] = {};
     auto mul = [&](u64 x, u64 y) { return redc((u128)x * y, m.q, m.qinv); };
-    auto pair = [](const u64 *p) { return *reinterpret_cast<const ulonglong2 *>(p); };
-    if (b.extra[z]) r0 = pair(b.extra[z] + o), r1 = pair(b.extra[z] + (size_t)ext * n + o);
+    auto load = [](const u64 *p) { return *reinterpret_cast<const words *>(p); };
+    if (b.extra[z]) {
+        const words x = load(b.extra[z] + o), y = load(b.extra[z] + (size_t)ext * n + o);
+#pragma unroll
+        for (int k = 0; k < W; k++) r0[k] = x[k], r1[k] = y[k];
+    }
     if (b.here[z] && r <= level) {
-        const ulonglong2 w = pair(b.here[z] + o), x = pair(b.c_here[z] + o), y = pair(b.c_here[z] + (size_t)(level + 1) * n + o);
-        const u64 wx = mul(w.x, pm), wy = mul(w.y, pm);
-        r0.x = addmod(r0.x, mul(x.x, wx), m.q), r0.y = addmod(r0.y, mul(x.y, wy), m.q);
-        r1.x = addmod(r1.x, mul(y.x, wx), m.q), r1.y = addmod(r1.y, mul(y.y, wy), m.q);
+        const words w = load(b.here[z] + o), x = load(b.c_here[z] + o), y = load(b.c_here[z] + (size_t)(level + 1) * n + o);
+#pragma unroll
+        for (int k = 0; k < W; k++) {
+            const u64 wp = mul(w[k], pm);
+            r0[k] = addmod(r0[k], mul(x[k], wp), m.q), r1[k] = addmod(r1[k], mul(y[k], wp), m.q);
+        }
     }
     for (int s = 0; s < b.nsum; s++) {
         const WrItem it = b.it[z * b.nsum + s];
-        const unsigned src = perm_src(i2, it.g, logn), base = src & ~1u;
-        const bool swap = src & 1u;
-        u128 a0 = 0, a1 = 0, b0 = 0, b1 = 0;
-        for (int j = 0; j < beta; j++) {
-            const ulonglong2 d = pair(it.dig + ((size_t)j * ext + r) * n + base);
-            const u64 dx = swap ? d.y : d.x, dy = swap ? d.x : d.y;
-            const u64 *kb = it.key + ((size_t)j * nmod + mi) * n + i2;
-            const u64 ex = __builtin_nontemporal_load(kb), ey = __builtin_nontemporal_load(kb + 1);
-            const ulonglong2 ea = evk_a_words<SA>(it.key, eva, nmod, n, j, mi, i2, cg0, cg1, bound);
-            b0 += (u128)dx * ex, b1 += (u128)dy * ey, a0 += (u128)dx * ea.x, a1 += (u128)dy * ea.y;
+        const unsigned src = perm_src(i0, it.g, logn), base = src & ~(unsigned)(W - 1), flip = src & (W - 1);      // word k is word k ^ flip of the pair
+        words d[NB], e[NB], c;
+        u64 sk[NB];
+#pragma unroll
+        for (int j = 0; j < NB; j++)
+            if (j < beta) {
+                const size_t at = ((size_t)j * nmod + mi) * n + i0;
+                d[j] = load(it.dig + ((size_t)j * ext + r) * n + base);
+                e[j] = __builtin_nontemporal_load(reinterpret_cast<const words *>(it.key + at));
+                if (!SA) sk[j] = it.key[(size_t)eva.kdig * nmod * n + (size_t)j * nmod + mi];
+            }
+        if (r <= level) c = load(it.c + (size_t)r * n + base);
+        const words w = load(it.pt + o);
+#pragma unroll
+        for (int k = 0; k < W; k++) {
+            u128 sa = 0, sb = 0;
+            const u64 cg = ((u64)i0 + k + 1) * GOLD;
+#pragma unroll
+            for (int j = 0; j < NB; j++)
+                if (j < beta) {
+                    const u64 x = W == 1 ? d[j][0] : flip ? d[j][W - 1 - k] : d[j][k];
+                    const u64 a = SA ? __builtin_nontemporal_load(it.key + eva.a_off + ((size_t)j * nmod + mi) * n + i0 + k) : evk_a_draw(sk[j], cg, i0 + k, bound);
+                    sb += (u128)x * e[j][k], sa += (u128)x * a;
+                }
+            if (r <= level) sb += (u128)(W == 1 ? c[0] : flip ? c[W - 1 - k] : c[k]) * pm;
+            r0[k] = addmod(r0[k], mul(redc(sb, m.q, m.qinv), w[k]), m.q);
+            r1[k] = addmod(r1[k], mul(evk_a_reduce<SA>(sa, m), w[k]), m.q);
         }
-        if (r <= level) {
-            const ulonglong2 c = pair(it.c + (size_t)r * n + base);
-            b0 += (u128)(swap ? c.y : c.x) * pm, b1 += (u128)(swap ? c.x : c.y) * pm;
-        }
-        const ulonglong2 w = pair(it.pt + o);
-        r0.x = addmod(r0.x, mul(redc(b0, m.q, m.qinv), w.x), m.q), r0.y = addmod(r0.y, mul(redc(b1, m.q, m.qinv), w.y), m.q);
-        r1.x = addmod(r1.x, mul(evk_a_reduce<SA>(a0, m), w.x), m.q), r1.y = addmod(r1.y, mul(evk_a_reduce<SA>(a1, m), w.y), m.q);
     }
-    *reinterpret_cast<ulonglong2 *>(b.out[z] + o) = r0;
-    *reinterpret_cast<ulonglong2 *>(b.out[z] + (size_t)ext * n + o) = r1;
+    words x, y;
+#pragma unroll
+    for (int k = 0; k < W; k++) x[k] = r0[k], y[k] = r1[k];
+    *reinterpret_cast<words *>(b.out[z] + o) = x;
+    *reinterpret_cast<words *>(b.out[z] + (size_t)ext * n + o) = y;
+}
+template <int W>
+static void launch_weighted_words(cm_ctx *ctx, const WrBatch &b, int beta, int level, hipStream_t st) {
+    const int ext = level + 1 + ctx->K;
+    const dim3 grid(ctx->n / (W * ROT_TPB), ext, b.nz);
+#define WEIGHTED(SA_, NB_)                                                                                                                                     \
+    hipLaunchKernelGGL((k_weighted<SA_, NB_, W>), grid, dim3(ROT_TPB), 0, st, b, ctx->d_modc, beta, ext, level, ctx->L, ctx->nmod, ctx->n, ctx->logn, ctx->d_pmont, \
+                       evk_a_of(ctx), ctx->d_ubound)
+    if (ctx->evk_stored_a) {
+        if (beta <= 4) WEIGHTED(true, 4);
+        else WEIGHTED(true, CM_MAX_DIGITS);
+    } else if (beta <= 1) WEIGHTED(false, 1);
+    else if (beta <= 2) WEIGHTED(false, 2);
+    else if (beta <= 4) WEIGHTED(false, 4);
+    else if (beta <= 6) WEIGHTED(false, 6);
+    else WEIGHTED(false, CM_MAX_DIGITS);
+#undef WEIGHTED
 }
 void launch_weighted(cm_ctx *ctx, const WrBatch &b, int beta, int level, hipStream_t st) {
     Prof prof_(ctx, CM_K_INNER_PRODUCT, b.nz * b.nsum, st);
-    const int ext = level + 1 + ctx->K;
-    const dim3 grid(ctx->n / (2 * ROT_TPB), ext, b.nz);
-    if (ctx->evk_stored_a)
-        hipLaunchKernelGGL(k_weighted<true>, grid, dim3(ROT_TPB), 0, st, b, ctx->d_modc, beta, ext, level, ctx->L, ctx->nmod, ctx->n, ctx->logn,
-                           ctx->d_pmont, evk_a_of(ctx), ctx->d_ubound);
-    else
-        hipLaunchKernelGGL(k_weighted<false>, grid, dim3(ROT_TPB), 0, st, b, ctx->d_modc, beta, ext, level, ctx->L, ctx->nmod, ctx->n, ctx->logn,
-                           ctx->d_pmont, evk_a_of(ctx), ctx->d_ubound);
+    if (ctx->n == 4096) launch_weighted_words<1>(ctx, b, beta, level, st);
+    else launch_weighted_words<2>(ctx, b, beta, level, st);
 }
-cm_status weighted_down(cm_ctx *ctx, u64 *us, int level, int m, u64 *const *outs, u64 *tmp, hipStream_t st) {
-    if (ks_drop_fits(ctx, level, 1, m)) return ks_drop(ctx, us, level, 1, m, nullptr, 0, 0, 0, nullptr, 0, nullptr, st, false, outs);
+// The row pass of the digits inside the weighted sums (launch_rows_weighted) repeats it for every item: the faster form with one item an output.  Two
+// ciphertexts at level 22, one rotation each: raise, sums and row passes 242 -> 218 us; with two rotations at level 12 143 -> 159, at level 3 39 -> 43.
+bool weighted_rows(cm_ctx *ctx, int beta, int level, int nsum, int m) {
+    return ctx->n == 65536 && !ctx->evk_stored_a && beta <= 7 && nsum == 1 && ks_drop_fits(ctx, level, 1, m);
+}
+cm_status weighted_down(cm_ctx *ctx, u64 *us, int level, int m, u64 *const *outs, u64 *tmp, hipStream_t st, bool rows_done, bool onto) {
+    if (ks_drop_fits(ctx, level, 1, m)) return ks_drop(ctx, us, level, 1, m, nullptr, 0, 0, 0, nullptr, 0, nullptr, st, rows_done, outs, onto);
     const size_t ublk = 2 * (size_t)(level + 1 + ctx->K) * ctx->n;
-    for (int z = 0; z < m; z++) CMCHK(moddown_rescale_into(ctx, us + z * ublk, level, tmp, outs[z], st));
+    for (int z = 0; z < m; z++) {
+        // tmp holds what the first step leaves and, onto, the result behind it
+        u64 *to = onto ? tmp + 2 * (size_t)(level + 1) * ctx->n : outs[z];
+        CMCHK(moddown_rescale_into(ctx, us + z * ublk, level, tmp, to, st));
+        if (onto) launch_add(ctx, outs[z], outs[z], to, 2, level, st);
+    }
     return CM_OK;
 }
 
@@ -225,7 +243,7 @@ extern "C" cm_status cm_rotary_create(cm_ctx *ctx, int32_t heads, int32_t dim, i
         get(&r->d_low, polys * 2 * n), get(&r->d_high, (size_t)r->high * 4 * n);
         if (rot_dims < dim) get(&r->d_still, 2 * n);
         get(&r->d_v, (size_t)ROT_SETS * r->parts * 2 * n), get(&r->d_p, (size_t)ROT_SETS * r->parts * kl.ext * n);
-        get(&r->d_work, 2 * ln + r->batch * (2 * ln + dblk));
+        get(&r->d_work, 4 * ln + r->batch * (2 * ln + dblk));
         get((u64 **)&d_coeffs, chunk * n);
         std::vector<int> mods, ext_mods;
         for (size_t i = 0; i < chunk; i++) mods.push_back(r->ma), mods.push_back(r->mb);
@@ -303,7 +321,7 @@ extern "C" cm_status cm_rotary_set(cm_ctx *ctx, cm_rotary *r, const int32_t *pos
     for (int i = 0; i < r->t; i++) if (pos[i] < -1 || pos[i] >= r->room) return CM_E_LAYOUT;
     CM_TRY
     hipStream_t st = (hipStream_t)stream;
-    const int n = ctx->n, sets = split ? ROT_SETS : 1, ext = r->level + 1 + ctx->K;
+    const int n = ctx->n, sets = split ? ROT_SETS : 1;
     std::vector<RotEntry> entries;
     for (int i = 0; i < r->t; i++)
         if (pos[i] >= 0)
@@ -311,33 +329,33 @@ extern "C" cm_status cm_rotary_set(cm_ctx *ctx, cm_rotary *r, const int32_t *pos
                                1u | (i >= split ? 2u : 4u)});
     std::sort(entries.begin(), entries.end(), [](const RotEntry &a, const RotEntry &b) { return a.high < b.high; });
     std::vector<int32_t> kept(pos, pos + r->t);
-    size_t k0 = 0;
-    do {
-        const int m = (int)std::min<size_t>(ROT_ENTRIES, entries.size() - k0);
+    auto batch = [&](size_t k0, int m) {
         RotBatch b;
         for (int k = 0; k < ROT_ENTRIES; k++) b.e[k] = k < m ? entries[k0 + k] : RotEntry{0, 0, 1, 0};
-        Prof prof_(ctx, CM_K_ELEMENTWISE, sets * r->parts * 2, st);
-        hipLaunchKernelGGL(k_rotary_products, dim3(n / ROT_TPB, 2, sets), dim3(ROT_TPB), 0, st, r->d_v, b, m, r->d_low, r->d_still, r->d_high, ctx->d_modc,
-                           r->ma, r->mb, r->parts, n, ctx->logn, k0 > 0);
-        k0 += m;
-    } while (k0 < entries.size());
-    launch_ntt(ctx, r->d_v, r->d_mods, sets * r->parts * 2, true, st);
-    {
-        Prof prof_(ctx, CM_K_ELEMENTWISE, sets * r->parts * ext, st);
-        hipLaunchKernelGGL(k_rotary_round, dim3(n / ROT_TPB, sets * r->parts), dim3(ROT_TPB), 0, st, r->d_p, r->d_v, ctx->d_modc, r->ma, r->mb, r->inv, r->level,
-                           ctx->L, ext, n);
+        return b;
+    };
+    if (n == 65536 && entries.size() <= ROT_JOINED) {
+        launch_rotary_inv(ctx, r->d_v, batch(0, (int)entries.size()), (int)entries.size(), r->d_low, r->d_still, r->d_high, r->ma, r->mb, r->parts, sets, r->d_mods, st);
+    } else {
+        for (size_t k0 = 0; k0 == 0 || k0 < entries.size(); k0 += ROT_ENTRIES) {
+            const int m = (int)std::min<size_t>(ROT_ENTRIES, entries.size() - k0);
+            Prof prof_(ctx, CM_K_ELEMENTWISE, sets * r->parts * 2, st);
+            hipLaunchKernelGGL(k_rotary_products, dim3(n / ROT_TPB, 2, sets), dim3(ROT_TPB), 0, st, r->d_v, batch(k0, m), m, r->d_low, r->d_still, r->d_high,
+                               ctx->d_modc, r->ma, r->mb, r->parts, n, ctx->logn, k0 > 0);
+        }
+        launch_ntt(ctx, r->d_v, r->d_mods, sets * r->parts * 2, true, st);
     }
-    launch_ntt(ctx, r->d_p, r->d_ext_mods, sets * r->parts * ext, false, st);
+    launch_rotary_fwd(ctx, r->d_p, r->d_v, r->ma, r->mb, r->inv, r->level, sets * r->parts, r->d_ext_mods, st);
     r->pos.swap(kept), r->split = split, r->set = true;
     RETURN_LAUNCH_STATUS();
     CM_CATCH
 }
-// of up to r->batch ciphertexts, each with the plaintexts of `sets` sets from the first on: sums on the extended basis, us[z][set]
-cm_status rotary_sums(cm_ctx *ctx, const cm_evk *evk, const cm_rotary *r, int m, const u64 *const *xs, int first, int sets, u64 *us, hipStream_t st) {
+cm_status rotary_sums(cm_ctx *ctx, const cm_evk *evk, const cm_rotary *r, int m, const u64 *const *xs, int first, int sets, u64 *us, bool *rows_done,
+                      hipStream_t st) {
     const int level = r->level;
     const KsLevel &kl = ks_level(ctx, level);
     const size_t n = ctx->n, ln = (size_t)(level + 1) * n, dblk = (size_t)kl.beta * kl.ext * n, ublk = 2 * (size_t)kl.ext * n;
-    u64 *second = r->d_work + 2 * ln, *ksin = second + r->batch * ln, *digits = ksin + r->batch * ln;
+    u64 *second = r->d_work + 4 * ln, *ksin = second + r->batch * ln, *digits = ksin + r->batch * ln;
     const u64 *keys[2];
     unsigned g[2];
     for (int s = 0; s < r->parts - 1; s++) {
@@ -351,7 +369,9 @@ cm_status rotary_sums(cm_ctx *ctx, const cm_evk *evk, const cm_rotary *r, int m,
         hipLaunchKernelGGL(k_second, dim3(n / ROT_TPB, level + 1, m), dim3(ROT_TPB), 0, st, second, b, level + 1, (int)n);
         d = second;
     }
-    CMCHK(ks_raise_many(ctx, r->tabs, d, ksin, digits, st, m));
+    const bool half = weighted_rows(ctx, kl.beta, level, r->parts - 1, m * sets);
+    CMCHK(ks_raise_many(ctx, r->tabs, d, ksin, digits, st, m, 0, half));
+    *rows_done = half;
     WrBatch b;
     b.nz = m * sets, b.nsum = r->parts - 1;
     for (int z = 0; z < m; z++)
@@ -364,7 +384,8 @@ cm_status rotary_sums(cm_ctx *ctx, const cm_evk *evk, const cm_rotary *r, int m,
                 it.dig = digits + z * dblk, it.c = xs[z], it.key = keys[s], it.g = g[s], it.pt = p + (size_t)(1 + s) * kl.ext * n;
             }
         }
-    launch_weighted(ctx, b, kl.beta, level, st);
+    if (half) launch_rows_weighted(ctx, b, kl.beta, level, st, level);
+    else launch_weighted(ctx, b, kl.beta, level, st);
     return CM_OK;
 }
 extern "C" cm_status cm_rotary_apply(cm_ctx *ctx, const cm_evk *evk, const cm_rotary *r, int32_t count, const cm_ct *x, cm_ct *y, void *stream) {
@@ -387,8 +408,9 @@ extern "C" cm_status cm_rotary_apply(cm_ctx *ctx, const cm_evk *evk, const cm_ro
         const u64 *xs[CM_KS_BATCH];
         u64 *outs[CM_KS_BATCH];
         for (int z = 0; z < m; z++) xs[z] = x[i0 + z].dev, outs[z] = y[i0 + z].dev;
-        CMCHK(rotary_sums(ctx, evk, r, m, xs, 0, 1, us, st));
-        CMCHK(weighted_down(ctx, us, r->level, m, outs, r->d_work, st));
+        bool rows;
+        CMCHK(rotary_sums(ctx, evk, r, m, xs, 0, 1, us, &rows, st));
+        CMCHK(weighted_down(ctx, us, r->level, m, outs, r->d_work, st, rows));
     }
     for (int i = 0; i < count; i++) y[i].level = r->level - 1, y[i].ncomp = 2, y[i].scale = x[i].scale;      // plaintext scale = the prime just removed
     RETURN_LAUNCH_STATUS();
