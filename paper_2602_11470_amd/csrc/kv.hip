@@ -407,27 +407,43 @@ extern "C" cm_status cm_kv_append_group(cm_ctx *ctx, const cm_evk *evk, cm_kv *k
 }
 
 
-// out = the sum of a mask's turns: entry k through the Galois map g[k]
+// Sums of a mask's turns, one for each of up to RUN_MASKS outputs: out[z] = the entries begin[z] .. begin[z + 1] - 1 of mask[z] through their Galois maps
 #define RUN_TURNS 64
+#define RUN_MASKS 3
 struct MaskTurns {
-    unsigned g[RUN_TURNS];
+    u64 *out[RUN_MASKS];
+    const u64 *mask[RUN_MASKS];
+    int begin[RUN_MASKS + 1];
+    unsigned g[RUN_MASKS * RUN_TURNS];
 };
-__global__ __launch_bounds__(256) void k_mask_turns(u64 *out, const u64 *__restrict__ mask, MaskTurns t, int count, const ModC *__restrict__ modc, int n,
-                                                    int logn, int accumulate) {
+__global__ __launch_bounds__(256) void k_mask_turns(MaskTurns t, const ModC *__restrict__ modc, int n, int logn, int accumulate) {
     const unsigned i = blockIdx.x * 256 + threadIdx.x;
+    const int z = blockIdx.z;
     const size_t row = (size_t)blockIdx.y * n;
-    const u64 q = modc[blockIdx.y].q;
-    u64 v = accumulate ? out[row + i] : 0;
-    for (int k = 0; k < count; k++) v = addmod(v, mask[row + perm_src(i, t.g[k], logn)], q);
-    out[row + i] = v;
+    const u64 q = modc[blockIdx.y].q, *mask = t.mask[z] + row;
+    u64 *out = t.out[z] + row + i;
+    u64 v = accumulate ? *out : 0;
+    for (int k = t.begin[z]; k < t.begin[z + 1]; k++) v = addmod(v, mask[perm_src(i, t.g[k], logn)], q);
+    *out = v;
 }
-static void launch_mask_turns(cm_ctx *ctx, u64 *out, const u64 *mask, const std::vector<u64> &gs, int limbs, hipStream_t st) {
-    for (size_t k0 = 0; k0 < gs.size(); k0 += RUN_TURNS) {
+struct MaskSum {
+    u64 *out;
+    const u64 *mask;
+    std::vector<u64> gs;
+};
+static void launch_mask_turns(cm_ctx *ctx, const MaskSum *sums, int count, int limbs, hipStream_t st) {
+    size_t most = 0;
+    for (int z = 0; z < count; z++) most = std::max(most, sums[z].gs.size());
+    for (size_t k0 = 0; k0 < most; k0 += RUN_TURNS) {
         MaskTurns t;
-        const int m = (int)std::min<size_t>(RUN_TURNS, gs.size() - k0);
-        for (int k = 0; k < RUN_TURNS; k++) t.g[k] = k < m ? (unsigned)gs[k0 + k] : 1;
-        Prof prof_(ctx, CM_K_ELEMENTWISE, limbs, st);
-        hipLaunchKernelGGL(k_mask_turns, dim3(ctx->n / 256, limbs), dim3(256), 0, st, out, mask, t, m, ctx->d_modc, ctx->n, ctx->logn, k0 > 0);
+        t.begin[0] = 0;
+        for (int z = 0; z < RUN_MASKS; z++) {
+            const MaskSum &s = sums[z < count ? z : 0];
+            t.out[z] = s.out, t.mask[z] = s.mask, t.begin[z + 1] = t.begin[z];
+            for (size_t k = k0; z < count && k < s.gs.size() && k < k0 + RUN_TURNS; k++) t.g[t.begin[z + 1]++] = (unsigned)s.gs[k];
+        }
+        Prof prof_(ctx, CM_K_ELEMENTWISE, count * limbs, st);
+        hipLaunchKernelGGL(k_mask_turns, dim3(ctx->n / 256, limbs, count), dim3(256), 0, st, t, ctx->d_modc, ctx->n, ctx->logn, k0 > 0);
     }
 }
 // A run of tokens from the place of the next append on.  Its masks are sums of turns of the masks that single appends use: of one residue for the
@@ -452,12 +468,16 @@ extern "C" cm_status cm_kv_append_run(cm_ctx *ctx, const cm_evk *evk, cm_kv *kv,
     CMCHK(kv_append_checks(ctx, evk, kv, k_new, v_new, ntok));
     hipStream_t st = (hipStream_t)stream;
     const size_t n = ctx->n, ctw_up = 2 * (size_t)(lv + 1) * n, ctw = kv_ctw(kv);
-    u64 *vmask = kv->d_work, *prod = vmask + (size_t)(lv + 1) * n, *res = prod + ctw_up, *shifted = res + ctw_up, *us = arena_batch_sums(ctx);
-    std::vector<u64> rows, residues[2];
+    // the masks follow one another: of V and the index, then of the K ciphertexts
+    const size_t mw = (size_t)(lv + 1) * n;
+    u64 *vmask = kv->d_work, *prod = vmask + 3 * mw, *shifted = prod + ctw_up, *us = arena_batch_sums(ctx);
+    const bool masked_keys = !rotary || kv->indexed;
+    MaskSum sums[RUN_MASKS] = {{vmask, kv->d_mask_v, {}}, {vmask + mw, kv->d_mask_k, {}}, {vmask + 2 * mw, kv->d_mask_k, {}}};
     for (int i = begin; i < end; i++) {
-        rows.push_back(rot_g(kv, -((long long)(i / t) * kv->H * t + i % t)));
-        residues[i / t].push_back(rot_g(kv, -(i % t)));
+        sums[0].gs.push_back(rot_g(kv, -((long long)(i / t) * kv->H * t + i % t)));
+        sums[1 + i / t].gs.push_back(rot_g(kv, -(i % t)));
     }
+    launch_mask_turns(ctx, sums, masked_keys ? 1 + pages : 1, lv + 1, st);
     const u64 *k_src = k_new->dev;
     bool rows_done;
     if (rotary && !kv->indexed) {
@@ -472,13 +492,16 @@ extern "C" cm_status cm_kv_append_run(cm_ctx *ctx, const cm_evk *evk, cm_kv *kv,
             CMCHK(weighted_down(ctx, us, lk, 1, &turned, rotary->d_work, st, rows_done));
             k_src = turned;
         }
-        for (int p = 0; p < pages; p++) {
-            launch_mask_turns(ctx, res, kv->d_mask_k, residues[p], lv + 1, st);
-            launch_mul_pt(ctx, prod, k_src, res, 2, lv + 1, st);
-            CMCHK(rescale_into(ctx, prod, 2, lv, kv->d_k + (size_t)(c + p) * ctw, st, nullptr, nullptr, true));
-        }
+        // K: a masked product a page, rescaled onto its ciphertext, formed inside the rescale where it does that
+        MulPtBatch mb;
+        u64 *outs[2], *last = shifted, *red = last + 4 * n;
+        for (int p = 0; p < pages; p++) mb.src[p] = k_src, mb.g[p] = 1, mb.at[p] = 1 + p, outs[p] = kv->d_k + (size_t)(c + p) * ctw;
+        if (!rescale_masked_into(ctx, mb, pages, vmask, lv, outs, st, last, red, true))
+            for (int p = 0; p < pages; p++) {
+                launch_mul_pt(ctx, prod, k_src, vmask + (1 + p) * mw, 2, lv + 1, st);
+                CMCHK(rescale_into(ctx, prod, 2, lv, outs[p], st, nullptr, nullptr, true));
+            }
     }
-    launch_mask_turns(ctx, vmask, kv->d_mask_v, rows, lv + 1, st);
     CMCHK(kv_put(ctx, evk, kv, k_src, v_new->dev, vmask, c, 0, shifted, st));
     kv->pos += ntok;
     if (kv->ntok < kv->pos) kv->ntok = kv->pos;
