@@ -157,7 +157,8 @@ bool launch_inner_product_fanout(cm_ctx *ctx, const IpFan &f, const u64 *dig, co
                                  hipStream_t st);
 // Rotations that share their digits, times plaintexts, on the extended basis (rotary.hip): output z < nz (out[z] = [2][ext][n]) is
 // extra[z] (nullable, may be out[z] itself) + here[z] P c_here[z] (here nullable) + the sum of items z*nsum .. z*nsum + nsum - 1, each
-// pt ((sum_j perm_g(dig_j) key_j) + (P perm_g(c's first component), 0)); plaintexts [ext][n] in multiplier form, c [2][level+1][n].
+// pt ((sum_j perm_g(dig_j) key_j) + (P perm_g(c's first component), 0)); plaintexts [ext][n] in multiplier form, c [2][level+1][n], whose second
+// component dig is raised from: a digit's own limbs are read there.
 #define WR_ITEMS 32
 #define WR_OUTS CM_KS_BATCH
 struct WrItem {
@@ -235,6 +236,10 @@ struct FinishBatch {
     __host__ __device__ const u64 *mul_row(int r, int l, int n) const { return mul_pt + ((size_t)(mul[r] >> 16) * ext + l) * n; }
 };
 void launch_cols_inv(cm_ctx *ctx, u64 *data, const int *d_rows, const int *d_mod_idx, int limbs, hipStream_t st);
+struct SecondBatch {
+    const u64 *c[CM_KS_BATCH];
+};
+void launch_seconds_inv(cm_ctx *ctx, u64 *data, const SecondBatch &b, int m, int limbs, const int *d_mods, hipStream_t st);
 // Plaintexts of rotary positions (rotary.hip).  v[set][part][2][n]: the products of up to ROT_ENTRIES entries of the tables under the moduli ma, mb, in coefficients
 #define ROT_ENTRIES 64
 struct RotEntry {
@@ -322,6 +327,9 @@ void ks_many_tables_destroy(KsManyTables *t);
 // (through the Galois map g if g != 0); ksin: m*(level+1) limbs of scratch
 cm_status ks_raise_many(cm_ctx *ctx, const KsManyTables &t, const u64 *cts, u64 *ksin, u64 *digits, hipStream_t st,
                         int m = -1, u64 g = 0, bool half = false);
+// n = 65536: the same of the second components of ciphertexts that lie apart (cts[k] [2][level+1][n]).  The digits' own limbs are not copied: weighted
+// rotations read them where they are.
+cm_status ks_raise_apart(cm_ctx *ctx, const KsManyTables &t, const u64 *const *cts, u64 *ksin, u64 *digits, hipStream_t st, int m, bool half = false);
 // outs[r][2][level+1][n] = ModDown(us + r*2*ext*n) for r < cnt (any cnt; runs in batches); special limbs of us are overwritten
 // second components only: outs[r] + (level+1)*n <- ModDown(us[r][1]); the first components of us (all their limbs)
 // and of outs are left as they are

@@ -2126,6 +2126,23 @@ void launch_ntt_src(cm_ctx *ctx, u64 *data, const int *d_rows, const u64 *src, c
         hipLaunchKernelGGL(ntt_full_inv, grid, full, 0, st, data, src, d_src_rows, d_rows, d_mod_idx, t, n, (unsigned)g, fi);
     }
 }
+// data[z][limbs][n] = the coefficients of the second components of b.c[z] ([2][limbs][n]), z < m; d_mods: 0 .. limbs - 1 for each
+__global__ __launch_bounds__(SMALL_THREADS) void small_rows_inv_seconds(u64 *__restrict__ data, SecondBatch b, int limbs, NttTables t, int n) {
+    __shared__ u64 lds[SMALL_CHUNK + SMALL_CHUNK / 16];
+    const int per = n / SMALL_CHUNK, limb = blockIdx.x / per, chunk = blockIdx.x % per, z = limb / limbs, mi = limb % limbs;
+    u64 *p = data + (size_t)limb * n + (size_t)chunk * SMALL_CHUNK;
+    const u64 *src = b.c[z] + (size_t)(limbs + mi) * n;
+    if (t.fpq[mi].q != 0.0) small_rows_inv_body<FpArith>(lds, p, src, 0, t, mi, n, chunk, limb, FoldIn());
+    else small_rows_inv_body<IntArith>(lds, p, src, 0, t, mi, n, chunk, limb, FoldIn());
+}
+void launch_seconds_inv(cm_ctx *ctx, u64 *data, const SecondBatch &b, int m, int limbs, const int *d_mods, hipStream_t st) {
+    {
+        Prof prof_(ctx, CM_K_NTT_INV, 0, st);              // the limbs are counted with their second pass
+        hipLaunchKernelGGL(small_rows_inv_seconds, dim3(m * limbs * (ctx->n / SMALL_CHUNK)), dim3(SMALL_THREADS), 0, st, data, b, limbs,
+                           tables_of(ctx, true, m * limbs), ctx->n);
+    }
+    launch_cols_inv(ctx, data, nullptr, d_mods, m * limbs, st);
+}
 // the second pass of an inverse transform whose row pass is done (launch_rows_ip)
 void launch_cols_inv(cm_ctx *ctx, u64 *data, const int *d_rows, const int *d_mod_idx, int limbs, hipStream_t st) {
     if (limbs <= 0) return;

@@ -671,6 +671,19 @@ cm_status ks_raise_many(cm_ctx *ctx, const KsManyTables &t, const u64 *cts, u64 
     return CM_OK;
 }
 
+cm_status ks_raise_apart(cm_ctx *ctx, const KsManyTables &t, const u64 *const *cts, u64 *ksin, u64 *digits, hipStream_t st, int m, bool half) {
+    if (m < 1 || m > t.cnt || m > CM_KS_BATCH || ctx->n != 65536) return CM_E_INVAL;
+    const KsLevelFull &k = ks_level_full(ctx, t.level);
+    SecondBatch b;
+    for (int z = 0; z < CM_KS_BATCH; z++) b.c[z] = cts[z < m ? z : 0];
+    launch_seconds_inv(ctx, ksin, b, m, t.level + 1, t.d_in_mods, st);
+    ConvBatch cb;
+    cb.tabs = k.d_modup, cb.batch = m * k.beta, cb.tab_step = 1, cb.ns = ctx->alpha, cb.max_nt = k.modup_max_nt, cb.tab_period = k.beta, cb.in_group = k.beta;
+    cb.in_stride = (size_t)(t.level + 1) * ctx->n, cb.out_stride = (size_t)k.ext * ctx->n, cb.half = half, cb.near = k.near_up && k.pays_up;
+    launch_conv_ntt(ctx, cb, digits, ksin, st, t.d_ntt_rows, t.d_ntt_mods, m * t.n_ntt);
+    return CM_OK;
+}
+
 // cnt hoisted rotations of one ciphertext `in` ([2][level+1][n]) whose raised digits are given:
 // outs[r] = ModDown(sum_j perm_{g_r}(digits_j) * key_r) + perm_{g_r}(in.c0).  The ModDown of up to
 // CM_KS_BATCH rotations runs as one batch so that its transforms and conversions fill the machine.

@@ -60,9 +60,6 @@ __global__ __launch_bounds__(ROT_TPB) void k_rotary_products(u64 *__restrict__ v
     if (parts == 3) out[2 * poly] = dn;
 }
 // out[z][limbs][n] = the second components of b.c[z]
-struct SecondBatch {
-    const u64 *c[CM_KS_BATCH];
-};
 __global__ __launch_bounds__(ROT_TPB) void k_second(u64 *__restrict__ out, SecondBatch b, int limbs, int n) {
     const size_t i = blockIdx.x * ROT_TPB + threadIdx.x, at = (size_t)blockIdx.y * n + i;
     out[(size_t)blockIdx.z * limbs * n + at] = b.c[blockIdx.z][(size_t)limbs * n + at];
@@ -73,7 +70,7 @@ __global__ __launch_bounds__(ROT_TPB) void k_second(u64 *__restrict__ out, Secon
 // words, the sums reduced and multiplied by the item's plaintext.  All loads of an item are requested before the first is used (NB bounds its
 // digits); one word a lane at n = 4096, where a launch is as long as a lane's chain.
 template <bool SA, int NB, int W>
-__global__ __launch_bounds__(ROT_TPB) void k_weighted(WrBatch b, const ModC *__restrict__ modc, int beta, int ext, int level, int L, int nmod, int n,
+__global__ __launch_bounds__(ROT_TPB) void k_weighted(WrBatch b, const ModC *__restrict__ modc, int beta, int ext, int level, int alpha, int L, int nmod, int n,
                                                       int logn, const u64 *__restrict__ pmont, EvkA eva, const u64 *__restrict__ ubound) {
     typedef u64 words __attribute__((ext_vector_type(W)));
     const unsigned i0 = (blockIdx.x * ROT_TPB + threadIdx.x) * W;
@@ -81,6 +78,7 @@ __global__ __launch_bounds__(ROT_TPB) void k_weighted(WrBatch b, const ModC *__r
     const ModC m = modc[mi];
     const size_t o = (size_t)r * n + i0;
     const u64 bound = ubound[mi], pm = r <= level ? pmont[r] : 0;
+    const int own = r <= level ? r / alpha : -1;
     u64 r0[W] = {}, r1[W] = {};
     auto mul = [&](u64 x, u64 y) { return redc((u128)x * y, m.q, m.qinv); };
     auto load = [](const u64 *p) { return *reinterpret_cast<const words *>(p); };
@@ -106,7 +104,7 @@ __global__ __launch_bounds__(ROT_TPB) void k_weighted(WrBatch b, const ModC *__r
         for (int j = 0; j < NB; j++)
             if (j < beta) {
                 const size_t at = ((size_t)j * nmod + mi) * n + i0;
-                d[j] = load(it.dig + ((size_t)j * ext + r) * n + base);
+                d[j] = load((j == own ? it.c + (size_t)(level + 1 + r) * n : it.dig + ((size_t)j * ext + r) * n) + base);
                 e[j] = __builtin_nontemporal_load(reinterpret_cast<const words *>(it.key + at));
                 if (!SA) sk[j] = it.key[(size_t)eva.kdig * nmod * n + (size_t)j * nmod + mi];
             }
@@ -139,7 +137,7 @@ static void launch_weighted_words(cm_ctx *ctx, const WrBatch &b, int beta, int l
     const int ext = level + 1 + ctx->K;
     const dim3 grid(ctx->n / (W * ROT_TPB), ext, b.nz);
 #define WEIGHTED(SA_, NB_)                                                                                                                                     \
-    hipLaunchKernelGGL((k_weighted<SA_, NB_, W>), grid, dim3(ROT_TPB), 0, st, b, ctx->d_modc, beta, ext, level, ctx->L, ctx->nmod, ctx->n, ctx->logn, ctx->d_pmont, \
+    hipLaunchKernelGGL((k_weighted<SA_, NB_, W>), grid, dim3(ROT_TPB), 0, st, b, ctx->d_modc, beta, ext, level, ctx->alpha, ctx->L, ctx->nmod, ctx->n, ctx->logn, ctx->d_pmont, \
                        evk_a_of(ctx), ctx->d_ubound)
     if (ctx->evk_stored_a) {
         if (beta <= 4) WEIGHTED(true, 4);
@@ -362,15 +360,19 @@ cm_status rotary_sums(cm_ctx *ctx, const cm_evk *evk, const cm_rotary *r, int m,
         g[s] = (unsigned)galois_of_step(ctx, s ? -r->step : r->step), keys[s] = find_key(evk, g[s]);
         if (!keys[s]) return CM_E_NOKEY;
     }
-    const u64 *d = xs[0] + ln;
-    if (m > 1) {
-        SecondBatch b;
-        for (int z = 0; z < CM_KS_BATCH; z++) b.c[z] = xs[z < m ? z : 0];
-        hipLaunchKernelGGL(k_second, dim3(n / ROT_TPB, level + 1, m), dim3(ROT_TPB), 0, st, second, b, level + 1, (int)n);
-        d = second;
-    }
     const bool half = weighted_rows(ctx, kl.beta, level, r->parts - 1, m * sets);
-    CMCHK(ks_raise_many(ctx, r->tabs, d, ksin, digits, st, m, 0, half));
+    if (n == 65536) {
+        CMCHK(ks_raise_apart(ctx, r->tabs, xs, ksin, digits, st, m, half));
+    } else {
+        const u64 *d = xs[0] + ln;
+        if (m > 1) {
+            SecondBatch b;
+            for (int z = 0; z < CM_KS_BATCH; z++) b.c[z] = xs[z < m ? z : 0];
+            hipLaunchKernelGGL(k_second, dim3(n / ROT_TPB, level + 1, m), dim3(ROT_TPB), 0, st, second, b, level + 1, (int)n);
+            d = second;
+        }
+        CMCHK(ks_raise_many(ctx, r->tabs, d, ksin, digits, st, m));
+    }
     *rows_done = half;
     WrBatch b;
     b.nz = m * sets, b.nsum = r->parts - 1;

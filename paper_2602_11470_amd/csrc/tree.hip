@@ -26,7 +26,7 @@ struct cm_tree {
     u64 *d_one = nullptr;                     // [level][n]: the mask's value at row 0, residue 0
     u64 *d_unseen = nullptr;                  // [E - 1][level][n]: entry m - 1: in the rows m .. E - 1
     u64 *d_work = nullptr;
-    KsManyTables tabs;                        // raise of the second components of CM_KS_BATCH results
+    KsManyTables tabs, q_tabs;                // raise of the second components of CM_KS_BATCH results, of the query's
     KvPasses passes;                          // for caches with the creating one's baby steps; others' passes run one at a time
 };
 
@@ -61,7 +61,7 @@ __global__ __launch_bounds__(256) void k_add_dropped(u64 *__restrict__ out, cons
 
 extern "C" void cm_tree_destroy(cm_tree *tr) {
     if (!tr) return;
-    ks_many_tables_destroy(&tr->tabs);
+    ks_many_tables_destroy(&tr->tabs), ks_many_tables_destroy(&tr->q_tabs);
     kv_passes_destroy(&tr->passes);
     hipFree(tr->d_q), hipFree(tr->d_v), hipFree(tr->d_one), hipFree(tr->d_unseen), hipFree(tr->d_work);
     delete tr;
@@ -100,6 +100,7 @@ extern "C" cm_status cm_tree_create(cm_ctx *ctx, const cm_kv *kv, int32_t group,
         get(&tr->d_work, tree_work_words(ctx, level));
         if (status == CM_OK && hipMalloc((void **)&d_mods, CM_MAX_LIMBS * 4) != hipSuccess) status = CM_E_NOMEM;
         if (status == CM_OK) status = ks_many_tables_create(ctx, level - 1, CM_KS_BATCH, &tr->tabs, 2, 1);
+        if (status == CM_OK) status = ks_many_tables_create(ctx, level + 1, 1, &tr->q_tabs, 2, 1);
         // a plaintext on `limbs` limbs, the special ones of a level among them (mont), or the first ones alone
         auto put = [&](u64 *dst, const int64_t *c, int limbs, int lv, bool mont) {
             if (status != CM_OK) return;
@@ -211,7 +212,8 @@ extern "C" cm_status cm_tree_qk(cm_ctx *ctx, const cm_evk *evk, const cm_tree *t
     const KsLevel &up = ks_level(ctx, lv + 1);
     const size_t ctw = kv_ctw(kv);
     u64 *digits = tr->d_work, *x = digits + (size_t)up.beta * up.ext * n, *tmp = x + CM_KS_BATCH * ctw, *us = arena_batch_sums(ctx);
-    if (t > 1) CMCHK(ks_raise(ctx, q->dev + (size_t)(lv + 2) * n, lv + 1, digits, st));
+    if (t > 1 && n == 65536) CMCHK(ks_raise_apart(ctx, tr->q_tabs, &q->dev, x, digits, st, 1));
+    else if (t > 1) CMCHK(ks_raise(ctx, q->dev + (size_t)(lv + 2) * n, lv + 1, digits, st));
     const u64 *unseen = nullptr;
     unsigned gu = 0;
     {
@@ -315,7 +317,8 @@ extern "C" cm_status cm_tree_sv(cm_ctx *ctx, const cm_evk *evk, const cm_tree *t
             }
         }
         if (m == skip) continue;
-        CMCHK(ks_raise_many(ctx, tr->tabs, parts, ksin, digits, st, m - skip));
+        if (n == 65536) CMCHK(ks_raise_apart(ctx, tr->tabs, to + skip, ksin, digits, st, m - skip));
+        else CMCHK(ks_raise_many(ctx, tr->tabs, parts, ksin, digits, st, m - skip));
         WrBatch b;
         b.nz = 1, b.nsum = 2 * (m - skip);
         for (int z = skip; z < m; z++)
