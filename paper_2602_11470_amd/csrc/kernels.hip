@@ -408,7 +408,7 @@ bool tensor_sum_passes_pays(int n, int limbs, int cnt, int groups, int passes) {
     return groups == 1 ? cnt >= 16 : cnt >= 4 || groups <= 4;
 }
 bool tensor_sum_passes_fits(const cm_ctx *ctx, int cnt, int groups, int limbs, int passes) {
-    if ((passes != 2 && passes != TS_PASSES) || cnt > TS_MAX_CNT) return false;
+    if ((passes != 2 && passes != TS_PASSES && passes != TS_WIDE) || cnt > TS_MAX_CNT) return false;
     for (int l = 0; l < limbs; l++)
         if (ctx->mod[l] >= (1ULL << 50)) return false;
     return tensor_sum_passes_pays(ctx->n, limbs, cnt, groups, passes);
@@ -417,6 +417,10 @@ void launch_tensor_sum_passes(cm_ctx *ctx, u64 *out, size_t out_pass, const u64 
                               int limbs, hipStream_t st, int gs, int ts) {
     Prof prof_(ctx, CM_K_ELEMENTWISE, 3 * limbs * groups * passes, st);
     const dim3 grid(ctx->n / TS_CO, limbs);
+    if (passes == TS_WIDE) {
+        hipLaunchKernelGGL(k_tensor_sum_passes<TS_WIDE>, grid, dim3(64 * TS_WIDE), 0, st, out, a, b, ctx->d_fpq, limbs, ctx->n, cnt, groups, gs, ts, out_pass, a_pass);
+        return;
+    }
     if (passes == 2)
         hipLaunchKernelGGL(k_tensor_sum_passes<2>, grid, dim3(128), 0, st, out, a, b, ctx->d_fpq, limbs, ctx->n, cnt, groups, gs, ts, out_pass, a_pass);
     else

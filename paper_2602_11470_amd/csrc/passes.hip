@@ -27,14 +27,16 @@ void launch_copies(u64 *const *dst, const u64 *const *src, int m, size_t words, 
 
 // Rotations of several ciphertexts by the same steps, before their ModDown: out[a][p] = sum_j sigma_a(dig_p,j) key_a,j for `per` keys a
 // a workgroup and PS_GROUP passes p.  As in k_inner_product_fanout a lane keeps the digit words of two source positions and writes each result
-// where the key's Galois map sends them; here it keeps those of PS_GROUP passes, so a key's words are read and drawn once for all.
+// where the key's Galois map sends them; here it keeps those of PS_GROUP passes, so a key's words are read and drawn once for all.  seconds
+// (nullable): the polynomials that were raised, `stride` words apart, where a digit's own limbs are read.
 struct FanPasses {
     int n, per;                         // keys, of a workgroup
     const u64 *key[PS_KEYS];
     unsigned ginv[PS_KEYS];
 };
 template <bool SA, int NB>
-__global__ __launch_bounds__(PS_TPB) void k_fan_passes(FanPasses f, u64 *__restrict__ out, const u64 *__restrict__ dig, int passes, const ModC *__restrict__ modc,
+__global__ __launch_bounds__(PS_TPB) void k_fan_passes(FanPasses f, u64 *__restrict__ out, const u64 *__restrict__ dig, const u64 *__restrict__ seconds,
+                                                       size_t stride, int alpha, int passes, const ModC *__restrict__ modc,
                                                        int beta, int ext, int level, int L, int nmod, int n, int logn, EvkA eva, const u64 *__restrict__ ubound) {
     const int chunks = (f.n + f.per - 1) / f.per;
     const unsigned s2 = (blockIdx.x * PS_TPB + threadIdx.x) * 2;
@@ -43,13 +45,18 @@ __global__ __launch_bounds__(PS_TPB) void k_fan_passes(FanPasses f, u64 *__restr
     const ModC m = modc[mi];
     const u64 bound = ubound[mi];
     const bool small = m.q < (1ULL << 50);
+    const int own = r <= level ? r / alpha : -1;
     const size_t dblk = (size_t)beta * ext * n, ublk = 2 * (size_t)ext * n;
     ulonglong2 d[PS_GROUP][NB];
 #pragma unroll
     for (int p = 0; p < PS_GROUP; p++)
 #pragma unroll
         for (int j = 0; j < NB; j++)
-            if (j < beta) d[p][j] = *reinterpret_cast<const ulonglong2 *>(dig + min(p0 + p, passes - 1) * dblk + ((size_t)j * ext + r) * n + s2);
+            if (j < beta) {
+                const int q = min(p0 + p, passes - 1);
+                const u64 *w = seconds && j == own ? seconds + q * stride + (size_t)r * n : dig + q * dblk + ((size_t)j * ext + r) * n;
+                d[p][j] = *reinterpret_cast<const ulonglong2 *>(w + s2);
+            }
     for (int a = first; a < end; a++) {
         const unsigned dst = perm_src(s2, f.ginv[a], logn), base = dst & ~1u;
         const bool swap = dst & 1u;
@@ -91,12 +98,12 @@ __global__ __launch_bounds__(PS_TPB) void k_fan_passes(FanPasses f, u64 *__restr
         }
     }
 }
-static void launch_fan_passes(cm_ctx *ctx, const FanPasses &f, u64 *out, const u64 *dig, int passes, int beta, int level, hipStream_t st) {
+static void launch_fan_passes(cm_ctx *ctx, const FanPasses &f, u64 *out, const u64 *dig, const u64 *seconds, size_t stride, int passes, int beta, int level, hipStream_t st) {
     Prof prof_(ctx, CM_K_INNER_PRODUCT, f.n * passes, st);
     const int ext = level + 1 + ctx->K;
     const dim3 grid(ctx->n / (2 * PS_TPB), ext, (f.n + f.per - 1) / f.per * ((passes + PS_GROUP - 1) / PS_GROUP));
 #define FANP(SA_, NB_)                                                                                                                                  \
-    hipLaunchKernelGGL((k_fan_passes<SA_, NB_>), grid, dim3(PS_TPB), 0, st, f, out, dig, passes, ctx->d_modc, beta, ext, level, ctx->L, ctx->nmod, ctx->n, \
+    hipLaunchKernelGGL((k_fan_passes<SA_, NB_>), grid, dim3(PS_TPB), 0, st, f, out, dig, seconds, stride, ctx->alpha, passes, ctx->d_modc, beta, ext, level, ctx->L, ctx->nmod, ctx->n, \
                        ctx->logn, evk_a_of(ctx), ctx->d_ubound)
     if (ctx->evk_stored_a) {
         if (beta <= 2) FANP(true, 2);
@@ -118,9 +125,9 @@ void kv_passes_create(cm_ctx *ctx, const cm_kv *kv, int passes, KvPasses *kp) {
     if (passes < 2 || kv->r_o > 8 || kl.beta > 6) return;
     const size_t n = ctx->n, ctw = kv_ctw(kv), ln = ctw / 2, dblk = (size_t)kl.beta * kl.ext * n, ublk = 2 * (size_t)kl.ext * n;
     ks_batches_grow(ctx);
-    kp->P = std::min(passes, CM_KS_BATCH * kv->r_o <= CM_MASK_BATCH ? CM_KS_BATCH : PS_GROUP), kp->r_i = kv->r_i, kp->r_o = kv->r_o, kp->level = kv->level;
+    kp->P = std::min(passes, CM_KS_BATCH), kp->r_i = kv->r_i, kp->r_o = kv->r_o, kp->level = kv->level;
     // a turn's relinearisations at once where their digits stay below 1 GB
-    kp->D = std::max<int>(kp->P, (int)std::min<size_t>(kp->P * kv->r_o, ((size_t)1 << 30) / (dblk * 8)));
+    kp->D = std::max<int>(kp->P, (int)std::min<size_t>(std::min(kp->P * kv->r_o, CM_MASK_BATCH), ((size_t)1 << 30) / (dblk * 8)));
     kp->B = std::min(kp->D, ks_batch_max(ctx, kv->level)), kp->G = std::max(1, kp->D / kp->P);
     const size_t words = kp->P * (kv->r_i * ctw + kv->r_o * (3 * ln + ctw) + 2 * ublk) + kp->D * (ln + dblk);
     bool ok = hipMalloc((void **)&kp->babies, words * 8) == hipSuccess;
@@ -144,7 +151,11 @@ cm_status kv_passes_run(cm_ctx *ctx, const cm_evk *evk, const cm_kv *kv, const K
     u64 *us = arena_batch_sums(ctx);
     // rotations by rows: keys in groups whose results one ModDown takes
     if (r_i > 1) {
-        CMCHK(ks_raise_many(ctx, kp.baby_tabs, kp.babies, kp.ksin, kp.digits, st, m));
+        const bool apart = n == 65536;                 // the digits' own limbs are read where they are
+        const u64 *first[CM_KS_BATCH];
+        for (int p = 0; p < m; p++) first[p] = kp.babies + p * r_i * ctw;
+        if (apart) CMCHK(ks_raise_apart(ctx, kp.baby_tabs, first, kp.ksin, kp.digits, st, m));
+        else CMCHK(ks_raise_many(ctx, kp.baby_tabs, kp.babies, kp.ksin, kp.digits, st, m));
         const int most = std::max(1, std::min({ks_batch_max(ctx, lv) / m, PS_KEYS, CM_MASK_BATCH / m}));
         for (int j0 = 1; j0 < r_i; j0 += most) {
             FanPasses f;
@@ -157,7 +168,7 @@ cm_status kv_passes_run(cm_ctx *ctx, const cm_evk *evk, const cm_kv *kv, const K
                 for (int p = 0; p < m && a < f.n; p++)
                     gs[a * m + p] = g, adds[a * m + p] = kp.babies + p * r_i * ctw, to[a * m + p] = kp.babies + (p * r_i + j0 + a) * ctw;
             }
-            launch_fan_passes(ctx, f, us, kp.digits, m, kl.beta, lv, st);
+            launch_fan_passes(ctx, f, us, kp.digits, apart ? kp.babies + ln : nullptr, r_i * ctw, m, kl.beta, lv, st);
             CMCHK(moddown_batch_turned(ctx, us, lv, f.n * m, adds, 1, gs, to, st));
         }
     }
@@ -166,7 +177,7 @@ cm_status kv_passes_run(cm_ctx *ctx, const cm_evk *evk, const cm_kv *kv, const K
     for (int p = 0; p < m;) {
         u64 *sum = kp.sums + p * r_o * 3 * ln;
         const u64 *a = kp.babies + p * r_i * ctw;
-        const int joint = m - p >= TS_PASSES ? TS_PASSES : m - p >= 2 ? 2 : 1;
+        const int joint = m - p >= TS_WIDE ? TS_WIDE : m - p >= TS_PASSES ? TS_PASSES : m - p >= 2 ? 2 : 1;
         if (joint > 1 && tensor_sum_passes_fits(ctx, r_i, r_o, limbs, joint)) {
             launch_tensor_sum_passes(ctx, sum, r_o * 3 * ln, a, r_i * ctw, joint, array, r_i, r_o, limbs, st, gs, ts);
             p += joint;
