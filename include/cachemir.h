@@ -511,8 +511,8 @@ cm_status cm_inner_rot_create(cm_ctx *ctx, int32_t t, int32_t delta, int32_t lev
  * token stands at which residue, and at which position, is said by cm_rotary_set, which only enqueues kernels; so one object serves every
  * step, layer (of one level) and tree of drafts.
  * What is turned: the first rot_dims dims of a head (even, 2 .. dim; the others leave as they are); pairs of neighbours (2m, 2m+1), or with
- * CM_ROTARY_HALVES (m, rot_dims/2 + m): at position p by p freq[m] (host, rot_dims/2 of them; null: 10000^(-2m/rot_dims)), cosines and sines
- * times gain.  Residues without a token come out zero, whatever partial sums a projection left there; so do no other slots.
+ * CM_ROTARY_HALVES (m, rot_dims/2 + m): at position p by p freq[m] (host, rot_dims/2 of them, times room below 2^53 in size, else CM_E_INVAL; null:
+ * 10000^(-2m/rot_dims)), cosines and sines times gain.  Residues without a token come out zero, whatever partial sums a projection left there.
  * room: positions 0 .. room - 1 (at most 2^24) can be set.  level: of the ciphertexts to turn; they come out one below, their scale kept.  The
  * special moduli have to be above 2.1 gain q_level (else CM_E_INVAL).
  * coeffs (nullable, host [cm_rotary_polys(room)][n]): integer coefficients of the tables.  With position = R high + low (R the power of two at or
@@ -544,7 +544,8 @@ int32_t cm_rotary_steps(const cm_rotary *rotary, int32_t *steps, int32_t cap);
 enum { CM_ROTARY_PLAIN = 0, CM_ROTARY_LINEAR = 1, CM_ROTARY_BASE = 2, CM_ROTARY_BANDS = 3 };
 cm_status cm_rotary_freqs(int32_t rot_dims, double base, int32_t scaling, const double *par, double *out);
 /* pos: host [t] (t = S / (heads dim), heads padded), the position of the token at every residue, -1 where there is none (read before the call
- * returns); outside -1 .. room - 1: CM_E_LAYOUT.  Enqueued: calls on the object that follow on the stream see it.  split: the residues below it belong
+ * returns); outside -1 .. room - 1: CM_E_LAYOUT.  Enqueued: calls on the object that follow on the stream see it (a captured call sees what is set when
+ * it is replayed; a captured cm_kv_append_run that passes into the next page needs the split it was captured with).  split: the residues below it belong
  * to the next page (cm_kv_append_run); 0: there is none.  cm_rotary_apply does not look at it. */
 cm_status cm_rotary_set(cm_ctx *ctx, cm_rotary *rotary, const int32_t *pos, int32_t split, void *stream);
 /* y[i] = x[i] turned, i < count <= CM_ROTARY_MAX (the queries and keys of a token, a group, a tree).  No y may share memory with an x or another y

@@ -214,7 +214,7 @@ extern "C" cm_status cm_rotary_create(cm_ctx *ctx, int32_t heads, int32_t dim, i
     if (heads > S || dim > S || rot_dims > dim) return CM_E_LAYOUT;
     while (!rot_pow2(heads)) heads++;          // a head count that is not a power of two is padded to the next one
     if (!rot_pow2(dim) || (long long)heads * dim > S) return CM_E_LAYOUT;
-    for (int m = 0; freq && m < rot_dims / 2; m++) if (!isfinite(freq[m])) return CM_E_INVAL;
+    for (int m = 0; freq && m < rot_dims / 2; m++) if (!(fabs(freq[m]) * room < 0x1p53)) return CM_E_INVAL;
     // the plaintexts' coefficients are at most gain q_level in size: below half of the first special modulus, which they are rounded under, and
     // below the signed words of the encoding
     const double q = (double)ctx->mod[level], top = fmax(gain, 1.0) * q;

@@ -20,7 +20,11 @@ def rings():
     from paper_2602_11470_amd import binding as B
     wide = params.Params(n=4096, q=params.scan_primes(58, 4096, 1) + params.scan_primes(54, 4096, 5), p=params.scan_primes(60, 4096, 2), alpha=2, scale=2.0 ** 50,
                          hamming=0, name="wide")
-    make = {"small": (B.config1, params.config1), "wide": (lambda: B.Context(4096, 6, 2, 2, 58, 54, 60, 2.0 ** 50), lambda: wide), "big": (B.llama_ring, None)}
+    # ten digits of one prime; seven special primes (no ModDown and rescale in one, no third way of raising)
+    digits = lambda: params.toy(n_qi=9)  # noqa: E731
+    special = lambda: params.Params(n=4096, q=params.scan_primes(50, 4096, 8), p=params.scan_primes(60, 4096, 7), alpha=4, scale=2.0 ** 50, hamming=0, name="special")  # noqa: E731
+    make = {"digits": (lambda: B.Context(4096, 10, 1, 1, 50, 40, 60, 2.0 ** 40), digits), "special": (lambda: B.Context(4096, 8, 7, 4, 50, 50, 60, 2.0 ** 50), special),
+            "small": (B.config1, params.config1), "wide": (lambda: B.Context(4096, 6, 2, 2, 58, 54, 60, 2.0 ** 50), lambda: wide), "big": (B.llama_ring, None)}
     made = {}
 
     def get(name):
@@ -88,7 +92,8 @@ def _status(call):
 # ring, heads, dim, level, rot, halves, gain, room, ciphertexts
 ROTARY = [("small", 4, 16, 2, 16, True, 1.0, 60, 1), ("small", 4, 16, 4, 16, False, 1.0, 37, 3), ("small", 3, 32, 1, 8, True, 1.3, 20, 2),
           ("small", 1, 2, 2, 2, False, 1.0, 5, 1), ("small", 8, 256, 3, 64, False, 0.25, 1, 2), ("wide", 4, 64, 5, 32, True, 1.0, 50, 2),
-          ("wide", 16, 16, 3, 16, True, 1.0, 9, 9)]
+          ("wide", 16, 16, 3, 16, True, 1.0, 9, 9), ("digits", 8, 32, 8, 32, False, 1.0, 12, 2), ("special", 8, 32, 6, 16, False, 1.0, 12, 3),
+          ("special", 8, 32, 2, 32, True, 1.0, 5, 1)]
 
 
 @pytest.mark.parametrize("case", ROTARY, ids=str)
@@ -192,6 +197,7 @@ def test_rotary_refusals(rings, keysets):
     assert create() == 0 and create(freq=None) == 0 and create(rot=2, room=1) == 0
     assert create(heads=0) == create(dim=1) == create(rot=3) == create(rot=0) == create(gain=0.0) == create(gain=np.inf) == create(room=0) == create(flags=2) == -1
     assert create(room=(1 << 24) + 1) == create(gain=np.nan) == create(freq=np.array([np.nan] + [1.0] * 7)) == create(ctx=None) == -1
+    assert create(freq=np.full(8, 2.0 ** 49)) == create(freq=np.full(8, -np.inf)) == -1 and create(freq=np.full(8, -2.0 ** 48)) == 0      # 16 positions: 2^53
     assert create(gain=float(2 ** 19)) == -1                          # 2^19 q = 2^59, half of the special modulus
     assert create(level=0) == create(level=5) == -2
     assert create(rot=18) == create(dim=48, rot=16) == create(heads=256) == create(heads=4096, dim=2, rot=2) == -5
@@ -240,7 +246,8 @@ def test_rotary_refusals(rings, keysets):
 RUNS = [("small", 4, 16, 16, False, 2, 77, 1, ""), ("small", 4, 16, 4, True, 2, 90, 32, ""), ("small", 8, 32, 8, False, 2, 101, 6, "pairs"),
         ("small", 8, 32, 8, True, 2, 101, 8, "halves"), ("small", 8, 32, 32, False, 3, 248, 8, "halves"), ("small", 8, 32, 1, True, 2, 251, 5, "pairs"),
         ("small", 8, 256, 16, False, 2, 9, 1, "halves"), ("small", 3, 32, 16, False, 3, 13, 4, "pairs"), ("wide", 4, 64, 8, True, 3, 63, 2, "pairs"),
-        ("wide", 4, 64, 16, False, 4, 60, 8, "halves"), ("small", 1, 16, 16, False, 2, 100, 100, "halves")]
+        ("wide", 4, 64, 16, False, 4, 60, 8, "halves"), ("digits", 8, 32, 8, False, 7, 45, 7, "pairs"),
+        ("special", 8, 32, 8, False, 4, 45, 7, "pairs"), ("special", 8, 32, 4, True, 3, 45, 7, "halves"), ("small", 1, 16, 16, False, 2, 100, 100, "halves")]
 
 
 def _masks(gctx, kv, lay, level):
@@ -404,6 +411,8 @@ def test_append_run_refusals(rings, keysets):
 TREES = [("small", 8, 32, 1, 8, 3, "index", 101, [-1, 0, 0, 1, -1, 3], 0, 64), ("small", 8, 32, 2, 8, 3, "index", 101, [-1, 0, 0, 1, -1, 3], 3, 0),
          ("small", 16, 32, 4, 32, 3, "index unrolled", 16, [-1], 0, 16), ("small", 8, 128, 1, 16, 3, "index unrolled", 250, [-1, 0, 1, 2, 3, 3], 2, 128),
          ("small", 16, 128, 1, 16, 2, "index", 30, [-1, 0], 1, 0), ("small", 8, 16, 1, 4, 3, "", 13, [-1, 0, 1], 0, 0), ("small", 8, 16, 2, 16, 3, "unrolled", 16, [-1, -1, 1], 0, 0),
+         ("small", 8, 32, 1, 2, 3, "index unrolled", 40, [-1, 0, 1], 0, 0), ("digits", 8, 32, 1, 8, 7, "index unrolled", 40, [-1, 0, 1], 0, 0),
+         ("special", 8, 32, 2, 8, 5, "index unrolled", 40, [-1, 0, 1], 0, 0), ("special", 8, 32, 1, 16, 3, "index", 40, [-1, 0, 1], 0, 0),
          ("wide", 6, 32, 1, 8, 3, "index unrolled", 0, [-1, 0, 0, 1], 0, 0), ("wide", 4, 32, 16, 8, 2, "index", 511 - 16, [-1] * 17, 5, 0)]
 
 
@@ -548,6 +557,94 @@ def test_tree_refusals(rings, keysets):
     assert sv(at, evk=part[1]) == -4 and sv(at, kv=other) == -5 and sv(at, kv=lower) == -2 and sv(at[:-1] + [q]) == -2
     at[3].d.scale *= 2
     assert sv(at) == -3
+
+
+@pytest.mark.parametrize("ring, heads, dim, r_i, level", [("small", 8, 32, 8, 2), ("big", 64, 64, 16, 2)])
+def test_stored_key_halves_give_the_same_words(rings, ring, heads, dim, r_i, level):
+    """Keys with both halves stored (CM_OPT_EVK_STORED_A) go through kernels of their own."""
+    import torch
+    from paper_2602_11470_amd import binding as B
+    gctx, _ = rings(ring)
+    kv = gctx.kv_create(heads, dim, level, r_i=r_i, key_index=True, unrolled_ladders=True)
+    pairs, tree = [gctx.rotary(heads, dim, level + 2, 32, halves=h) for h in (False, True)], gctx.tree(kv)
+    t = tree.passes
+    sk = gctx.keygen_secret(1)
+    steps = kv.steps() + tree.steps() + pairs[0].steps() + pairs[1].steps()
+    gen = torch.Generator(device="cuda").manual_seed(3)
+
+    def uniform(words):
+        for i in range(words.shape[-2]):
+            words[..., i, :] = torch.empty(words.shape[:-2] + (gctx.n,), dtype=torch.int64, device="cuda").random_(0, int(gctx.moduli()[i]), generator=gen)
+
+    def ct(lv):
+        c = B.Ct(gctx, lv)
+        c.d.scale = gctx.scale
+        uniform(_words(c))
+        return c
+    x, k, v, q, weights = [ct(level + 2) for _ in range(3)], ct(level + 2), ct(level + 1), ct(level + 1), [ct(level) for _ in range(t)]
+    cache = [kv.words(w) for w in (B.CM_QK, B.CM_SV, B.CM_KV_INDEX)]
+    for w in cache:
+        uniform(w)
+    before, found = [w.clone() for w in cache], []
+    try:
+        for stored in (0, 1):
+            gctx.set_option(B.CM_OPT_EVK_STORED_A, stored)
+            keys = gctx.keygen_rotations(sk, steps, 2, with_relin=True)
+            out = []
+            for w, b in zip(cache, before):
+                w.copy_(b)
+            kv.set_tokens(2 * t + 1)
+            for r in pairs:
+                gctx.rotary_set(r, [i if i % 3 else -1 for i in range(t)])
+                out += gctx.rotary_apply(keys, r, x)
+            gctx.rotary_set(pairs[1], [-1] + [3] * 3 + [-1] * (t - 4))
+            kv.append_run(keys, k, v, 3, rotary=pairs[1])
+            out += gctx.tree_qk(keys, tree, kv, [-1, 0, 0], 2 * t + 1, q) + [gctx.tree_sv(keys, tree, kv, weights)]
+            found.append([_words(c).clone() for c in out] + [w.clone() for w in cache])
+            del keys
+    finally:
+        gctx.set_option(B.CM_OPT_EVK_STORED_A, 0)
+    assert all(torch.equal(a, b) for a, b in zip(*found))
+
+
+def test_a_drafting_step_on_the_full_ring(rings, keysets):
+    """64 heads of 64 dims: a prompt of nine tokens and five drafted ones appended with their positions, the scores and values of their queries."""
+    from oracle import packing
+    gctx, _ = rings("big")
+    H, E, level = 64, 64, 3
+    lay = packing.KvLayout(gctx.S, H, E, 16)
+    tables = packing.RotaryTables(gctx.S, H, E, 32, halves=True)
+    t, rng = lay.t, np.random.default_rng(1)
+    kv = gctx.kv_create(H, E, level, r_i=16, key_index=True, unrolled_ladders=True)
+    rotary, tree = gctx.rotary(H, E, level + 2, 32, halves=True), gctx.tree(kv)
+    keys = keysets("big", kv.steps() + tree.steps() + rotary.steps(), True)
+    enc = lambda slots, lv: _enc(rings, keys, "big", slots, lv, int(rng.integers(1 << 30)))[0]  # noqa: E731
+    K, V = np.zeros((2, lay.capacity, H, E))
+    parents, depth = [-1, 0, 0, 2, 1], [0, 1, 1, 2, 2]
+    place = 0
+    for positions in (range(8), [8], [9 + d for d in depth]):
+        ks, vs = 0.3 * rng.normal(size=(2, E, H, t))
+        at = [-1] * t
+        for i, p in enumerate(positions):
+            a = place + i
+            at[a % t] = p
+            K[a], V[a] = tables.turn(ks[:, :, a % t].T, p), vs[:, :, a % t].T
+        gctx.rotary_set(rotary, at, max(0, place % t + len(positions) - t))
+        kv.append_run(keys[1], enc(ks.reshape(-1), level + 2), enc(vs.reshape(-1), level + 1), len(positions), rotary=rotary)
+        place += len(positions)
+    assert place == 14 and kv.tokens() == 14
+    qs = 0.3 * rng.normal(size=(E, H, t))
+    scores = gctx.tree_qk(keys[1], tree, kv, parents, 9, enc(qs.reshape(-1), level + 1))
+    Kp, Vp = K.reshape(E, t, H, E), V.reshape(E, t, H, E)
+    s = 0.3 * rng.normal(size=(t, E, H, t))
+    want = np.zeros((E, H, t))
+    for d in range(t):
+        plain = np.einsum("chje,ehj->chj", Kp.transpose(0, 2, 1, 3), np.roll(qs, d, axis=2)) - 24.0 * packing.tree_hidden(lay, 1, parents, 9, 0, 0, d)
+        # scale 2^50: noise of 2^6 units a coefficient times the 64 products of a sum
+        assert np.abs(gctx.decrypt(keys[0], scores[d]).real.reshape(E, H, t) - plain).max() < TOL / 100
+        want += np.roll(np.einsum("chj,cjhe->ehj", s[d], Vp), -d, axis=2)
+    out = gctx.tree_sv(keys[1], tree, kv, [enc(s[d].reshape(-1), level) for d in range(t)])
+    assert out.level == 1 and np.abs(gctx.decrypt(keys[0], out).real.reshape(E, H, t) - want).max() < TOL / 100
 
 
 # ---- replayed, on other streams, together --------------------------------------------------------------------------------
