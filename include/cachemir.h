@@ -524,8 +524,8 @@ cm_status cm_inner_rot_create(cm_ctx *ctx, int32_t t, int32_t delta, int32_t lev
  *   y = rescale(ModDown(p0 P x + p_up Rot'(x, step) + p_dn Rot'(x, -step))),
  * Rot' the hoisted rotation in the extended basis (cm_rotate_hoisted before its ModDown), step = heads t or, halves, rot_dims/2 heads t slots; where
  * 2 step = S both rotations are one, with the plaintext [V_up + V_dn].
- * Device memory: 8 (R + high parts) polynomials of n words, 9 plaintexts, and the raised digits of up to eight ciphertexts (256 MB of
- * them at most, one at least). */
+ * Device memory: 8 R + 4 (high parts) polynomials of n words, up to 9 plaintexts on the extended basis, and the raised digits of up to eight ciphertexts
+ * (256 MB of them at most, one at least). */
 typedef struct cm_rotary cm_rotary;
 enum { CM_ROTARY_HALVES = 1 };
 #define CM_ROTARY_ROOM (1 << 24)
@@ -545,7 +545,8 @@ enum { CM_ROTARY_PLAIN = 0, CM_ROTARY_LINEAR = 1, CM_ROTARY_BASE = 2, CM_ROTARY_
 cm_status cm_rotary_freqs(int32_t rot_dims, double base, int32_t scaling, const double *par, double *out);
 /* pos: host [t] (t = S / (heads dim), heads padded), the position of the token at every residue, -1 where there is none (read before the call
  * returns); outside -1 .. room - 1: CM_E_LAYOUT.  Enqueued: calls on the object that follow on the stream see it (a captured call sees what is set when
- * it is replayed; a captured cm_kv_append_run that passes into the next page needs the split it was captured with).  split: the residues below it belong
+ * it is replayed; a captured cm_kv_append_run that passes into the next page needs the split it was captured with; a captured cm_rotary_set sets its
+ * positions again at every replay, while cm_kv_append_run checks those of the call made last).  split: the residues below it belong
  * to the next page (cm_kv_append_run); 0: there is none.  cm_rotary_apply does not look at it. */
 cm_status cm_rotary_set(cm_ctx *ctx, cm_rotary *rotary, const int32_t *pos, int32_t split, void *stream);
 /* y[i] = x[i] turned, i < count <= CM_ROTARY_MAX (the queries and keys of a token, a group, a tree).  No y may share memory with an x or another y
@@ -580,7 +581,10 @@ cm_status cm_kv_append_run(cm_ctx *ctx, const cm_evk *evk, cm_kv *kv, const cm_r
  * 2^61 (else CM_E_INVAL).  coeffs (nullable, host [2 (t_kv - 1) + 2][n]): the residues from 1, 2, .. t_kv - 1 on, scale q_{level+1}, the same at scale
  * q_{level-1} (the residues below are that scale in all slots, less these), the mask's value in slots (0, h, 0) and in slots (0, h, r), both at the scores' scale.
  * cm_tree_steps: the rotations needed beyond those of the cache's product (cm_kv_steps; of those only the steps that are multiples of t_kv).
- * The calls use the work areas of the cache and of the object.  No score may share memory with q or another score (CM_E_INVAL). */
+ * The calls use the work areas of the cache and of the object.  No score may share memory with q or another score (CM_E_INVAL).
+ * Device memory: 4 (t_kv - 1) plaintexts on the extended basis, dim polynomials, and for up to eight passes taken together their baby steps, tensor sums and
+ * digits (8 ciphertexts a baby step, 20 a giant step, up to 1 GB of digits; where that cannot be had or the cache has more than eight giant
+ * steps, the passes run one at a time, with the same results). */
 typedef struct cm_tree cm_tree;
 cm_status cm_tree_create(cm_ctx *ctx, const cm_kv *kv, int32_t group, double mask, double scale, const int64_t *coeffs, cm_tree **out);
 void cm_tree_destroy(cm_tree *tree);

@@ -173,7 +173,7 @@ struct WrBatch {
 };
 void launch_weighted(cm_ctx *ctx, const WrBatch &b, int beta, int level, hipStream_t st);
 // the same from half-transformed digits (ConvBatch::half), with the row pass of the inverse transform of the rows from inv_from on (0: none), as
-// launch_rows_ip; only where it applies (rows_weighted_fits)
+// launch_rows_ip; only where it applies (weighted_rows)
 void launch_rows_weighted(cm_ctx *ctx, const WrBatch &b, int beta, int level, hipStream_t st, int inv_from);
 #define IP_MULTI_KEYS 3
 struct IpKeys {
@@ -240,7 +240,7 @@ struct SecondBatch {
     const u64 *c[CM_KS_BATCH];
 };
 void launch_seconds_inv(cm_ctx *ctx, u64 *data, const SecondBatch &b, int m, int limbs, const int *d_mods, hipStream_t st);
-// Plaintexts of rotary positions (rotary.hip).  v[set][part][2][n]: the products of up to ROT_ENTRIES entries of the tables under the moduli ma, mb, in coefficients
+// Plaintexts of rotary positions (rotary.hip).  v[set][part][2][n]: the products of up to ROT_ENTRIES entries of the tables under the moduli ma, mb, in coefficients (n = 65536)
 #define ROT_ENTRIES 64
 struct RotEntry {
     unsigned short low, high;

@@ -342,7 +342,8 @@ bool tensor_sum_held(int n, int limbs, int cnt, int groups) {
 // The same sums for PASSES sets of ciphertexts a against one b: out[pass] and a[pass] stacked at out_pass and a_pass words.  A wave
 // owns a pass for 64 coefficients; the words of a group are staged in LDS for all of them, the next group's requested ahead.
 // Bound by HBM: with a launch a pass the cache was read once per pass of a grouped query.  Four passes over 128 ciphertexts of ten
-// limbs 4 x 317 -> 582 us, grouped-query attention at level 9 12860 -> 11640.  108 registers because the
+// limbs 4 x 317 -> 582 us, grouped-query attention at level 9 12860 -> 11640.  Eight (five limbs) 547 us, two launches of four 580: half of the traffic
+// by then are the passes' own ciphertexts and sums.  108 registers because the
 // terms are worked on four at a time (sched_barrier); left to itself the compiler spills 187 of 128.
 #define TS_CO 64
 template <int PASSES>

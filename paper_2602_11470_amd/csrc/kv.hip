@@ -407,7 +407,9 @@ extern "C" cm_status cm_kv_append_group(cm_ctx *ctx, const cm_evk *evk, cm_kv *k
 }
 
 
-// Sums of a mask's turns, one for each of up to RUN_MASKS outputs: out[z] = the entries begin[z] .. begin[z + 1] - 1 of mask[z] through their Galois maps
+// Sums of a mask's turns, one for each of up to RUN_MASKS outputs: out[z] = the entries begin[z] .. begin[z + 1] - 1 of mask[z] through their Galois maps.
+// Gathers from the caches: five tokens at six limbs 6 us of a call of 967, 21 tokens, two masks, eleven limbs 29 us of 1600.  All masks of a run in one launch:
+// at n = 4096 each would take the launch alone (3.7 us).  The call itself is bound by its masked rescales, as a single append is.
 #define RUN_TURNS 64
 #define RUN_MASKS 3
 struct MaskTurns {

@@ -945,7 +945,8 @@ __device__ __forceinline__ void rip_out(u64 *lds, u64 *out, const u64 (&x)[4], c
 }
 // SHARED: one key for all outputs (one item each, no Galois element): the wave runs over outputs z0 .. z1-1, draws the uniform half
 // of its key words once into LDS and keeps the twiddles.
-// WEIGHTED: every item's sum times its plaintext (w.pt), and here P c on top (WrBatch); an item ends its own sums.
+// WEIGHTED: every item's sum times its plaintext (w.pt), and here P c on top (WrBatch); an item ends its own sums.  Two ciphertexts at level 22, one rotation
+// each: 134 us for 27 limbs, the half-transformed digits read once (their row pass, written and read again, took 24 us more; weighted_rows).
 struct RipWeights {
     const u64 *pt[WR_ITEMS];
     const u64 *here[WR_OUTS], *c_here[WR_OUTS];

@@ -29,6 +29,8 @@ void launch_copies(u64 *const *dst, const u64 *const *src, int m, size_t words, 
 // a workgroup and PS_GROUP passes p.  As in k_inner_product_fanout a lane keeps the digit words of two source positions and writes each result
 // where the key's Galois map sends them; here it keeps those of PS_GROUP passes, so a key's words are read and drawn once for all.  seconds
 // (nullable): the polynomials that were raised, `stride` words apart, where a digit's own limbs are read.
+// Bound by its writes at n = 65536: four keys, eight passes, two digits, nine limbs 83 us (302 MB written, 3.7 TB/s), one digit, eight limbs 61 us (4.4).
+// Eight, four and two keys a workgroup are equal there; at n = 4096, where a launch is as long as a workgroup's chain, one key 11.9 us, eight 23.7.
 struct FanPasses {
     int n, per;                         // keys, of a workgroup
     const u64 *key[PS_KEYS];
@@ -126,7 +128,8 @@ void kv_passes_create(cm_ctx *ctx, const cm_kv *kv, int passes, KvPasses *kp) {
     const size_t n = ctx->n, ctw = kv_ctw(kv), ln = ctw / 2, dblk = (size_t)kl.beta * kl.ext * n, ublk = 2 * (size_t)kl.ext * n;
     ks_batches_grow(ctx);
     kp->P = std::min(passes, CM_KS_BATCH), kp->r_i = kv->r_i, kp->r_o = kv->r_o, kp->level = kv->level;
-    // a turn's relinearisations at once where their digits stay below 1 GB
+    // a turn's relinearisations at once where their digits stay below 1 GB.  Eight passes over (16, 8) at level 4, 32, 16 and 8 in a batch: 5162, 5242 and
+    // 5405 us, at level 3 3811, 3844 and 3953; ModDowns of the rotations by rows in batches of 32, 16 and 8: 5162, 5273 and 5389
     kp->D = std::max<int>(kp->P, (int)std::min<size_t>(std::min(kp->P * kv->r_o, CM_MASK_BATCH), ((size_t)1 << 30) / (dblk * 8)));
     kp->B = std::min(kp->D, ks_batch_max(ctx, kv->level)), kp->G = std::max(1, kp->D / kp->P);
     const size_t words = kp->P * (kv->r_i * ctw + kv->r_o * (3 * ln + ctw) + 2 * ublk) + kp->D * (ln + dblk);
@@ -172,7 +175,7 @@ cm_status kv_passes_run(cm_ctx *ctx, const cm_evk *evk, const cm_kv *kv, const K
             CMCHK(moddown_batch_turned(ctx, us, lv, f.n * m, adds, 1, gs, to, st));
         }
     }
-    // products with the cache, four passes at a time
+    // products with the cache: eight passes over 128 ciphertexts of five limbs in one launch 547 us, four at a time 580
     const int gs = array == kv->d_x ? 1 : r_i, ts = array == kv->d_x ? r_o : 1;
     for (int p = 0; p < m;) {
         u64 *sum = kp.sums + p * r_o * 3 * ln;
@@ -202,7 +205,7 @@ cm_status kv_passes_run(cm_ctx *ctx, const cm_evk *evk, const cm_kv *kv, const K
             ip.it[r].dig = kp.digits + r * dblk, ip.it[r].key = relin, ip.it[r].own = adds[r] + 2 * ln, ip.out[r] = us + r * ublk;
         }
         if (half) launch_rows_ip(ctx, ip, kl.beta, lv, st, lv + 1);
-        else if (n == 4096) launch_inner_product_batch(ctx, ip, kl.beta, lv, st);       // lanes that walk over all items are too few to fill the chip
+        else if (n == 4096) launch_inner_product_batch(ctx, ip, kl.beta, lv, st);       // lanes that walk over 32 items do not fill the chip: 70 us, 12 apart
         else launch_inner_product_shared_key(ctx, ip, kl.beta, lv, st);
         CMCHK(moddown_batch_into(ctx, us, lv, cnt, adds, 2, 0, nullptr, to, st, half));
     }
