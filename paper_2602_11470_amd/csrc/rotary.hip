@@ -74,11 +74,14 @@ __global__ __launch_bounds__(ROT_TPB) void k_second(u64 *__restrict__ out, Secon
 // At n = 65536 bound by HBM and by drawing the keys' uniform halves: 14 items of two digits into seven outputs of ten limbs 77 us (0.3 GB: keys 147 MB,
 // plaintexts and outputs 73 MB each; 3.9 TB/s), two ciphertexts at level 3 17 us.  Rotating first, each to its ModDown, and multiplying then would write and
 // read every rotation and end in as many ModDowns.
-template <bool SA, int NB, int W>
+// SPLIT waves share the items of 64 W words and join their sums in LDS (sums of more than two items at n = 4096, whose launch does not fill the
+// chip: 14 items of four digits 24.9 -> 10.1 us).
+template <bool SA, int NB, int W, int SPLIT>
 __global__ __launch_bounds__(ROT_TPB) void k_weighted(WrBatch b, const ModC *__restrict__ modc, int beta, int ext, int level, int alpha, int L, int nmod, int n,
                                                       int logn, const u64 *__restrict__ pmont, EvkA eva, const u64 *__restrict__ ubound) {
     typedef u64 words __attribute__((ext_vector_type(W)));
-    const unsigned i0 = (blockIdx.x * ROT_TPB + threadIdx.x) * W;
+    const int part = threadIdx.x / (ROT_TPB / SPLIT);
+    const unsigned i0 = (blockIdx.x * (ROT_TPB / SPLIT) + threadIdx.x % (ROT_TPB / SPLIT)) * W;
     const int r = blockIdx.y, z = blockIdx.z, mi = r <= level ? r : L + 1 + (r - level - 1);
     const ModC m = modc[mi];
     const size_t o = (size_t)r * n + i0;
@@ -87,12 +90,12 @@ __global__ __launch_bounds__(ROT_TPB) void k_weighted(WrBatch b, const ModC *__r
     u64 r0[W] = {}, r1[W] = {};
     auto mul = [&](u64 x, u64 y) { return redc((u128)x * y, m.q, m.qinv); };
     auto load = [](const u64 *p) { return *reinterpret_cast<const words *>(p); };
-    if (b.extra[z]) {
+    if (part == 0 && b.extra[z]) {
         const words x = load(b.extra[z] + o), y = load(b.extra[z] + (size_t)ext * n + o);
 #pragma unroll
         for (int k = 0; k < W; k++) r0[k] = x[k], r1[k] = y[k];
     }
-    if (b.here[z] && r <= level) {
+    if (part == 0 && b.here[z] && r <= level) {
         const words w = load(b.here[z] + o), x = load(b.c_here[z] + o), y = load(b.c_here[z] + (size_t)(level + 1) * n + o);
 #pragma unroll
         for (int k = 0; k < W; k++) {
@@ -100,7 +103,7 @@ __global__ __launch_bounds__(ROT_TPB) void k_weighted(WrBatch b, const ModC *__r
             r0[k] = addmod(r0[k], mul(x[k], wp), m.q), r1[k] = addmod(r1[k], mul(y[k], wp), m.q);
         }
     }
-    for (int s = 0; s < b.nsum; s++) {
+    for (int s = part; s < b.nsum; s += SPLIT) {
         const WrItem it = b.it[z * b.nsum + s];
         const unsigned src = perm_src(i0, it.g, logn), base = src & ~(unsigned)(W - 1), flip = src & (W - 1);      // word k is word k ^ flip of the pair
         words d[NB], e[NB], c;
@@ -131,18 +134,30 @@ __global__ __launch_bounds__(ROT_TPB) void k_weighted(WrBatch b, const ModC *__r
             r1[k] = addmod(r1[k], mul(evk_a_reduce<SA>(sa, m), w[k]), m.q);
         }
     }
+    if (SPLIT > 1) {
+        __shared__ u64 sums[SPLIT][2 * W][ROT_TPB / SPLIT];
+        const int lane = threadIdx.x % (ROT_TPB / SPLIT);
+#pragma unroll
+        for (int k = 0; k < W; k++) sums[part][k][lane] = r0[k], sums[part][W + k][lane] = r1[k];
+        __syncthreads();
+        if (part) return;
+#pragma unroll
+        for (int q = 1; q < SPLIT; q++)
+#pragma unroll
+            for (int k = 0; k < W; k++) r0[k] = addmod(r0[k], sums[q][k][lane], m.q), r1[k] = addmod(r1[k], sums[q][W + k][lane], m.q);
+    }
     words x, y;
 #pragma unroll
     for (int k = 0; k < W; k++) x[k] = r0[k], y[k] = r1[k];
     *reinterpret_cast<words *>(b.out[z] + o) = x;
     *reinterpret_cast<words *>(b.out[z] + (size_t)ext * n + o) = y;
 }
-template <int W>
+template <int W, int SPLIT = 1>
 static void launch_weighted_words(cm_ctx *ctx, const WrBatch &b, int beta, int level, hipStream_t st) {
     const int ext = level + 1 + ctx->K;
-    const dim3 grid(ctx->n / (W * ROT_TPB), ext, b.nz);
+    const dim3 grid(ctx->n * SPLIT / (W * ROT_TPB), ext, b.nz);
 #define WEIGHTED(SA_, NB_)                                                                                                                                     \
-    hipLaunchKernelGGL((k_weighted<SA_, NB_, W>), grid, dim3(ROT_TPB), 0, st, b, ctx->d_modc, beta, ext, level, ctx->alpha, ctx->L, ctx->nmod, ctx->n, ctx->logn, ctx->d_pmont, \
+    hipLaunchKernelGGL((k_weighted<SA_, NB_, W, SPLIT>), grid, dim3(ROT_TPB), 0, st, b, ctx->d_modc, beta, ext, level, ctx->alpha, ctx->L, ctx->nmod, ctx->n, ctx->logn, ctx->d_pmont, \
                        evk_a_of(ctx), ctx->d_ubound)
     if (ctx->evk_stored_a) {
         if (beta <= 4) WEIGHTED(true, 4);
@@ -156,7 +171,8 @@ static void launch_weighted_words(cm_ctx *ctx, const WrBatch &b, int beta, int l
 }
 void launch_weighted(cm_ctx *ctx, const WrBatch &b, int beta, int level, hipStream_t st) {
     Prof prof_(ctx, CM_K_INNER_PRODUCT, b.nz * b.nsum, st);
-    if (ctx->n == 4096) launch_weighted_words<1>(ctx, b, beta, level, st);
+    if (ctx->n == 4096 && b.nsum > 2) launch_weighted_words<1, 4>(ctx, b, beta, level, st);
+    else if (ctx->n == 4096) launch_weighted_words<1>(ctx, b, beta, level, st);
     else launch_weighted_words<2>(ctx, b, beta, level, st);
 }
 // The row pass of the digits inside the weighted sums (launch_rows_weighted) repeats it for every item: the faster form with one item an output.  Two
