@@ -20,6 +20,7 @@
 #include "rotary.h"
 
 #define ROT_TPB 256
+#define ROT_AHEAD 4               // entries whose words are requested together
 // Tokens up to which the products are formed inside the inverse transform's row pass (launch_rotary_inv), whose lanes each do four words of them: one
 // token 8.5 us joined, 10.9 apart; eight 24 and 18.
 #define ROT_JOINED 4
@@ -41,22 +42,35 @@ __global__ __launch_bounds__(ROT_TPB) void k_rotary_products(u64 *__restrict__ v
         here = out[0], up = out[poly];
         if (parts == 3) dn = out[2 * poly];
     }
-    for (int k = 0; k < count; k++) {
-        const RotEntry e = b.e[k];
-        if (e.sets >> set & 1u) {
-            const u64 *p = low + (size_t)e.low * 4 * poly + at + perm_src(i, e.g, logn);
-            c1 = addmod(c1, p[0], m.q), c2 = addmod(c2, p[poly], m.q), s1 = addmod(s1, p[2 * poly], m.q), s2 = addmod(s2, p[3 * poly], m.q);
-            if (still) st = addmod(st, still[at + perm_src(i, e.g, logn)], m.q);
+    auto mul = [&](u64 x, u64 y) { return redc((u128)x * y, m.q, m.qinv); };
+    for (int k0 = 0; k0 < count; k0 += ROT_AHEAD) {
+        u64 w[ROT_AHEAD][5], h[ROT_AHEAD][2];
+        auto ends = [&](int k) { return k + 1 >= count || b.e[k + 1].high != b.e[k].high; };
+#pragma unroll
+        for (int a = 0; a < ROT_AHEAD; a++) {
+            const RotEntry e = b.e[k0 + a];
+            if (k0 + a >= count) continue;
+            const unsigned src = perm_src(i, e.g, logn);
+            const u64 *p = low + (size_t)e.low * 4 * poly + at + src, *t = high + (size_t)e.high * 2 * poly + at + i;
+#pragma unroll
+            for (int q = 0; q < 4; q++) w[a][q] = p[q * poly];
+            w[a][4] = still ? still[at + src] : 0;
+            if (ends(k0 + a)) h[a][0] = t[0], h[a][1] = t[poly];
         }
-        if (k + 1 < count && b.e[k + 1].high == e.high) continue;
-        const u64 c = high[(size_t)e.high * 2 * poly + at + i], s = high[((size_t)e.high * 2 + 1) * poly + at + i];
-        auto mul = [&](u64 x, u64 y) { return redc((u128)x * y, m.q, m.qinv); };
-        here = addmod(here, submod(mul(addmod(addmod(c1, c2, m.q), st, m.q), c), mul(addmod(s1, s2, m.q), s), m.q), m.q);
-        up = submod(up, addmod(mul(s1, c), mul(c1, s), m.q), m.q);
-        const u64 d = addmod(mul(s2, c), mul(c2, s), m.q);
-        if (parts == 3) dn = addmod(dn, d, m.q);
-        else up = addmod(up, d, m.q);
-        c1 = c2 = s1 = s2 = st = 0;
+#pragma unroll
+        for (int a = 0; a < ROT_AHEAD; a++) {
+            if (k0 + a >= count) continue;
+            if (b.e[k0 + a].sets >> set & 1u)
+                c1 = addmod(c1, w[a][0], m.q), c2 = addmod(c2, w[a][1], m.q), s1 = addmod(s1, w[a][2], m.q), s2 = addmod(s2, w[a][3], m.q), st = addmod(st, w[a][4], m.q);
+            if (!ends(k0 + a)) continue;
+            const u64 c = h[a][0], s = h[a][1];
+            here = addmod(here, submod(mul(addmod(addmod(c1, c2, m.q), st, m.q), c), mul(addmod(s1, s2, m.q), s), m.q), m.q);
+            up = submod(up, addmod(mul(s1, c), mul(c1, s), m.q), m.q);
+            const u64 d = addmod(mul(s2, c), mul(c2, s), m.q);
+            if (parts == 3) dn = addmod(dn, d, m.q);
+            else up = addmod(up, d, m.q);
+            c1 = c2 = s1 = s2 = st = 0;
+        }
     }
     out[0] = here, out[poly] = up;
     if (parts == 3) out[2 * poly] = dn;
