@@ -89,104 +89,134 @@ __global__ __launch_bounds__(ROT_TPB) void k_second(u64 *__restrict__ out, Secon
 // plaintexts and outputs 73 MB each; 3.9 TB/s), two ciphertexts at level 3 17 us.  Rotating first, each to its ModDown, and multiplying then would write and
 // read every rotation and end in as many ModDowns.
 // SPLIT waves share the items of 64 W words and join their sums in LDS (sums of more than two items at n = 4096, whose launch does not fill the
-// chip: 14 items of four digits 24.9 -> 10.1 us).
-template <bool SA, int NB, int W, int SPLIT>
+// chip: 14 items of four digits 24.9 -> 10.1 us).  Z: outputs of a lane, whose items have the same keys.
+template <bool SA, int NB, int W, int SPLIT, int Z>
 __global__ __launch_bounds__(ROT_TPB) void k_weighted(WrBatch b, const ModC *__restrict__ modc, int beta, int ext, int level, int alpha, int L, int nmod, int n,
                                                       int logn, const u64 *__restrict__ pmont, EvkA eva, const u64 *__restrict__ ubound) {
     typedef u64 words __attribute__((ext_vector_type(W)));
     const int part = threadIdx.x / (ROT_TPB / SPLIT);
     const unsigned i0 = (blockIdx.x * (ROT_TPB / SPLIT) + threadIdx.x % (ROT_TPB / SPLIT)) * W;
-    const int r = blockIdx.y, z = blockIdx.z, mi = r <= level ? r : L + 1 + (r - level - 1);
+    const int r = blockIdx.y, z0 = blockIdx.z * Z, mi = r <= level ? r : L + 1 + (r - level - 1);
     const ModC m = modc[mi];
     const size_t o = (size_t)r * n + i0;
     const u64 bound = ubound[mi], pm = r <= level ? pmont[r] : 0;
     const int own = r <= level ? r / alpha : -1;
-    u64 r0[W] = {}, r1[W] = {};
+    u64 r0[Z][W] = {}, r1[Z][W] = {};
     auto mul = [&](u64 x, u64 y) { return redc((u128)x * y, m.q, m.qinv); };
     auto load = [](const u64 *p) { return *reinterpret_cast<const words *>(p); };
-    if (part == 0 && b.extra[z]) {
-        const words x = load(b.extra[z] + o), y = load(b.extra[z] + (size_t)ext * n + o);
 #pragma unroll
-        for (int k = 0; k < W; k++) r0[k] = x[k], r1[k] = y[k];
-    }
-    if (part == 0 && b.here[z] && r <= level) {
-        const words w = load(b.here[z] + o), x = load(b.c_here[z] + o), y = load(b.c_here[z] + (size_t)(level + 1) * n + o);
+    for (int zz = 0; zz < Z; zz++) {
+        const int z = z0 + zz;
+        if (part == 0 && b.extra[z]) {
+            const words x = load(b.extra[z] + o), y = load(b.extra[z] + (size_t)ext * n + o);
 #pragma unroll
-        for (int k = 0; k < W; k++) {
-            const u64 wp = mul(w[k], pm);
-            r0[k] = addmod(r0[k], mul(x[k], wp), m.q), r1[k] = addmod(r1[k], mul(y[k], wp), m.q);
+            for (int k = 0; k < W; k++) r0[zz][k] = x[k], r1[zz][k] = y[k];
+        }
+        if (part == 0 && b.here[z] && r <= level) {
+            const words w = load(b.here[z] + o), x = load(b.c_here[z] + o), y = load(b.c_here[z] + (size_t)(level + 1) * n + o);
+#pragma unroll
+            for (int k = 0; k < W; k++) {
+                const u64 wp = mul(w[k], pm);
+                r0[zz][k] = addmod(r0[zz][k], mul(x[k], wp), m.q), r1[zz][k] = addmod(r1[zz][k], mul(y[k], wp), m.q);
+            }
         }
     }
     for (int s = part; s < b.nsum; s += SPLIT) {
-        const WrItem it = b.it[z * b.nsum + s];
-        const unsigned src = perm_src(i0, it.g, logn), base = src & ~(unsigned)(W - 1), flip = src & (W - 1);      // word k is word k ^ flip of the pair
-        words d[NB], e[NB], c;
+        const WrItem &first = b.it[z0 * b.nsum + s];             // its key and Galois map are those of all Z
+        const unsigned src = perm_src(i0, first.g, logn), base = src & ~(unsigned)(W - 1), flip = src & (W - 1);      // word k is word k ^ flip of the pair
+        words d[Z][NB], e[NB], c[Z], w[Z];
         u64 sk[NB];
 #pragma unroll
         for (int j = 0; j < NB; j++)
             if (j < beta) {
                 const size_t at = ((size_t)j * nmod + mi) * n + i0;
-                d[j] = load((j == own ? it.c + (size_t)(level + 1 + r) * n : it.dig + ((size_t)j * ext + r) * n) + base);
-                e[j] = __builtin_nontemporal_load(reinterpret_cast<const words *>(it.key + at));
-                if (!SA) sk[j] = it.key[(size_t)eva.kdig * nmod * n + (size_t)j * nmod + mi];
+#pragma unroll
+                for (int zz = 0; zz < Z; zz++) {
+                    const WrItem &it = b.it[(z0 + zz) * b.nsum + s];
+                    d[zz][j] = load((j == own ? it.c + (size_t)(level + 1 + r) * n : it.dig + ((size_t)j * ext + r) * n) + base);
+                }
+                e[j] = __builtin_nontemporal_load(reinterpret_cast<const words *>(first.key + at));
+                if (!SA) sk[j] = first.key[(size_t)eva.kdig * nmod * n + (size_t)j * nmod + mi];
             }
-        if (r <= level) c = load(it.c + (size_t)r * n + base);
-        const words w = load(it.pt + o);
+#pragma unroll
+        for (int zz = 0; zz < Z; zz++) {
+            const WrItem &it = b.it[(z0 + zz) * b.nsum + s];
+            if (r <= level) c[zz] = load(it.c + (size_t)r * n + base);
+            w[zz] = load(it.pt + o);
+        }
 #pragma unroll
         for (int k = 0; k < W; k++) {
-            u128 sa = 0, sb = 0;
+            u128 sa[Z] = {}, sb[Z] = {};
             const u64 cg = ((u64)i0 + k + 1) * GOLD;
 #pragma unroll
             for (int j = 0; j < NB; j++)
                 if (j < beta) {
-                    const u64 x = W == 1 ? d[j][0] : flip ? d[j][W - 1 - k] : d[j][k];
-                    const u64 a = SA ? __builtin_nontemporal_load(it.key + eva.a_off + ((size_t)j * nmod + mi) * n + i0 + k) : evk_a_draw(sk[j], cg, i0 + k, bound);
-                    sb += (u128)x * e[j][k], sa += (u128)x * a;
+                    const u64 a = SA ? __builtin_nontemporal_load(first.key + eva.a_off + ((size_t)j * nmod + mi) * n + i0 + k) : evk_a_draw(sk[j], cg, i0 + k, bound);
+#pragma unroll
+                    for (int zz = 0; zz < Z; zz++) {
+                        const u64 x = W == 1 ? d[zz][j][0] : flip ? d[zz][j][W - 1 - k] : d[zz][j][k];
+                        sb[zz] += (u128)x * e[j][k], sa[zz] += (u128)x * a;
+                    }
                 }
-            if (r <= level) sb += (u128)(W == 1 ? c[0] : flip ? c[W - 1 - k] : c[k]) * pm;
-            r0[k] = addmod(r0[k], mul(redc(sb, m.q, m.qinv), w[k]), m.q);
-            r1[k] = addmod(r1[k], mul(evk_a_reduce<SA>(sa, m), w[k]), m.q);
+#pragma unroll
+            for (int zz = 0; zz < Z; zz++) {
+                if (r <= level) sb[zz] += (u128)(W == 1 ? c[zz][0] : flip ? c[zz][W - 1 - k] : c[zz][k]) * pm;
+                r0[zz][k] = addmod(r0[zz][k], mul(redc(sb[zz], m.q, m.qinv), w[zz][k]), m.q);
+                r1[zz][k] = addmod(r1[zz][k], mul(evk_a_reduce<SA>(sa[zz], m), w[zz][k]), m.q);
+            }
         }
     }
     if (SPLIT > 1) {
-        __shared__ u64 sums[SPLIT][2 * W][ROT_TPB / SPLIT];
+        __shared__ u64 sums[SPLIT][2 * W * Z][ROT_TPB / SPLIT];
         const int lane = threadIdx.x % (ROT_TPB / SPLIT);
 #pragma unroll
-        for (int k = 0; k < W; k++) sums[part][k][lane] = r0[k], sums[part][W + k][lane] = r1[k];
+        for (int k = 0; k < W * Z; k++) sums[part][k][lane] = r0[k / W][k % W], sums[part][W * Z + k][lane] = r1[k / W][k % W];
         __syncthreads();
         if (part) return;
 #pragma unroll
         for (int q = 1; q < SPLIT; q++)
 #pragma unroll
-            for (int k = 0; k < W; k++) r0[k] = addmod(r0[k], sums[q][k][lane], m.q), r1[k] = addmod(r1[k], sums[q][W + k][lane], m.q);
+            for (int k = 0; k < W * Z; k++)
+                r0[k / W][k % W] = addmod(r0[k / W][k % W], sums[q][k][lane], m.q), r1[k / W][k % W] = addmod(r1[k / W][k % W], sums[q][W * Z + k][lane], m.q);
     }
-    words x, y;
 #pragma unroll
-    for (int k = 0; k < W; k++) x[k] = r0[k], y[k] = r1[k];
-    *reinterpret_cast<words *>(b.out[z] + o) = x;
-    *reinterpret_cast<words *>(b.out[z] + (size_t)ext * n + o) = y;
+    for (int zz = 0; zz < Z; zz++) {
+        words x, y;
+#pragma unroll
+        for (int k = 0; k < W; k++) x[k] = r0[zz][k], y[k] = r1[zz][k];
+        *reinterpret_cast<words *>(b.out[z0 + zz] + o) = x;
+        *reinterpret_cast<words *>(b.out[z0 + zz] + (size_t)ext * n + o) = y;
+    }
 }
-template <int W, int SPLIT = 1>
+template <int W, int SPLIT = 1, int Z = 1>
 static void launch_weighted_words(cm_ctx *ctx, const WrBatch &b, int beta, int level, hipStream_t st) {
     const int ext = level + 1 + ctx->K;
-    const dim3 grid(ctx->n * SPLIT / (W * ROT_TPB), ext, b.nz);
+    const dim3 grid(ctx->n * SPLIT / (W * ROT_TPB), ext, b.nz / Z);
 #define WEIGHTED(SA_, NB_)                                                                                                                                     \
-    hipLaunchKernelGGL((k_weighted<SA_, NB_, W, SPLIT>), grid, dim3(ROT_TPB), 0, st, b, ctx->d_modc, beta, ext, level, ctx->alpha, ctx->L, ctx->nmod, ctx->n, ctx->logn, ctx->d_pmont, \
+    hipLaunchKernelGGL((k_weighted<SA_, NB_, W, SPLIT, Z>), grid, dim3(ROT_TPB), 0, st, b, ctx->d_modc, beta, ext, level, ctx->alpha, ctx->L, ctx->nmod, ctx->n, ctx->logn, ctx->d_pmont, \
                        evk_a_of(ctx), ctx->d_ubound)
-    if (ctx->evk_stored_a) {
-        if (beta <= 4) WEIGHTED(true, 4);
-        else WEIGHTED(true, CM_MAX_DIGITS);
-    } else if (beta <= 1) WEIGHTED(false, 1);
-    else if (beta <= 2) WEIGHTED(false, 2);
-    else if (beta <= 4) WEIGHTED(false, 4);
-    else if (beta <= 6) WEIGHTED(false, 6);
-    else WEIGHTED(false, CM_MAX_DIGITS);
+    const bool sa = ctx->evk_stored_a;
+    if (beta <= 1 && !sa) WEIGHTED(false, 1);
+    else if (beta <= 2 && !sa) WEIGHTED(false, 2);
+    else if (beta <= 4) {
+        if (sa) WEIGHTED(true, 4);
+        else WEIGHTED(false, 4);
+    } else if constexpr (Z == 1) {
+        if (sa) WEIGHTED(true, CM_MAX_DIGITS);
+        else if (beta <= 6) WEIGHTED(false, 6);
+        else WEIGHTED(false, CM_MAX_DIGITS);
+    }
 #undef WEIGHTED
 }
 void launch_weighted(cm_ctx *ctx, const WrBatch &b, int beta, int level, hipStream_t st) {
     Prof prof_(ctx, CM_K_INNER_PRODUCT, b.nz * b.nsum, st);
+    // Outputs of the same keys, two a lane: a key's words are read and drawn once for both.  Four ciphertexts turned at level 12 (four digits) 398 -> 381 us, two
+    // 215 -> 208, at levels 3 and 7 1 % less; with six digits (176 registers) 426 -> 435.
+    bool pairs = ctx->n == 65536 && b.nz % 2 == 0 && beta <= 4;
+    for (int i = 0; i < b.nz * b.nsum && pairs; i++) pairs = b.it[i].key == b.it[i % b.nsum].key;
     if (ctx->n == 4096 && b.nsum > 2) launch_weighted_words<1, 4>(ctx, b, beta, level, st);
     else if (ctx->n == 4096) launch_weighted_words<1>(ctx, b, beta, level, st);
+    else if (pairs) launch_weighted_words<2, 1, 2>(ctx, b, beta, level, st);
     else launch_weighted_words<2>(ctx, b, beta, level, st);
 }
 // The row pass of the digits inside the weighted sums (launch_rows_weighted) repeats it for every item: the faster form with one item an output.  Two

@@ -149,6 +149,31 @@ def test_rotary_with_its_own_tables_on_the_full_ring(rings, keysets, heads, dim,
             assert np.abs(got[:, :, r] - want).max() < TOL / 1000
 
 
+@pytest.mark.parametrize("level, halves", [(3, False), (6, False), (12, False), (12, True), (22, False)])
+def test_ciphertexts_turned_together_are_those_turned_alone(rings, keysets, level, halves):
+    """On the full ring, one to six digits, odd and even counts, more than a batch: word for word."""
+    import torch
+    from paper_2602_11470_amd import binding as B
+    gctx, _ = rings("big")
+    rotary = gctx.rotary(16, 64, level, 40, halves=halves, rot_dims=32)
+    keys = keysets("big", rotary.steps(), False)
+    gctx.rotary_set(rotary, [(7 * i) % 40 if i % 5 else -1 for i in range(rotary.residues)])
+    gen = torch.Generator(device="cuda").manual_seed(level)
+    xs = []
+    for i in range(11):
+        x = B.Ct(gctx, level)
+        x.d.scale = gctx.scale
+        for l, q in enumerate(gctx.moduli()[: level + 1]):
+            _words(x)[:, l] = torch.empty(2, gctx.n, dtype=torch.int64, device="cuda").random_(0, int(q), generator=gen)
+        xs.append(x)
+    alone = [_words(gctx.rotary_apply(keys[1], rotary, [x])[0]).clone() for x in xs]
+    for count in (2, 3, 8, 11):
+        for y, want in zip(gctx.rotary_apply(keys[1], rotary, xs[:count]), alone):
+            assert torch.equal(_words(y), want)
+    twice = gctx.rotary_apply(keys[1], rotary, [xs[1], xs[1]])
+    assert all(torch.equal(_words(y), alone[1]) for y in twice)
+
+
 def test_rotary_is_the_embedding_of_one_token(rings, keysets):
     """What cm_rope_* does for one position and residue, and for a group."""
     gctx, _ = rings("small")
