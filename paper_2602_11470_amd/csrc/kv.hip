@@ -408,10 +408,12 @@ extern "C" cm_status cm_kv_append_group(cm_ctx *ctx, const cm_evk *evk, cm_kv *k
 
 
 // Sums of a mask's turns, one for each of up to RUN_MASKS outputs: out[z] = the entries begin[z] .. begin[z + 1] - 1 of mask[z] through their Galois maps.
-// Gathers from the caches: five tokens at six limbs 6 us of a call of 967, 21 tokens, two masks, eleven limbs 29 us of 1600.  All masks of a run in one launch:
+// Gathers from the caches at their rate (21 tokens, two masks, eleven limbs 242 MB in 22 us of a call of 1600; one word at a time 29); five tokens at six
+// limbs 6 us of 967.  All masks of a run in one launch:
 // at n = 4096 each would take the launch alone (3.7 us).  The call itself is bound by its masked rescales, as a single append is.
 #define RUN_TURNS 64
 #define RUN_MASKS 3
+#define RUN_AHEAD 8                // words requested before the first is used
 struct MaskTurns {
     u64 *out[RUN_MASKS];
     const u64 *mask[RUN_MASKS];
@@ -425,7 +427,14 @@ __global__ __launch_bounds__(256) void k_mask_turns(MaskTurns t, const ModC *__r
     const u64 q = modc[blockIdx.y].q, *mask = t.mask[z] + row;
     u64 *out = t.out[z] + row + i;
     u64 v = accumulate ? *out : 0;
-    for (int k = t.begin[z]; k < t.begin[z + 1]; k++) v = addmod(v, mask[perm_src(i, t.g[k], logn)], q);
+    const int end = t.begin[z + 1];
+    for (int k = t.begin[z]; k < end; k += RUN_AHEAD) {
+        u64 w[RUN_AHEAD];
+#pragma unroll
+        for (int a = 0; a < RUN_AHEAD; a++) w[a] = k + a < end ? mask[perm_src(i, t.g[min(k + a, end - 1)], logn)] : 0;
+#pragma unroll
+        for (int a = 0; a < RUN_AHEAD; a++) v = addmod(v, w[a], q);
+    }
     *out = v;
 }
 struct MaskSum {
