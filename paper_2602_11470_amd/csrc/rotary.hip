@@ -122,7 +122,10 @@ __global__ __launch_bounds__(ROT_TPB) void k_weighted(WrBatch b, const ModC *__r
         }
     }
     for (int s = part; s < b.nsum; s += SPLIT) {
-        const WrItem &first = b.it[z0 * b.nsum + s];             // its key and Galois map are those of all Z
+        WrItem its[Z];                                           // of the same key and Galois map
+#pragma unroll
+        for (int zz = 0; zz < Z; zz++) its[zz] = b.it[(z0 + zz) * b.nsum + s];
+        const WrItem &first = its[0];
         const unsigned src = perm_src(i0, first.g, logn), base = src & ~(unsigned)(W - 1), flip = src & (W - 1);      // word k is word k ^ flip of the pair
         words d[Z][NB], e[NB], c[Z], w[Z];
         u64 sk[NB];
@@ -131,18 +134,15 @@ __global__ __launch_bounds__(ROT_TPB) void k_weighted(WrBatch b, const ModC *__r
             if (j < beta) {
                 const size_t at = ((size_t)j * nmod + mi) * n + i0;
 #pragma unroll
-                for (int zz = 0; zz < Z; zz++) {
-                    const WrItem &it = b.it[(z0 + zz) * b.nsum + s];
-                    d[zz][j] = load((j == own ? it.c + (size_t)(level + 1 + r) * n : it.dig + ((size_t)j * ext + r) * n) + base);
-                }
+                for (int zz = 0; zz < Z; zz++)
+                    d[zz][j] = load((j == own ? its[zz].c + (size_t)(level + 1 + r) * n : its[zz].dig + ((size_t)j * ext + r) * n) + base);
                 e[j] = __builtin_nontemporal_load(reinterpret_cast<const words *>(first.key + at));
                 if (!SA) sk[j] = first.key[(size_t)eva.kdig * nmod * n + (size_t)j * nmod + mi];
             }
 #pragma unroll
         for (int zz = 0; zz < Z; zz++) {
-            const WrItem &it = b.it[(z0 + zz) * b.nsum + s];
-            if (r <= level) c[zz] = load(it.c + (size_t)r * n + base);
-            w[zz] = load(it.pt + o);
+            if (r <= level) c[zz] = load(its[zz].c + (size_t)r * n + base);
+            w[zz] = load(its[zz].pt + o);
         }
 #pragma unroll
         for (int k = 0; k < W; k++) {
