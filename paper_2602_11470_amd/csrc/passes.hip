@@ -210,9 +210,10 @@ cm_status kv_passes_run(cm_ctx *ctx, const cm_evk *evk, const cm_kv *kv, const K
         CMCHK(moddown_batch_into(ctx, us, lv, cnt, adds, 2, 0, nullptr, to, st, half));
     }
     if (kv->unrolled) {
-        // sum_g Rot(inner_g, g G) next to P inner_0, on the extended basis
+        // sum_g Rot(inner_g, g G) on the extended basis; inner_0 joins behind the ModDown (ModDown(u + P x) = ModDown(u) + x, word for word), or as P inner_0
+        const bool joins = r_o > 1 && ks_drop_fits(ctx, lv, 1, m);
         u64 *cur = kp.acc, *nxt = kp.nxt;
-        launch_raise_by_P(ctx, cur, kp.inner, lv, st, m);
+        if (!joins) launch_raise_by_P(ctx, cur, kp.inner, lv, st, m);
         const int most = std::max(1, std::min(kp.G, IP_MAX_ITEMS / m));
         for (int g0 = 1; g0 < r_o; g0 += most) {
             const int cnt = std::min(most, r_o - g0);
@@ -228,12 +229,13 @@ cm_status kv_passes_run(cm_ctx *ctx, const cm_evk *evk, const cm_kv *kv, const K
                     it.dig = kp.digits + (s * m + p) * dblk, it.key = find_key(evk, gal), it.g = (unsigned)gal;
                     it.c0 = c + (s * m + p) * ctw, it.own = it.c0 + ln;
                 }
-                b.out[p] = nxt + p * ublk, b.extra[p] = cur + p * ublk;
+                b.out[p] = nxt + p * ublk, b.extra[p] = joins && g0 == 1 ? nullptr : cur + p * ublk;
             }
             if (half) launch_rows_ip(ctx, b, kl.beta, lv, st);
             else launch_inner_product_batch(ctx, b, kl.beta, lv, st);
             std::swap(cur, nxt);
         }
+        if (joins) return ks_drop(ctx, cur, lv, 1, m, kp.inner, ctw, 2, 0, nullptr, 0, nullptr, st, false, outs);
         if (ks_drop_fits(ctx, lv, 1, m)) return ks_drop(ctx, cur, lv, 1, m, nullptr, 0, 0, 0, nullptr, 0, nullptr, st, false, outs);
         for (int p = 0; p < m; p++) CMCHK(moddown_rescale_into(ctx, cur + p * ublk, lv, kp.inner, outs[p], st));
         return CM_OK;
