@@ -217,6 +217,10 @@ struct MacFp {
     __device__ __forceinline__ static double from_u64(u64 raw) {                 // raw < 2^52
         return __longlong_as_double((long long)(raw | 0x4330000000000000ULL)) - 4503599627370496.0;
     }
+    __device__ __forceinline__ double centred(u64 raw) const {                   // raw < q -> -q/2 .. q/2
+        const double x = from_u64(raw);
+        return x + x > q ? x - q : x;
+    }
     __device__ __forceinline__ u64 canon(double v) const {                       // |v| < 2^53 -> [0, q)
         const double r = norm(v);                                                // |r| < q: q is added under the sign mask
         const int m = __double2hiint(r) >> 31;
@@ -343,7 +347,11 @@ bool tensor_sum_held(int n, int limbs, int cnt, int groups) {
 // owns a pass for 64 coefficients; the words of a group are staged in LDS for all of them, the next group's requested ahead.
 // Bound by HBM: with a launch a pass the cache was read once per pass of a grouped query.  Four passes over 128 ciphertexts of ten
 // limbs 4 x 317 -> 582 us, grouped-query attention at level 9 12860 -> 11640.  Eight (five limbs) 547 us, two launches of four 580: half of the traffic
-// by then are the passes' own ciphertexts and sums.  108 registers because the
+// by then are the passes' own ciphertexts and sums.
+// The middle component is (a0 + a1)(b0 + b1) less the outer ones, three products a term for four.  Residues are centred, so |a|, |b| <= q/2 and the sums'
+// product is at most q^2: its quotient by q, below 2^50, is off by at most 3 2^-53 2^50 < 0.4 before it is rounded, which leaves |r| < 0.9 q; eight
+// terms and a renormalised sum stay below 7.8 q < 2^53.  Eight passes 540 -> 512 us, with words that are used once passed by the caches 504 (3.7 TB/s of the
+// traffic); grouped-query attention at level 9 11383 -> 11283.  108 registers because the
 // terms are worked on four at a time (sched_barrier); left to itself the compiler spills 187 of 128.
 #define TS_CO 64
 template <int PASSES>
@@ -370,30 +378,30 @@ __global__ __launch_bounds__(64 * PASSES, 4) void k_tensor_sum_passes(u64 *__res
     double a0[TS_MAX_CNT], a1[TS_MAX_CNT];
 #pragma unroll
     for (int j = 0; j < TS_MAX_CNT; j++) {
-        a0[j] = j < cnt ? MacFp::from_u64(a[(size_t)j * 2 * cs + o]) : 0.0;
-        a1[j] = j < cnt ? MacFp::from_u64(a[(size_t)j * 2 * cs + cs + o]) : 0.0;
+        a0[j] = j < cnt ? F.centred(__builtin_nontemporal_load(a + (size_t)j * 2 * cs + o)) : 0.0;
+        a1[j] = j < cnt ? F.centred(__builtin_nontemporal_load(a + (size_t)j * 2 * cs + cs + o)) : 0.0;
     }
     for (int z = 0; z < groups; z++) {
         // two buffers in turn: a wave that writes to one has passed the barrier behind the others' reads of it
         double *s = sb[z & 1] + co;
 #pragma unroll
-        for (int it = 0; it < ROWS; it++) s[(pass * ROWS + it) * TS_CO] = MacFp::from_u64(r[it]);
+        for (int it = 0; it < ROWS; it++) s[(pass * ROWS + it) * TS_CO] = F.centred(r[it]);
         __syncthreads();
         if (z + 1 < groups) request(z + 1);
         double d0 = 0.0, d1 = 0.0, d2 = 0.0;
 #pragma unroll
         for (int j = 0; j < TS_MAX_CNT; j++) {
-            const double b0 = s[2 * j * TS_CO], b1 = s[(2 * j + 1) * TS_CO], b0q = b0 * F.qinv, b1q = b1 * F.qinv;
-            d0 += F.mulmod(a0[j], b0, b0q);
-            d1 += F.mulmod(a0[j], b1, b1q) + F.mulmod(a1[j], b0, b0q);
-            d2 += F.mulmod(a1[j], b1, b1q);
-            if (j & 1) d0 = F.norm(d0), d1 = F.norm(d1), d2 = F.norm(d2);
+            const double b0 = s[2 * j * TS_CO], b1 = s[(2 * j + 1) * TS_CO], bs = b0 + b1;
+            d0 += F.mulmod(a0[j], b0, b0 * F.qinv);
+            d1 += F.mulmod(a0[j] + a1[j], bs, bs * F.qinv);
+            d2 += F.mulmod(a1[j], b1, b1 * F.qinv);
+            if ((j & 7) == 7) d0 = F.norm(d0), d1 = F.norm(d1), d2 = F.norm(d2);
             if ((j & 3) == 3) __builtin_amdgcn_sched_barrier(0);
         }
         u64 *oz = out + (size_t)z * 3 * cs;
-        oz[o] = F.canon(d0);
-        oz[o + cs] = F.canon(d1);
-        oz[o + 2 * cs] = F.canon(d2);
+        __builtin_nontemporal_store(F.canon(d0), oz + o);
+        __builtin_nontemporal_store(F.canon(d1 - d0 - d2), oz + o + cs);
+        __builtin_nontemporal_store(F.canon(d2), oz + o + 2 * cs);
     }
 }
 // Where the joint launch is the faster way.  It always does the work of TS_MAX_CNT terms and its writes lie among its reads: with few

@@ -584,6 +584,33 @@ def test_tree_refusals(rings, keysets):
     assert sv(at) == -3
 
 
+@pytest.mark.parametrize("ring, heads, dim, level", [("small", 8, 32, 2), ("big", 32, 128, 3)])
+def test_products_of_extreme_words(rings, keysets, ring, heads, dim, level):
+    """Pass 0 of the joint products against the single one, sixteen equal terms a sum: a query without second component keeps its constant words
+    under rotation.  Halves of the modulus on either side, its largest word, and factors whose product is halfway between two multiples."""
+    import torch
+    from paper_2602_11470_amd import binding as B
+    gctx, _ = rings(ring)
+    kv = gctx.kv_create(heads, dim, level, r_i=16, key_index=True, unrolled_ladders=True)
+    tree = gctx.tree(kv, mask=0.0, scale=gctx.scale ** 2 / float(gctx.moduli()[level]))
+    keys = keysets(ring, kv.steps() + tree.steps(), True)
+    kv.set_tokens(2 * tree.passes)
+    q, mods = B.Ct(gctx, level + 1), [int(m) for m in gctx.moduli()]
+    q.d.scale = gctx.scale
+    pairs = [lambda m: (m // 2, m // 2), lambda m: (m // 2 + 1, m // 2), lambda m: (m // 2 + 1, m // 2 + 1), lambda m: (m - 1, m - 1),
+             lambda m: (m // 2 - 1, m // 2 * pow(m // 2 - 1, -1, m) % m), lambda m: (m // 3, (m // 2 + 1) * pow(m // 3, -1, m) % m)]
+    index = kv.words(B.CM_KV_INDEX)
+    for pair in pairs:
+        _words(q).zero_()
+        for l in range(level + 2):
+            _words(q)[0, l] = pair(mods[l])[0]
+            if l <= level:
+                index[..., l, :] = pair(mods[l])[1]
+        scores = gctx.tree_qk(keys[1], tree, kv, [-1], 2 * tree.passes - 1, q)
+        single = gctx.vmm_kv(keys[1], kv, B.CM_QK_GROUP, gctx.level_drop(q, level))
+        assert torch.equal(_words(scores[0]), _words(single))
+
+
 @pytest.mark.parametrize("ring, heads, dim, r_i, level", [("small", 8, 32, 8, 2), ("big", 64, 64, 16, 2)])
 def test_stored_key_halves_give_the_same_words(rings, ring, heads, dim, r_i, level):
     """Keys with both halves stored (CM_OPT_EVK_STORED_A) go through kernels of their own."""
