@@ -84,7 +84,7 @@ __global__ __launch_bounds__(ROT_TPB) void k_second(u64 *__restrict__ out, Secon
 // ---- weighted rotations -----------------------------------------------------------------------------------------------
 // A lane has W neighbouring words of an output and runs over its items: the item's digits through the Galois map, its key's
 // words, the sums reduced and multiplied by the item's plaintext.  All loads of an item are requested before the first is used (NB bounds its
-// digits); one word a lane at n = 4096, where a launch is as long as a lane's chain (two items, one digit 5.7 -> 4.7 us, four digits 9.5 -> 6.3).
+// digits), keys and plaintexts past the caches; one word a lane at n = 4096, where a launch is as long as a lane's chain (two items, one digit 5.7 -> 4.7 us, four digits 9.5 -> 6.3).
 // At n = 65536 bound by HBM and by drawing the keys' uniform halves: 14 items of two digits into seven outputs of ten limbs 77 us (0.3 GB: keys 147 MB,
 // plaintexts and outputs 73 MB each; 3.9 TB/s), two ciphertexts at level 3 17 us.  Rotating first, each to its ModDown, and multiplying then would write and
 // read every rotation and end in as many ModDowns.
@@ -142,7 +142,7 @@ __global__ __launch_bounds__(ROT_TPB) void k_weighted(WrBatch b, const ModC *__r
 #pragma unroll
         for (int zz = 0; zz < Z; zz++) {
             if (r <= level) c[zz] = load(its[zz].c + (size_t)r * n + base);
-            w[zz] = load(its[zz].pt + o);
+            w[zz] = __builtin_nontemporal_load(reinterpret_cast<const words *>(its[zz].pt + o));
         }
 #pragma unroll
         for (int k = 0; k < W; k++) {
