@@ -192,7 +192,7 @@ struct cm_ctx {
     std::map<int, u64 *> qlinv;                    // level -> [level][2]: q_level^{-1} mod q_i, Shoup
     u64 *d_cdt = nullptr;                          // Gaussian table [CM_GAUSS_K]
     u64 cdt[CM_GAUSS_K];
-    int lazy_terms;                                // products that may be summed before one REDC
+    int lazy_terms;                                // digits whose products may be summed before one reduction, a first component's among them
     // options (cm_ctx_set_option)
     bool evk_stored_a = false;     // evaluation keys carry both halves; the inner products read the uniform half
     bool two_step_masks = false;   // cache appends multiply, store and rescale instead of fusing the product into the rescale

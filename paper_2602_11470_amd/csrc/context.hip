@@ -4,6 +4,7 @@
 #include <stdlib.h>
 #include <string.h>
 
+#include <algorithm>
 #include <complex>
 
 #include "common.h"
@@ -295,11 +296,9 @@ extern "C" cm_status cm_ctx_create(const cm_params *p, cm_ctx **out) {
         }
         ctx->mod.insert(ctx->mod.end(), sp.begin(), sp.end());
     }
-    u64 qmax = 0;
-    for (u64 m : ctx->mod) qmax = m > qmax ? m : qmax;
-    ctx->lazy_terms = (int)((((u128)1) << 64) / qmax) - 1;
-    if (ctx->lazy_terms > 64) ctx->lazy_terms = 64;
-    if (ctx->lazy_terms < 2) { delete ctx; return CM_E_INVAL; }
+    // on ciphertext limbs a first component joins the sums
+    ctx->lazy_terms = CM_MAX_DIGITS;
+    for (int m = 0; m < ctx->nmod; m++) ctx->lazy_terms = std::min(ctx->lazy_terms, (int)std::min<u64>(64, 0xFFFFFFFFFFFFFFFFULL / ctx->mod[m]) - (m <= ctx->L));
 
     // Montgomery constants and NTT tables
     std::vector<u64> tw((size_t)ctx->nmod * n), itw(tw.size()), ninv(ctx->nmod);

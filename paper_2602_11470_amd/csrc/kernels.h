@@ -13,8 +13,8 @@ __host__ __device__ __forceinline__ u64 mix64(u64 z) {
 // keys of the generator streams of a_j.  The uniform half is drawn directly in the evaluation domain, so word i of
 // limb mi of a_j is draw i of that stream (rejected at or above bound = q floor(2^64/q), then taken mod q): the inner
 // products regenerate it instead of reading it, which takes a third off their traffic.  The draw enters the sums as
-// the raw 64-bit word v (v = a mod q): sum_j d_j v_j < beta q 2^64 fits 128 bits, REDC gives (sum 2^-64) mod q below
-// (beta + 1) q, and a second REDC against 2^128 mod q gives sum mod q in [0, q) -- two reductions per output instead of
+// the raw 64-bit word v (v = a mod q): sum_j d_j v_j < beta q 2^64 fits 128 bits for up to eight digits (q < 2^61; more: less_of_sum), REDC gives
+// (sum 2^-64) mod q below (beta + 1) q, and a second REDC against 2^128 mod q gives sum mod q in [0, q) -- two reductions per output instead of
 // one per key word.  ctr_gold = (i + 1) GOLD is the counter term of attempt 0, shared by all digits of a lane.
 __device__ __forceinline__ u64 evk_a_draw(u64 stream_key, u64 ctr_gold, unsigned i, u64 bound) {
     u64 v = mix64(stream_key + ctr_gold);
@@ -48,6 +48,15 @@ __device__ __forceinline__ ulonglong2 evk_a_words(const u64 *__restrict__ key, c
 template <bool SA>
 __device__ __forceinline__ u64 evk_a_reduce(u128 T, const ModC &m) {
     return SA ? redc(T, m.q, m.qinv) : redc_raw(T, m);
+}
+// Sums of more digits than cm_ctx::lazy_terms (eight for 61-bit special moduli, seven for ciphertext moduli of that size, sixteen below) may pass what the reductions take: 128 bits for raw draws (RAW), q 2^64
+// for words in multiplier form, whose terms are below q^2 < q 2^61, a first component's P c among them.  Such a sum loses a multiple of q 2^64, which is
+// zero mod q, after every fourth digit and, in multiplier form, before its reduction: raw ones stay below 4 q 2^64 + 4 q 2^64 < 2^128, the others
+// below q 2^64 + 5 q 2^61.  The kernels that do this (WIDE) are instantiations of their own: the others have no instruction more.
+template <bool RAW>
+__device__ __forceinline__ void less_of_sum(u128 &T, u64 q) {
+    const u64 s = RAW ? 4 * q : q;
+    if ((u64)(T >> 64) >= s) T -= (u128)s << 64;
 }
 inline EvkA evk_a_of(const cm_ctx *ctx) {
     return EvkA{ctx->evk_stored_a ? evk_a_offset(ctx) : 0, (ctx->L + ctx->alpha) / ctx->alpha};

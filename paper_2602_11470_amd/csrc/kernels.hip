@@ -481,7 +481,7 @@ void launch_automorphism(cm_ctx *ctx, u64 *out, const u64 *in, int rows, u64 g, 
 // rotations).  Two adjacent coefficients per lane (16-byte accesses); the permutation keeps
 // aligned pairs together (it maps i^1 to src^1).
 // `extra` may be the output itself (a running sum): every lane reads its own words before it writes them.
-template <bool SA>
+template <bool SA, bool WIDE>
 __global__ __launch_bounds__(TPB) void k_inner_product(u64 *u0, u64 *u1,
                                                        const u64 *__restrict__ dig, const u64 *__restrict__ evk,
                                                        const ModC *__restrict__ modc,
@@ -510,12 +510,17 @@ __global__ __launch_bounds__(TPB) void k_inner_product(u64 *u0, u64 *u1,
         b1 += (u128)dy * eb.y;
         a0 += (u128)dx * ea.x;
         a1 += (u128)dy * ea.y;
+        if (WIDE && (j & 3) == 3) less_of_sum<false>(b0, m.q), less_of_sum<false>(b1, m.q), less_of_sum<!SA>(a0, m.q), less_of_sum<!SA>(a1, m.q);
     }
     if (c0 && r <= level) {           // + P * sigma_g(c0): the rotation stays in the extended basis
         ulonglong2 d = *reinterpret_cast<const ulonglong2 *>(c0 + (size_t)r * n + base);
         const u64 pm = pmont[r];
         b0 += (u128)(swap ? d.y : d.x) * pm;
         b1 += (u128)(swap ? d.x : d.y) * pm;
+    }
+    if (WIDE) {
+        less_of_sum<false>(b0, m.q), less_of_sum<false>(b1, m.q);
+        if (SA) less_of_sum<false>(a0, m.q), less_of_sum<false>(a1, m.q);
     }
     size_t o = (size_t)r * n + i2;
     ulonglong2 r0 = make_ulonglong2(redc(b0, m.q, m.qinv), redc(b1, m.q, m.qinv));
@@ -533,7 +538,7 @@ __global__ __launch_bounds__(TPB) void k_inner_product(u64 *u0, u64 *u1,
 // (each with its own digits, key, Galois element and optional c0) and an optional addend.
 // APART (IpBatch::apart) is an instantiation of its own: as a run-time branch it cost all other calls 11 to 15 % of this kernel
 // (31 giant steps on 6 limbs of n = 4096, five digits: 51 us without it, 59 with it).
-template <bool SA, bool APART>
+template <bool SA, bool APART, bool WIDE>
 __global__ __launch_bounds__(TPB) void k_inner_product_batch(IpBatch b, const ModC *__restrict__ modc, int beta, int ext,
                                                              int level, int L, int nmod, int n, int logn,
                                                              const u64 *__restrict__ pmont, EvkA eva,
@@ -577,6 +582,7 @@ __global__ __launch_bounds__(TPB) void k_inner_product_batch(IpBatch b, const Mo
             b1 += (u128)dy * eb.y;
             a0 += (u128)dx * ea.x;
             a1 += (u128)dy * ea.y;
+            if (WIDE && (j & 3) == 3) less_of_sum<false>(b0, m.q), less_of_sum<false>(b1, m.q), less_of_sum<!SA>(a0, m.q), less_of_sum<!SA>(a1, m.q);
         }
         if (it.c0 && it.c0_ext) {            // a first component that never left the extended basis
             ulonglong2 d = *reinterpret_cast<const ulonglong2 *>(it.c0 + (size_t)r * n + base);
@@ -586,6 +592,10 @@ __global__ __launch_bounds__(TPB) void k_inner_product_batch(IpBatch b, const Mo
             const u64 pm = pmont[r];
             b0 += (u128)(swap ? d.y : d.x) * pm;
             b1 += (u128)(swap ? d.x : d.y) * pm;
+        }
+        if (WIDE) {
+            less_of_sum<false>(b0, m.q), less_of_sum<false>(b1, m.q);
+            if (SA) less_of_sum<false>(a0, m.q), less_of_sum<false>(a1, m.q);
         }
         r0.x = addmod(r0.x, redc(b0, m.q, m.qinv), m.q), r0.y = addmod(r0.y, redc(b1, m.q, m.qinv), m.q);
         r1.x = addmod(r1.x, evk_a_reduce<SA>(a0, m), m.q), r1.y = addmod(r1.y, evk_a_reduce<SA>(a1, m), m.q);
@@ -915,9 +925,16 @@ void launch_inner_product_batch(cm_ctx *ctx, const IpBatch &b, int beta, int lev
     Prof prof_(ctx, CM_K_INNER_PRODUCT, b.nz * b.nsum, st);
     int ext = level + 1 + ctx->K;
     const dim3 grid(ctx->n / (2 * TPB), ext, b.nz);
+    const bool wide = beta > ctx->lazy_terms;
 #define BATCH_LAUNCH(SA_, APART_)                                                                                               \
-    hipLaunchKernelGGL((k_inner_product_batch<SA_, APART_>), grid, dim3(TPB), 0, st, b, ctx->d_modc, beta, ext, level, ctx->L, ctx->nmod, \
-                       ctx->n, ctx->logn, ctx->d_pmont, evk_a_of(ctx), ctx->d_ubound)
+    do {                                                                                                                        \
+        if (wide)                                                                                                               \
+            hipLaunchKernelGGL((k_inner_product_batch<SA_, APART_, true>), grid, dim3(TPB), 0, st, b, ctx->d_modc, beta, ext, level, ctx->L, ctx->nmod, \
+                               ctx->n, ctx->logn, ctx->d_pmont, evk_a_of(ctx), ctx->d_ubound);                                  \
+        else                                                                                                                    \
+            hipLaunchKernelGGL((k_inner_product_batch<SA_, APART_, false>), grid, dim3(TPB), 0, st, b, ctx->d_modc, beta, ext, level, ctx->L, ctx->nmod, \
+                               ctx->n, ctx->logn, ctx->d_pmont, evk_a_of(ctx), ctx->d_ubound);                                  \
+    } while (0)
     if (ctx->evk_stored_a) {
         if (b.apart) BATCH_LAUNCH(true, true);
         else BATCH_LAUNCH(true, false);
@@ -947,14 +964,16 @@ void launch_inner_product(cm_ctx *ctx, u64 *u0, u64 *u1, const u64 *dig, const u
                           hipStream_t st, const u64 *c0, const u64 *extra) {
     Prof prof_(ctx, CM_K_INNER_PRODUCT, 1, st);
     int ext = level + 1 + ctx->K;
-    if (ctx->evk_stored_a)
-        hipLaunchKernelGGL(k_inner_product<true>, dim3(ctx->n / (2 * TPB), ext), dim3(TPB), 0, st, u0, u1, dig, evk, ctx->d_modc,
-                           beta, ext, level, ctx->L, ctx->nmod, ctx->n, ctx->logn, (unsigned)g, c0, ctx->d_pmont, extra,
-                           evk_a_of(ctx), ctx->d_ubound);
-    else
-        hipLaunchKernelGGL(k_inner_product<false>, dim3(ctx->n / (2 * TPB), ext), dim3(TPB), 0, st, u0, u1, dig, evk, ctx->d_modc,
-                           beta, ext, level, ctx->L, ctx->nmod, ctx->n, ctx->logn, (unsigned)g, c0, ctx->d_pmont, extra,
-                           evk_a_of(ctx), ctx->d_ubound);
+#define IP_LAUNCH(SA_, WIDE_)                                                                                                            \
+    hipLaunchKernelGGL((k_inner_product<SA_, WIDE_>), dim3(ctx->n / (2 * TPB), ext), dim3(TPB), 0, st, u0, u1, dig, evk, ctx->d_modc, \
+                       beta, ext, level, ctx->L, ctx->nmod, ctx->n, ctx->logn, (unsigned)g, c0, ctx->d_pmont, extra, evk_a_of(ctx), ctx->d_ubound)
+    const bool wide = beta > ctx->lazy_terms;
+    if (ctx->evk_stored_a) {
+        if (wide) IP_LAUNCH(true, true);
+        else IP_LAUNCH(true, false);
+    } else if (wide) IP_LAUNCH(false, true);
+    else IP_LAUNCH(false, false);
+#undef IP_LAUNCH
 }
 
 // ---- rescale ---------------------------------------------------------------------------------

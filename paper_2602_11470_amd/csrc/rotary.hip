@@ -90,7 +90,7 @@ __global__ __launch_bounds__(ROT_TPB) void k_second(u64 *__restrict__ out, Secon
 // read every rotation and end in as many ModDowns.
 // SPLIT waves share the items of 64 W words and join their sums in LDS (sums of more than two items at n = 4096, whose launch does not fill the
 // chip: 14 items of four digits 24.9 -> 10.1 us).  Z: outputs of a lane, whose items have the same keys.
-template <bool SA, int NB, int W, int SPLIT, int Z>
+template <bool SA, int NB, int W, int SPLIT, int Z, bool WIDE>
 __global__ __launch_bounds__(ROT_TPB) void k_weighted(WrBatch b, const ModC *__restrict__ modc, int beta, int ext, int level, int alpha, int L, int nmod, int n,
                                                       int logn, const u64 *__restrict__ pmont, EvkA eva, const u64 *__restrict__ ubound) {
     typedef u64 words __attribute__((ext_vector_type(W)));
@@ -156,11 +156,14 @@ __global__ __launch_bounds__(ROT_TPB) void k_weighted(WrBatch b, const ModC *__r
                     for (int zz = 0; zz < Z; zz++) {
                         const u64 x = W == 1 ? d[zz][j][0] : flip ? d[zz][j][W - 1 - k] : d[zz][j][k];
                         sb[zz] += (u128)x * e[j][k], sa[zz] += (u128)x * a;
+                        if (WIDE && (j & 3) == 3) less_of_sum<false>(sb[zz], m.q), less_of_sum<!SA>(sa[zz], m.q);
                     }
                 }
 #pragma unroll
             for (int zz = 0; zz < Z; zz++) {
                 if (r <= level) sb[zz] += (u128)(W == 1 ? c[zz][0] : flip ? c[zz][W - 1 - k] : c[zz][k]) * pm;
+                if (WIDE) less_of_sum<false>(sb[zz], m.q);
+                if (WIDE && SA) less_of_sum<false>(sa[zz], m.q);
                 r0[zz][k] = addmod(r0[zz][k], mul(redc(sb[zz], m.q, m.qinv), w[zz][k]), m.q);
                 r1[zz][k] = addmod(r1[zz][k], mul(evk_a_reduce<SA>(sa[zz], m), w[zz][k]), m.q);
             }
@@ -192,19 +195,22 @@ template <int W, int SPLIT = 1, int Z = 1>
 static void launch_weighted_words(cm_ctx *ctx, const WrBatch &b, int beta, int level, hipStream_t st) {
     const int ext = level + 1 + ctx->K;
     const dim3 grid(ctx->n * SPLIT / (W * ROT_TPB), ext, b.nz / Z);
-#define WEIGHTED(SA_, NB_)                                                                                                                                     \
-    hipLaunchKernelGGL((k_weighted<SA_, NB_, W, SPLIT, Z>), grid, dim3(ROT_TPB), 0, st, b, ctx->d_modc, beta, ext, level, ctx->alpha, ctx->L, ctx->nmod, ctx->n, ctx->logn, ctx->d_pmont, \
-                       evk_a_of(ctx), ctx->d_ubound)
+#define WEIGHTED(SA_, NB_, WIDE_)                                                                                                                              \
+    hipLaunchKernelGGL((k_weighted<SA_, NB_, W, SPLIT, Z, WIDE_>), grid, dim3(ROT_TPB), 0, st, b, ctx->d_modc, beta, ext, level, ctx->alpha, ctx->L, ctx->nmod, ctx->n, ctx->logn, \
+                       ctx->d_pmont, evk_a_of(ctx), ctx->d_ubound)
     const bool sa = ctx->evk_stored_a;
-    if (beta <= 1 && !sa) WEIGHTED(false, 1);
-    else if (beta <= 2 && !sa) WEIGHTED(false, 2);
+    if (beta <= 1 && !sa) WEIGHTED(false, 1, false);
+    else if (beta <= 2 && !sa) WEIGHTED(false, 2, false);
     else if (beta <= 4) {
-        if (sa) WEIGHTED(true, 4);
-        else WEIGHTED(false, 4);
+        if (sa) WEIGHTED(true, 4, false);
+        else WEIGHTED(false, 4, false);
     } else if constexpr (Z == 1) {
-        if (sa) WEIGHTED(true, CM_MAX_DIGITS);
-        else if (beta <= 6) WEIGHTED(false, 6);
-        else WEIGHTED(false, CM_MAX_DIGITS);
+        if (beta > ctx->lazy_terms) {
+            if (sa) WEIGHTED(true, CM_MAX_DIGITS, true);
+            else WEIGHTED(false, CM_MAX_DIGITS, true);
+        } else if (sa) WEIGHTED(true, CM_MAX_DIGITS, false);
+        else if (beta <= 6) WEIGHTED(false, 6, false);
+        else WEIGHTED(false, CM_MAX_DIGITS, false);
     }
 #undef WEIGHTED
 }
