@@ -397,7 +397,8 @@ void cm_kv_sel_destroy(cm_kv_sel *sel);
 int32_t cm_kv_sel_steps(const cm_kv_sel *sel, int32_t *steps, int32_t cap);
 /* dst = the kept tokens of src, moved (add = 0; what dst held is replaced), or dst += them (add != 0: the places must be empty
  * in dst; a fork and an adding take with a shift put two caches behind one another).  Frees pages, takes rejected drafts
- * back (keep a prefix), slides a window or closes gaps (shift < 0).  dst is another cache, one level below src (else
+ * back, slides a window or closes gaps (shift < 0).  A place that loses its token between kept ones stays; its scores are zero
+ * (cm_tree_set_empty hides it).  dst is another cache, one level below src (else
  * CM_E_LEVEL), with room for the last kept token (else CM_E_LAYOUT); src holds sel's ntok tokens and nothing behind them
  * (cm_kv_tokens differs: CM_E_LAYOUT).  Bit for bit: K pages kept whole are dropped one level; every other ciphertext is
  * multiplied by its mask and rescaled (cm_mul_pt, cm_rescale), and where its place asks for it rotated (cm_rotate).  evk may
@@ -564,9 +565,12 @@ cm_status cm_rotary_apply(cm_ctx *ctx, const cm_evk *evk, const cm_rotary *rotar
 cm_status cm_kv_append_run(cm_ctx *ctx, const cm_evk *evk, cm_kv *kv, const cm_rotary *rotary, int32_t ntok, const cm_ct *k, const cm_ct *v, void *stream);
 
 /* ---- attention of a tree of drafted tokens ----------------------------------------------------------------
- * `nodes` drafted tokens stand in the cache at places base .. base + nodes - 1, behind what was committed (appended by cm_kv_append_run, say; the
- * rejected ones are dropped by cm_kv_take); token i follows parent[i] (host, -1 <= parent[i] < i; -1: the last committed token).  Its query sees the
+ * `nodes` drafted tokens stand in the cache at places base .. base + nodes - 1, behind what was committed (appended by cm_kv_append_run, say); token i
+ * follows parent[i] (host, -1 <= parent[i] < i; -1: the last committed token).  Its query sees the
  * committed tokens from `first` on (a multiple of t_kv, at most base), the drafted tokens it follows, and itself.
+ * Rejected tokens are dropped by cm_kv_take.  Those behind the last accepted one leave nothing; a place between accepted ones stays, empty, until it is
+ * filled again (cm_kv_seek), and would be seen with a score of zero.  cm_tree_set_empty says which places hold no token: the cm_tree_qk calls that follow
+ * on the object hide them from every query (a captured one, those set when it was captured).
  * Queries stand in the layout of H = group heads heads (t = t_kv / group tokens a ciphertext, as for cm_gqa_qk; group = 1: the cache's own heads): that
  * of the token at place a at residue a mod t, tokens node0 .. node0 + t - 1 in one ciphertext, one level above the cache.  At residues without one
  * of them stand the scores of a query that sees no drafted token.
@@ -588,6 +592,8 @@ cm_status cm_kv_append_run(cm_ctx *ctx, const cm_evk *evk, cm_kv *kv, const cm_r
 typedef struct cm_tree cm_tree;
 cm_status cm_tree_create(cm_ctx *ctx, const cm_kv *kv, int32_t group, double mask, double scale, const int64_t *coeffs, cm_tree **out);
 void cm_tree_destroy(cm_tree *tree);
+/* places: host [count], 0 .. dim t_kv - 1 (else CM_E_LAYOUT), in any order; what was set before is replaced (count = 0: none). */
+cm_status cm_tree_set_empty(cm_tree *tree, const int32_t *places, int32_t count);
 int32_t cm_tree_passes(const cm_tree *tree);
 int32_t cm_tree_steps(const cm_tree *tree, int32_t *steps, int32_t cap);
 cm_status cm_tree_qk(cm_ctx *ctx, const cm_evk *evk, const cm_tree *tree, const cm_kv *kv, const int32_t *parent, int32_t nodes, int32_t base, int32_t node0,

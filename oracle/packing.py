@@ -574,8 +574,9 @@ class RotaryTables:
         return out
 
 
-def tree_hidden(lay, group, parents, base, node0, first, delta):
-    """Slots (c, h, j) of pass delta's scores that take the mask's value: the query in slot (j - delta) mod t against place c t + j."""
+def tree_hidden(lay, group, parents, base, node0, first, delta, empty=()):
+    """Slots (c, h, j) of pass delta's scores that take the mask's value: the query in slot (j - delta) mod t against place c t + j;
+    empty: places without a token."""
     t, per = lay.t, lay.t // group
     follows = []
     for i, p in enumerate(parents):
@@ -586,5 +587,5 @@ def tree_hidden(lay, group, parents, base, node0, first, delta):
             place, u = c * t + j, (j - delta) % t % per
             node = node0 + (u - base - node0) % per
             seen = follows[node] if node < len(parents) else set()
-            out[c, :, j] = not (first // t <= c <= last and (place < base or place - base in seen))
+            out[c, :, j] = not (first // t <= c <= last and (place < base or place - base in seen) and place not in empty)
     return out

@@ -130,6 +130,7 @@ _SIGS = {
     "cm_kv_append_run": ([_vp, _vp, _vp, _vp, _i32, _P(cm_ct), _P(cm_ct), _vp], _i32),
     "cm_tree_create": ([_vp, _vp, _i32, _f64, _f64, _vp, _P(_vp)], _i32),
     "cm_tree_destroy": ([_vp], None),
+    "cm_tree_set_empty": ([_vp, _vp, _i32], _i32),
     "cm_tree_passes": ([_vp], _i32),
     "cm_tree_steps": ([_vp, _vp, _i32], _i32),
     "cm_tree_qk": ([_vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _P(cm_ct), _vp, _vp], _i32),
@@ -657,6 +658,11 @@ class Tree:
         c = _np(coeffs, np.int64) if coeffs is not None else None
         _chk(lib.cm_tree_create(ctx.h, kv.h, group, mask, scale, c.ctypes.data if c is not None else None, C.byref(self.h)))
         self.passes = lib.cm_tree_passes(self.h)
+
+    def set_empty(self, places):
+        """The places of the cache that hold no token (those that kv_take dropped among kept ones): no query sees them."""
+        p = _np(list(places), np.int32)
+        _chk(lib.cm_tree_set_empty(self.h, p.ctypes.data, p.size))
 
     def steps(self):
         n = lib.cm_tree_steps(self.h, None, 0)

@@ -7,8 +7,8 @@
 // passes, and ModDown and rescale in one.  The results of scores times V move back by t_kv - delta; as sums they stay on the
 // extended basis until all passes are in, so that one ModDown and rescale ends them.
 //
-// What a query may not see takes the mask's value: the drafted places that it does not follow, those behind the last one in its page, and whole
-// pages.  Every place is one slot row of the mask turned to its page and residue (an exact permutation), so a tree is data of the call.
+// What a query may not see takes the mask's value: the drafted places that it does not follow, those behind the last one in its page, places whose
+// token has been dropped, and whole pages.  Every place is one slot row of the mask turned to its page and residue (an exact permutation), so a tree is data of the call.
 #include <math.h>
 
 #include <algorithm>
@@ -26,6 +26,7 @@ struct cm_tree {
     u64 *d_one = nullptr;                     // [level][n]: the mask's value at row 0, residue 0
     u64 *d_unseen = nullptr;                  // [E - 1][level][n]: entry m - 1: in the rows m .. E - 1
     u64 *d_work = nullptr;
+    std::vector<u64> empty;                   // of every page, the places that hold no token (bits)
     KsManyTables tabs, q_tabs;                // raise of the second components of CM_KS_BATCH results, of the query's
     KvPasses passes;                          // for caches with the creating one's baby steps; others' passes run one at a time
 };
@@ -92,6 +93,7 @@ extern "C" cm_status cm_tree_create(cm_ctx *ctx, const cm_kv *kv, int32_t group,
     try {
         const int t = kv->t, H = kv->H, E = kv->E, level = kv->level, S = kv->S, n = ctx->n;
         tr->ctx = ctx, tr->H = H, tr->E = E, tr->t_kv = t, tr->G = group, tr->level = level, tr->scale = scale;
+        tr->empty.assign(E, 0);
         const size_t lw = (size_t)level * n;
         auto get = [&](u64 **p, size_t words) {
             if (status == CM_OK && words && hipMalloc((void **)p, words * 8) != hipSuccess) status = CM_E_NOMEM;
@@ -160,6 +162,13 @@ extern "C" cm_status cm_tree_create(cm_ctx *ctx, const cm_kv *kv, int32_t group,
     *out = tr;
     return CM_OK;
 }
+extern "C" cm_status cm_tree_set_empty(cm_tree *tr, const int32_t *places, int32_t count) {
+    if (!tr || count < 0 || (count && !places)) return CM_E_INVAL;
+    for (int i = 0; i < count; i++) if (places[i] < 0 || places[i] >= tr->E * tr->t_kv) return CM_E_LAYOUT;
+    std::fill(tr->empty.begin(), tr->empty.end(), 0);
+    for (int i = 0; i < count; i++) tr->empty[places[i] / tr->t_kv] |= 1ULL << (places[i] % tr->t_kv);
+    return CM_OK;
+}
 extern "C" int32_t cm_tree_passes(const cm_tree *tr) { return tr ? tr->t_kv : 0; }
 extern "C" int32_t cm_tree_steps(const cm_tree *tr, int32_t *steps, int32_t cap) {
     if (!tr) return 0;
@@ -210,6 +219,10 @@ extern "C" cm_status cm_tree_qk(cm_ctx *ctx, const cm_evk *evk, const cm_tree *t
         if (node < nodes)
             for (int k = node; k >= 0; k = parent[k]) seen[u][(start + k) / t] |= 1ULL << ((start + k) % t);
     }
+    // pages with places to hide: the tree's, and those before it that are seen and have places without a token
+    std::vector<int> masked;
+    for (int r = 0; r < rows; r++) masked.push_back(page + r);
+    for (int c = first / t; c < page; c++) if (tr->empty[c]) masked.push_back(c);
     hipStream_t st = (hipStream_t)stream;
     const KsLevel &up = ks_level(ctx, lv + 1);
     const size_t ctw = kv_ctw(kv);
@@ -255,17 +268,18 @@ extern "C" cm_status cm_tree_qk(cm_ctx *ctx, const cm_evk *evk, const cm_tree *t
             else if (kv->indexed) CMCHK(kv_sv(ctx, evk, kv, &in, &out, st, false, kv->d_x, false));
             else CMCHK(kv_qk(ctx, evk, kv, &in, &out, st, false));
         }
-        for (int r0 = 0; r0 < rows; r0 += TREE_ROWS) {
+        for (int r0 = 0; r0 < (int)masked.size(); r0 += TREE_ROWS) {
             TreeMask mk;
-            const int mr = std::min(TREE_ROWS, rows - r0);
+            const int mr = std::min(TREE_ROWS, (int)masked.size() - r0);
             for (int z = 0; z < CM_KS_BATCH; z++) mk.score[z] = scores[d0 + (z < m ? z : 0)].dev;
             for (int r = 0; r < TREE_ROWS; r++) {
-                mk.row[r] = r < mr ? (unsigned)rot_g(kv, -(long long)(page + r0 + r) * kv->H * t) : 1;
+                const int c = masked[r0 + (r < mr ? r : 0)];
+                mk.row[r] = r < mr ? (unsigned)rot_g(kv, -(long long)c * kv->H * t) : 1;
                 for (int z = 0; z < CM_KS_BATCH; z++) {
-                    u64 bits = 0;
-                    for (int j = 0; j < t && r < mr && z < m; j++) {
-                        const int place = (r0 + r) * t + j, u = (j - (d0 + z) + t) % t % per;
-                        if (place >= start && !(seen[u][r0 + r] >> j & 1)) bits |= 1ULL << j;
+                    u64 bits = r < mr && z < m ? tr->empty[c] : 0;
+                    for (int j = 0; j < t && r < mr && z < m && c >= page; j++) {
+                        const int place = (c - page) * t + j, u = (j - (d0 + z) + t) % t % per;
+                        if (place >= start && !(seen[u][c - page] >> j & 1)) bits |= 1ULL << j;
                     }
                     mk.bits[r][z] = bits;
                 }
