@@ -398,6 +398,7 @@ extern "C" cm_status cm_rotary_set(cm_ctx *ctx, cm_rotary *r, const int32_t *pos
                                1u | (i >= split ? 2u : 4u)});
     std::sort(entries.begin(), entries.end(), [](const RotEntry &a, const RotEntry &b) { return a.high < b.high; });
     std::vector<int32_t> kept(pos, pos + r->t);
+    r->set = false;                     // until everything has been enqueued: a call that fails leaves no positions
     auto batch = [&](size_t k0, int m) {
         RotBatch b;
         for (int k = 0; k < ROT_ENTRIES; k++) b.e[k] = k < m ? entries[k0 + k] : RotEntry{0, 0, 1, 0};
@@ -415,8 +416,10 @@ extern "C" cm_status cm_rotary_set(cm_ctx *ctx, cm_rotary *r, const int32_t *pos
         launch_ntt(ctx, r->d_v, r->d_mods, sets * r->parts * 2, true, st);
     }
     launch_rotary_fwd(ctx, r->d_p, r->d_v, r->ma, r->mb, r->inv, r->level, sets * r->parts, r->d_ext_mods, st);
+    auto enqueued = [] { RETURN_LAUNCH_STATUS(); };
+    CMCHK(enqueued());
     r->pos.swap(kept), r->split = split, r->set = true;
-    RETURN_LAUNCH_STATUS();
+    return CM_OK;
     CM_CATCH
 }
 cm_status rotary_sums(cm_ctx *ctx, const cm_evk *evk, const cm_rotary *r, int m, const u64 *const *xs, int first, int sets, u64 *us, bool *rows_done,
