@@ -545,9 +545,10 @@ int32_t cm_rotary_steps(const cm_rotary *rotary, int32_t *steps, int32_t cap);
 enum { CM_ROTARY_PLAIN = 0, CM_ROTARY_LINEAR = 1, CM_ROTARY_BASE = 2, CM_ROTARY_BANDS = 3 };
 cm_status cm_rotary_freqs(int32_t rot_dims, double base, int32_t scaling, const double *par, double *out);
 /* pos: host [t] (t = S / (heads dim), heads padded), the position of the token at every residue, -1 where there is none (read before the call
- * returns); outside -1 .. room - 1: CM_E_LAYOUT.  Where enqueuing fails (CM_E_HIP) the object has no positions until they are set again.  Enqueued: calls on the object that follow on the stream see it (a captured call sees what is set when
- * it is replayed; a captured cm_kv_append_run that passes into the next page needs the split it was captured with; a captured cm_rotary_set sets its
- * positions again at every replay, while cm_kv_append_run checks those of the call made last).  split: the residues below it belong
+ * returns); outside -1 .. room - 1: CM_E_LAYOUT.  Where enqueuing fails (CM_E_HIP) the object has no positions until they are set again.
+ * Enqueued: calls on the object that follow on the stream see it (a captured call sees what is set when it is replayed; a captured
+ * cm_kv_append_run that passes into the next page needs the split it was captured with; a captured cm_rotary_set sets its positions
+ * again at every replay, while cm_kv_append_run checks those of the call made last).  split: the residues below it belong
  * to the next page (cm_kv_append_run); 0: there is none.  cm_rotary_apply does not look at it. */
 cm_status cm_rotary_set(cm_ctx *ctx, cm_rotary *rotary, const int32_t *pos, int32_t split, void *stream);
 /* y[i] = x[i] turned, i < count <= CM_ROTARY_MAX (the queries and keys of a token, a group, a tree).  No y may share memory with an x or another y

@@ -656,6 +656,7 @@ class Tree:
     def __init__(self, ctx, kv, group, mask, scale, coeffs):
         self.ctx, self.h = ctx, _vp()
         c = _np(coeffs, np.int64) if coeffs is not None else None
+        assert c is None or (c.ndim == 2 and c.shape[1] == ctx.n and len(c) >= 2 * kv.residues)
         _chk(lib.cm_tree_create(ctx.h, kv.h, group, mask, scale, c.ctypes.data if c is not None else None, C.byref(self.h)))
         self.passes = lib.cm_tree_passes(self.h)
 
@@ -705,7 +706,7 @@ class KvCache:
                                  (CM_KV_UNROLLED_LADDERS if unrolled_ladders else 0) | (CM_KV_KEY_INDEX if key_index else 0),
                                  C.byref(self.h)))
         self._owner, self._words = _KvHandle(self.h), {}
-        self.dim, self.r_i, self.pages = dim, r_i or dim, -(-max_tokens // t)
+        self.dim, self.r_i, self.residues, self.pages = dim, r_i or dim, t, -(-max_tokens // t)
         if shared_dims != 1:
             self.set_shared_dims(shared_dims)
 
