@@ -346,15 +346,18 @@ bool tensor_sum_held(int n, int limbs, int cnt, int groups) {
 // The same sums for PASSES sets of ciphertexts a against one b: out[pass] and a[pass] stacked at out_pass and a_pass words.  A wave
 // owns a pass for 64 coefficients; the words of a group are staged in LDS for all of them, the next group's requested ahead.
 // Bound by HBM: with a launch a pass the cache was read once per pass of a grouped query.  Four passes over 128 ciphertexts of ten
-// limbs 4 x 317 -> 582 us, grouped-query attention at level 9 12860 -> 11640.  Eight (five limbs) 547 us, two launches of four 580: half of the traffic
+// limbs 4 x 280 -> 558 us; eight of five limbs 513 us, two launches of four 595, eight single ones 1119: half of the traffic
 // by then are the passes' own ciphertexts and sums.
 // The middle component is (a0 + a1)(b0 + b1) less the outer ones, three products a term for four.  Residues are centred, so |a|, |b| <= q/2 and the sums'
 // product is at most q^2: its quotient by q, below 2^50, is off by at most 3 2^-53 2^50 < 0.4 before it is rounded, which leaves |r| < 0.9 q; eight
-// terms and a renormalised sum stay below 7.8 q < 2^53.  Eight passes 540 -> 512 us, with words that are used once passed by the caches 504 (3.7 TB/s of the
-// traffic); grouped-query attention at level 9 11383 -> 11283.  108 registers because the
-// terms are worked on four at a time (sched_barrier); left to itself the compiler spills 187 of 128.
+// terms and a renormalised sum stay below 7.8 q < 2^53.  Words that are used once pass by the caches.  Four passes of ten limbs 604 -> 558 us so,
+// grouped-query attention at level 9 0.6 to 1.1 % faster, at levels 3 and 4 0.3 to 0.9 %.
+// HELD: launches that the chip holds at once (n = 4096), whose words lie in the caches and whose time is a wave's latency: four products a term, no centring, no
+// words past the caches.  Two passes over (16, 2) of eight limbs 21.5 us without, 12.7 with, four over (16, 4) 29.6 and 24.2; grouped-query
+// attention on the small ring 0.3 to 0.6 % faster.  Registers: 128 and 108 (two and four passes), without 154, 128 and 126 (eight).
+// The terms are worked on four at a time (sched_barrier): left to itself the compiler spills.
 #define TS_CO 64
-template <int PASSES>
+template <int PASSES, bool HELD>
 __global__ __launch_bounds__(64 * PASSES, 4) void k_tensor_sum_passes(u64 *__restrict__ out, const u64 *__restrict__ a, const u64 *__restrict__ b,
                                                                    const FpQ *__restrict__ fpq, int limbs, int n, int cnt, int groups, int gs, int ts,
                                                                    size_t out_pass, size_t a_pass) {
@@ -378,41 +381,53 @@ __global__ __launch_bounds__(64 * PASSES, 4) void k_tensor_sum_passes(u64 *__res
     double a0[TS_MAX_CNT], a1[TS_MAX_CNT];
 #pragma unroll
     for (int j = 0; j < TS_MAX_CNT; j++) {
-        a0[j] = j < cnt ? F.centred(__builtin_nontemporal_load(a + (size_t)j * 2 * cs + o)) : 0.0;
-        a1[j] = j < cnt ? F.centred(__builtin_nontemporal_load(a + (size_t)j * 2 * cs + cs + o)) : 0.0;
+        const u64 *w = a + (size_t)j * 2 * cs + o;
+        a0[j] = j >= cnt ? 0.0 : HELD ? MacFp::from_u64(w[0]) : F.centred(__builtin_nontemporal_load(w));
+        a1[j] = j >= cnt ? 0.0 : HELD ? MacFp::from_u64(w[cs]) : F.centred(__builtin_nontemporal_load(w + cs));
     }
     for (int z = 0; z < groups; z++) {
         // two buffers in turn: a wave that writes to one has passed the barrier behind the others' reads of it
         double *s = sb[z & 1] + co;
 #pragma unroll
-        for (int it = 0; it < ROWS; it++) s[(pass * ROWS + it) * TS_CO] = F.centred(r[it]);
+        for (int it = 0; it < ROWS; it++) s[(pass * ROWS + it) * TS_CO] = HELD ? MacFp::from_u64(r[it]) : F.centred(r[it]);
         __syncthreads();
         if (z + 1 < groups) request(z + 1);
         double d0 = 0.0, d1 = 0.0, d2 = 0.0;
 #pragma unroll
         for (int j = 0; j < TS_MAX_CNT; j++) {
-            const double b0 = s[2 * j * TS_CO], b1 = s[(2 * j + 1) * TS_CO], bs = b0 + b1;
-            d0 += F.mulmod(a0[j], b0, b0 * F.qinv);
-            d1 += F.mulmod(a0[j] + a1[j], bs, bs * F.qinv);
-            d2 += F.mulmod(a1[j], b1, b1 * F.qinv);
-            if ((j & 7) == 7) d0 = F.norm(d0), d1 = F.norm(d1), d2 = F.norm(d2);
+            const double b0 = s[2 * j * TS_CO], b1 = s[(2 * j + 1) * TS_CO], b0q = b0 * F.qinv, b1q = b1 * F.qinv;
+            d0 += F.mulmod(a0[j], b0, b0q);
+            d2 += F.mulmod(a1[j], b1, b1q);
+            if (HELD) {
+                d1 += F.mulmod(a0[j], b1, b1q) + F.mulmod(a1[j], b0, b0q);
+            } else {
+                const double bs = b0 + b1;
+                d1 += F.mulmod(a0[j] + a1[j], bs, bs * F.qinv);
+            }
+            if (HELD ? j & 1 : (j & 7) == 7) d0 = F.norm(d0), d1 = F.norm(d1), d2 = F.norm(d2);
             if ((j & 3) == 3) __builtin_amdgcn_sched_barrier(0);
         }
-        u64 *oz = out + (size_t)z * 3 * cs;
-        __builtin_nontemporal_store(F.canon(d0), oz + o);
-        __builtin_nontemporal_store(F.canon(d1 - d0 - d2), oz + o + cs);
-        __builtin_nontemporal_store(F.canon(d2), oz + o + 2 * cs);
+        u64 *oz = out + (size_t)z * 3 * cs + o;
+        if (HELD) {
+            oz[0] = F.canon(d0), oz[cs] = F.canon(d1), oz[2 * cs] = F.canon(d2);
+        } else {
+            __builtin_nontemporal_store(F.canon(d0), oz);
+            __builtin_nontemporal_store(F.canon(d1 - d0 - d2), oz + cs);
+            __builtin_nontemporal_store(F.canon(d2), oz + 2 * cs);
+        }
     }
 }
 // Where the joint launch is the faster way.  It always does the work of TS_MAX_CNT terms and its writes lie among its reads: with few
 // terms, and two passes with few groups, a launch a pass takes less.  Ten limbs at n = 65536, (cnt, groups), joint against single: two
-// passes (16, 8) 464 us, 565; (16, 4) 310, 330; (16, 1) 200, 132; (8, 8) 358, 316; (1, 2) 87, 63; four passes (16, 8) 585, 1129;
-// (16, 1) 234, 265; (8, 1) 141, 146 (13 limbs: 180, 179); (4, 1) 78, 70; (1, 2) 104, 127; (2, 4) 208, 235; (2, 8) 398, 407 (21 limbs: 818, 790).
+// passes (16, 8) 444 us, 565; (16, 4) 301, 333 (five limbs 154, 151); (16, 1) 203, 134; (8, 8) 335, 319; (1, 2) 84, 64; four passes (16, 8) 558, 1128;
+// (16, 1) 238, 265; (8, 1) 140, 146 (21 limbs 288, 286; five 73, 60); (4, 1) 93, 69; (1, 2) 99, 127; (2, 4) 196, 236; (2, 8) 368, 404 and (1, 8) 346, 384,
+// which stay single.  Eight passes take the line of four; joint against the faster of fours and single ones: (16, 8) 1032, 1127;
+// (16, 2) 546, 550 (21 limbs 1151, 1148); (16, 1) 474, 476; (8, 8) 831, 885; (8, 1) 280, 281; (4, 1) 188, 165; (2, 4) 367, 384; (2, 8) 677, 727; (1, 2) 192, 208.
 // A launch that the chip holds at once (n = 4096) is bound by its own latency, and calls of it are faster joint or equal: 8 limbs, four
-// passes 6 to 36 us joint, 16 to 110 single, two passes 6.5 to 32 against 8.5 to 51; grouped-query attention at level 3 with two passes over
-// (2, 8), (1, 8) and (4, 4) 912, 847 and 810 us against 938, 866 and 825, with 13 limbs within 0.3 % of each other.
+// passes 7 to 39 us joint, 17 to 110 single, two passes 7 to 32 against 10 to 52, eight 11 to 57 against 34 to 224.
+static bool tensor_passes_held(int n, int limbs) { return n / TS_CO * limbs <= 1024; }
 bool tensor_sum_passes_pays(int n, int limbs, int cnt, int groups, int passes) {
-    if (n / TS_CO * limbs <= 1024) return true;
+    if (tensor_passes_held(n, limbs)) return true;
     if (passes == 2) return cnt >= 16 && groups >= 4;
     return groups == 1 ? cnt >= 16 : cnt >= 4 || groups <= 4;
 }
@@ -426,15 +441,17 @@ void launch_tensor_sum_passes(cm_ctx *ctx, u64 *out, size_t out_pass, const u64 
                               int limbs, hipStream_t st, int gs, int ts) {
     Prof prof_(ctx, CM_K_ELEMENTWISE, 3 * limbs * groups * passes, st);
     const dim3 grid(ctx->n / TS_CO, limbs);
-    if (passes == TS_WIDE) {
-        hipLaunchKernelGGL(k_tensor_sum_passes<TS_WIDE>, grid, dim3(64 * TS_WIDE), 0, st, out, a, b, ctx->d_fpq, limbs, ctx->n, cnt, groups, gs, ts, out_pass, a_pass);
-        return;
-    }
-    if (passes == 2)
-        hipLaunchKernelGGL(k_tensor_sum_passes<2>, grid, dim3(128), 0, st, out, a, b, ctx->d_fpq, limbs, ctx->n, cnt, groups, gs, ts, out_pass, a_pass);
-    else
-        hipLaunchKernelGGL(k_tensor_sum_passes<TS_PASSES>, grid, dim3(64 * TS_PASSES), 0, st, out, a, b, ctx->d_fpq, limbs, ctx->n, cnt, groups, gs, ts,
-                           out_pass, a_pass);
+#define TS_LAUNCH(PASSES_, HELD_)                                                                                                                      \
+    hipLaunchKernelGGL((k_tensor_sum_passes<PASSES_, HELD_>), grid, dim3(64 * PASSES_), 0, st, out, a, b, ctx->d_fpq, limbs, ctx->n, cnt, groups, gs, ts, \
+                       out_pass, a_pass)
+    const bool held = tensor_passes_held(ctx->n, limbs);
+    if (passes == TS_WIDE) TS_LAUNCH(TS_WIDE, false);      // trees on the small ring 0.8 % faster to 0.6 % slower held
+    else if (passes == TS_PASSES) {
+        if (held) TS_LAUNCH(TS_PASSES, true);
+        else TS_LAUNCH(TS_PASSES, false);
+    } else if (held) TS_LAUNCH(2, true);
+    else TS_LAUNCH(2, false);
+#undef TS_LAUNCH
 }
 void launch_tensor_sum(cm_ctx *ctx, u64 *out, const u64 *a, const u64 *b, int cnt, int groups, int limbs, hipStream_t st,
                        int group_stride, int term_stride) {

@@ -175,7 +175,7 @@ cm_status kv_passes_run(cm_ctx *ctx, const cm_evk *evk, const cm_kv *kv, const K
             CMCHK(moddown_batch_turned(ctx, us, lv, f.n * m, adds, 1, gs, to, st));
         }
     }
-    // products with the cache: eight passes over 128 ciphertexts of five limbs in one launch 504 us, four at a time 540
+    // products with the cache: eight passes over 128 ciphertexts of five limbs in one launch 513 us, four at a time 595
     const int gs = array == kv->d_x ? 1 : r_i, ts = array == kv->d_x ? r_o : 1;
     for (int p = 0; p < m;) {
         u64 *sum = kp.sums + p * r_o * 3 * ln;
