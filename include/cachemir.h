@@ -525,8 +525,9 @@ cm_status cm_inner_rot_create(cm_ctx *ctx, int32_t t, int32_t delta, int32_t lev
  *   y = rescale(ModDown(p0 P x + p_up Rot'(x, step) + p_dn Rot'(x, -step))),
  * Rot' the hoisted rotation in the extended basis (cm_rotate_hoisted before its ModDown), step = heads t or, halves, rot_dims/2 heads t slots; where
  * 2 step = S both rotations are one, with the plaintext [V_up + V_dn].
- * Device memory: 8 R + 4 (high parts) polynomials of n words, up to 9 plaintexts on the extended basis, and the raised digits of up to eight ciphertexts
- * (256 MB of them at most, one at least). */
+ * Device memory: 8 R + 4 (high parts) polynomials of n words (n = 65536: 0.4 GB for a room of 2^12, 2.7 for 2^17, 26 for 2^24, whose 24577 entries are encoded
+ * on the host), up to 9 plaintexts on the extended basis, and the raised digits of up to eight ciphertexts (256 MB of them at most, one at least).
+ * An entry's precision is that of the smaller of q_level and m2. */
 typedef struct cm_rotary cm_rotary;
 enum { CM_ROTARY_HALVES = 1 };
 #define CM_ROTARY_ROOM (1 << 24)
@@ -567,18 +568,21 @@ cm_status cm_kv_append_run(cm_ctx *ctx, const cm_evk *evk, cm_kv *kv, const cm_r
 
 /* ---- attention of a tree of drafted tokens ----------------------------------------------------------------
  * `nodes` drafted tokens stand in the cache at places base .. base + nodes - 1, behind what was committed (appended by cm_kv_append_run, say); token i
- * follows parent[i] (host, -1 <= parent[i] < i; -1: the last committed token).  Its query sees the
- * committed tokens from `first` on (a multiple of t_kv, at most base), the drafted tokens it follows, and itself.
+ * follows parent[i] (host, -1 <= parent[i] < i; -1: the last committed token).  Its query sees the committed tokens from `first` on (a multiple of
+ * t_kv, at most base), the drafted tokens it follows, and itself.
  * Rejected tokens are dropped by cm_kv_take.  Those behind the last accepted one leave nothing; a place between accepted ones stays, empty, until it is
  * filled again (cm_kv_seek), and would be seen with a score of zero.  cm_tree_set_empty says which places hold no token: the cm_tree_qk calls that follow
  * on the object hide them from every query (a captured one, those set when it was captured).
  * Queries stand in the layout of H = group heads heads (t = t_kv / group tokens a ciphertext, as for cm_gqa_qk; group = 1: the cache's own heads): that
  * of the token at place a at residue a mod t, tokens node0 .. node0 + t - 1 in one ciphertext, one level above the cache.  At residues without one
  * of them stand the scores of a query that sees no drafted token.
- * There are t_kv passes (cm_tree_passes, at most 64): scores[delta] holds at slot (c, hk, j) the score of the query in slot (j - delta) mod t_kv of
- * its block against the token of place c t_kv + j, plus the mask's value (-24 leaves 4e-11 of an exponential) where it is not seen; all pages
- * outside first's .. the last drafted token's among it.  One level below the cache with the key index, else two.  Exactly: the query moved by delta
- * residues, formed as cm_rotary_apply does from the rotations by -delta and t_kv - delta and the plaintexts of the residues from delta on and of those below (delta = 0: a level drop), then cm_vmm_kv(CM_QK_GROUP), then the masks added.
+ * There are t_kv passes (cm_tree_passes, at most 64), whatever nodes is: with few tokens for the residues of a page one cm_vmm_kv a token
+ * takes less (about five tokens of eight residues, eighteen of 32, are even at n = 65536).
+ * scores[delta] holds at slot (c, hk, j) the score of the query in slot (j - delta) mod t_kv of its block against the token of place c t_kv + j, plus the
+ * mask's value (-24 leaves 4e-11 of an exponential) where it is not seen; all pages outside first's .. the last drafted token's among it.  One level
+ * below the cache with the key index, else two.  Exactly: the query moved by delta residues, formed as cm_rotary_apply does from the rotations by -delta
+ * and t_kv - delta and the plaintexts of the residues from delta on and of those below (delta = 0: a level drop), then cm_vmm_kv(CM_QK_GROUP), then
+ * the masks added.
  * cm_tree_sv: t_kv score ciphertexts in that layout at the cache's level times the values (cm_vmm_kv(CM_SV_GROUP)), moved back by t_kv - delta residues and
  * summed: the attention output in the queries' layout, two levels below.  The moved results are summed in the extended basis, with
  * one ModDown and rescale; the first one, which does not move, is dropped a level and added.
@@ -589,7 +593,8 @@ cm_status cm_kv_append_run(cm_ctx *ctx, const cm_evk *evk, cm_kv *kv, const cm_r
  * The calls use the work areas of the cache and of the object.  No score may share memory with q or another score (CM_E_INVAL).
  * Device memory: 4 (t_kv - 1) plaintexts on the extended basis, dim polynomials, and for up to eight passes taken together their baby steps, tensor sums and
  * digits (8 ciphertexts a baby step, 20 a giant step, up to 1 GB of digits; where that cannot be had or the cache has more than eight giant
- * steps, the passes run one at a time, with the same results). */
+ * steps or the level more than six digits, the passes run one at a time, with the same results).  32 x 128 with sixteen baby steps at n = 65536: 2.6 GB at
+ * level 4, 7.0 at level 12. */
 typedef struct cm_tree cm_tree;
 cm_status cm_tree_create(cm_ctx *ctx, const cm_kv *kv, int32_t group, double mask, double scale, const int64_t *coeffs, cm_tree **out);
 void cm_tree_destroy(cm_tree *tree);

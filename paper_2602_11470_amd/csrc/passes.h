@@ -11,7 +11,7 @@ struct KvPasses {
     u64 *acc = nullptr, *nxt = nullptr;            // [P] sums on the extended basis
     KsManyTables baby_tabs, relin_tabs, giant_tabs;
 };
-// room for turns of up to `passes` passes over caches of kv's shape and level; P = 0 where passes are taken one at a time instead (r_o > 8, no memory)
+// room for turns of up to `passes` passes over caches of kv's shape and level; P = 0 where passes are taken one at a time instead (r_o > 8, more than six digits, no memory)
 void kv_passes_create(cm_ctx *ctx, const cm_kv *kv, int passes, KvPasses *kp);
 void kv_passes_destroy(KvPasses *kp);
 inline bool kv_passes_fit(const KvPasses &kp, const cm_kv *kv) { return kp.P && kp.r_i == kv->r_i && kp.r_o == kv->r_o && kp.level == kv->level; }
