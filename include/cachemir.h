@@ -542,7 +542,8 @@ int32_t cm_rotary_steps(const cm_rotary *rotary, int32_t *steps, int32_t cap);
  *   CM_ROTARY_LINEAR  par = {factor}: every frequency over factor;
  *   CM_ROTARY_BASE    par = {factor}: base factor^(rot_dims/(rot_dims-2)) in the place of base;
  *   CM_ROTARY_BANDS   par = {factor, low, high, context}: those that turn at least `high` times over `context` positions as they are, those that turn
- *                     at most `low` times over factor, in between a mean of both, linear in the turns. */
+ *                     at most `low` times over factor, in between a mean of both, linear in the turns.
+ * Parameters that leave no finite frequency: CM_E_INVAL. */
 enum { CM_ROTARY_PLAIN = 0, CM_ROTARY_LINEAR = 1, CM_ROTARY_BASE = 2, CM_ROTARY_BANDS = 3 };
 cm_status cm_rotary_freqs(int32_t rot_dims, double base, int32_t scaling, const double *par, double *out);
 /* pos: host [t] (t = S / (heads dim), heads padded), the position of the token at every residue, -1 where there is none (read before the call

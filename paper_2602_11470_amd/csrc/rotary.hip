@@ -272,6 +272,7 @@ extern "C" cm_status cm_rotary_freqs(int32_t rot_dims, double base, int32_t scal
             const double keep = fmin(1.0, fmax(0.0, (par[3] * f / (2 * M_PI) - par[1]) / (par[2] - par[1])));
             f = keep * f + (1 - keep) * f / par[0];
         }
+        if (!isfinite(f)) return CM_E_INVAL;          // a factor too small for the base or the frequencies
         out[m] = f;
     }
     return CM_OK;
