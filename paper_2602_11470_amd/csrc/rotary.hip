@@ -28,7 +28,7 @@ static bool rot_pow2(int x) { return x > 0 && (x & (x - 1)) == 0; }
 
 // v[set][part][2][n] (+)= the products of the tables' entries; limb blockIdx.y under modulus ma or mb.  A lane has one word of all parts, so an entry's four
 // words are read once.  Bound by the gathers' latency, up to some ten entries by the launch: one token at n = 4096 3.6 us; at n = 65536 (4 MB an entry) a
-// group of eight 17 us, 21 tokens of a tree 25 us.
+// group of eight 12 us, 21 tokens of a tree 25 us.
 __global__ __launch_bounds__(ROT_TPB) void k_rotary_products(u64 *__restrict__ v, RotBatch b, int count, const u64 *__restrict__ low,
                                                              const u64 *__restrict__ still, const u64 *__restrict__ high, const ModC *__restrict__ modc,
                                                              int ma, int mb, int parts, int n, int logn, int accumulate) {
@@ -86,7 +86,7 @@ __global__ __launch_bounds__(ROT_TPB) void k_second(u64 *__restrict__ out, Secon
 // words, the sums reduced and multiplied by the item's plaintext.  All loads of an item are requested before the first is used (NB bounds its
 // digits), keys and plaintexts past the caches; one word a lane at n = 4096, where a launch is as long as a lane's chain (two items, one digit 5.7 -> 4.7 us, four digits 9.5 -> 6.3).
 // At n = 65536 bound by HBM and by drawing the keys' uniform halves: 14 items of two digits into seven outputs of ten limbs 77 us (0.3 GB: keys 147 MB,
-// plaintexts and outputs 73 MB each; 3.9 TB/s), two ciphertexts at level 3 17 us.  Rotating first, each to its ModDown, and multiplying then would write and
+// plaintexts and outputs 73 MB each; 3.9 TB/s), two ciphertexts at level 3 20 us.  Rotating first, each to its ModDown, and multiplying then would write and
 // read every rotation and end in as many ModDowns.
 // SPLIT waves share the items of 64 W words and join their sums in LDS (sums of more than two items at n = 4096, whose launch does not fill the
 // chip: 14 items of four digits 24.9 -> 10.1 us).  Z: outputs of a lane, whose items have the same keys.
