@@ -114,3 +114,38 @@ def test_a_tree(rings, index):
     for d in range(t):
         want = np.einsum("chje,ehj->chj", Kp.transpose(0, 2, 1, 3), np.roll(qs, d, axis=2)) - 24.0 * packing.tree_hidden(lay, 1, parents, base, 0, 0, d)
         assert np.abs(gctx.decrypt(sk, scores[d]).real.reshape(E, H, t) - want).max() < 2.0 ** -31 * 2
+
+
+@pytest.mark.parametrize("stored_a", [0, 1])
+def test_the_full_ring(stored_a):
+    """n = 65536, where other forms of the sums run (two words a lane): positions of two ciphertexts and hoisted rotations."""
+    from oracle import ckks, packing, vmm
+    from paper_2602_11470_amd import binding as B
+    n, level = 65536, 15
+    prm = params.Params(n=n, q=params.scan_primes(59, n, 16), p=params.scan_primes(61, n, 3), alpha=1, scale=2.0 ** 55, hamming=64)
+    gctx, octx = B.Context(n, 16, 3, 1, 59, 59, 61, 2.0 ** 55, hamming=64), ckks.Context(prm)
+    try:
+        assert [int(x) for x in gctx.moduli()] == prm.moduli
+        gctx.set_option(B.CM_OPT_EVK_STORED_A, stored_a)
+        tables = packing.RotaryTables(gctx.S, 32, 128, 3, rot=16)
+        mods, slots, low = [float(m) for m in gctx.moduli()], tables.slots(), 4 * tables.low + 1
+        coeffs = np.stack([gctx.encode_coeffs(v, mods[level]) for v in slots[:low]] + [gctx.encode_coeffs(v, mods[gctx.L + 2]) for v in slots[low:]])
+        rotary = gctx.rotary(32, 128, level, 3, rot_dims=16, coeffs=coeffs)
+        osk, gsk = octx.keygen_secret(3), gctx.keygen_secret(3)
+        steps = rotary.steps() + [5]
+        okeys, gkeys = octx.keygen_rotations(osk, steps, 4), gctx.keygen_rotations(gsk, steps, 4)
+        positions = [2, -1, 0, 1, 2, 2, -1, 1]
+        gctx.rotary_set(rotary, positions)
+        pts = vmm.rotary_plaintexts(octx, tables, coeffs, positions, level)
+        c = gctx.encode_coeffs(np.random.default_rng(1).normal(size=gctx.S), 2.0 ** 40)
+        o = octx.encrypt(osk, octx.pt_from_coeffs(c, level, 2.0 ** 40), 5)
+        g = gctx.encrypt(gsk, gctx.pt_from_coeffs(c, level, 2.0 ** 40), 5)
+        want = octx.canonical(vmm.rotary(octx, okeys, tables, o, pts))
+        for y in gctx.rotary_apply(gkeys, rotary, [g, g]):
+            np.testing.assert_array_equal(gctx.ct_export(y), want)
+        _same(octx, gctx, octx.rotate(o, 5, okeys), gctx.rotate(gkeys, g, 5))
+        h = octx.hoist(o)
+        for st, got in zip(steps, gctx.rotate_hoisted(gkeys, g, steps)):
+            _same(octx, gctx, octx.rotate_hoisted(o, h, st, okeys), got)
+    finally:
+        gctx.close()
